@@ -386,6 +386,78 @@ int mimose_op_layernorm_bwd_dropout(int32_t dtype, const void* dy, int32_t dy_f3
 int mimose_op_softmax_xent(int32_t dtype, void* logits, int64_t ld, const int32_t* labels,
                            float* row_loss, float* loss, int32_t T, int32_t V, int32_t n_valid,
                            void* stream);
+/*
+ * Losses on the log-probabilities of given tokens, as fine-tuning after the first training uses them.
+ * logits [T, ld] (first V columns valid), labels int32 [T]; with p = softmax of a row,
+ *     logp = log p[label],   d loss / d logits[v] = (d loss / d logp) (1[v = label] - p[v]).
+ * A label outside [0, V) leaves its row out: the logits are not read (they may hold anything), logp is
+ * 0, the gradient 0.  dlogits (optional, storage type, leading dimension ld): the gradient, zeros in
+ * columns >= V; NULL: the loss alone; logits itself: in place; any other overlap is INVALID_ARG.
+ * Logits of any alignment and ld; rows of whole 16-byte chunks on 16-byte addresses run fastest.
+ * workspace: device scratch of mimose_op_token_loss_workspace_bytes(T), 16-byte aligned; only the preference
+ * loss needs it, the others then split long rows where there are few (NULL: they do not).
+ * mimose_last_error(NULL) says why a call was refused.
+ */
+uint64_t mimose_op_token_loss_workspace_bytes(int32_t T);
+/* logp fp32[T] */
+int mimose_op_token_logprob(int32_t dtype, const void* logits, int64_t ld, const int32_t* labels,
+                            float* logp, int32_t T, int32_t V, void* workspace,
+                            uint64_t workspace_bytes, void* stream);
+/* Preference loss on pairs of sequences: sequence 2p is the one preferred in pair p, 2p+1 the other.
+ * ends: device int32 [2*pairs], ascending: sequence s has the rows ends[s-1] .. ends[s]-1 (it may have
+ * none; rows from the last end on belong to none and get no gradient); NULL: L rows each, T = 2*pairs*L.
+ *     seq_logp[s] = sum of logp over the sequence's scored rows
+ *     margin[p]   = beta ((seq_logp[2p] - ref_logp[2p]) - (seq_logp[2p+1] - ref_logp[2p+1]))
+ *     loss        = mean over p of (1 - smoothing) log(1 + exp(-margin)) + smoothing log(1 + exp(margin))
+ * logp fp32[T], seq_logp fp32[2*pairs], margin fp32[pairs], loss fp32 scalar are written, ref_logp
+ * fp32[2*pairs] (the reference model's seq_logp) is read; all on the device. */
+int mimose_op_preference_loss(int32_t dtype, const void* logits, int64_t ld, const int32_t* labels,
+                              const int32_t* ends, int32_t pairs, int32_t L, const float* ref_logp,
+                              float beta, float smoothing, void* dlogits, float* logp,
+                              float* seq_logp, float* margin, float* loss, int32_t T, int32_t V,
+                              void* workspace, uint64_t workspace_bytes, void* stream);
+/* Clipped policy loss with a KL term.  Per scored row, with r = exp(logp - old_logp), A its advantage,
+ * d = ref_logp - logp, w = scale * weight (weight NULL: scale alone):
+ *     gain = min(r A, clip(r, 1 - clip_low, 1 + clip_high) A),   kl = exp(d) - d - 1
+ *     loss = sum of w (kl_weight kl - gain)
+ * A token whose gain the clip holds back passes no gradient through r (one on the bound does).  A row
+ * with w = 0 is left out of the loss whatever its other numbers are.  ref_logp may be NULL when
+ * kl_weight is 0.  old_logp, ref_logp, advantage, weight: fp32[T]; rows fp32 [T,4] (16-byte aligned)
+ * receives logp, w (kl_weight kl - gain), w kl, and w where the clip held the gain back; stats fp32[3]
+ * the sums of the last three: loss, KL, clipped share. */
+int mimose_op_policy_loss(int32_t dtype, const void* logits, int64_t ld, const int32_t* labels,
+                          const float* old_logp, const float* ref_logp, const float* advantage,
+                          const float* weight, float scale, float clip_low, float clip_high,
+                          float kl_weight, void* dlogits, float* rows, float* stats, int32_t T,
+                          int32_t V, void* workspace, uint64_t workspace_bytes, void* stream);
+/*
+ * AdamW over many tensors in one launch, the update of mimose_optimizer_step for a caller's own tensors.
+ * Per tensor: n elements, fp32 master values, fp32 gradient, optionally a bf16 copy that receives the
+ * master rounded to nearest-even; decay != 0: weight decay applies.  state_bits 32: m, v fp32[n].
+ * state_bits 8: m, v uint8[n] hold e4m3 codes (OCP: four exponent bits, three of mantissa) and m_scale,
+ * v_scale fp32[ceil(n/256)] one factor for each 256 elements: the first moment is code * m_scale, the
+ * square root of the second code * v_scale.  A step decodes, updates and rounds them anew with a dither
+ * that is a function of element and step alone; the parameter moves by the unrounded moments.  All
+ * zeros is the initial state of either.  Pointers 16-byte aligned (scales 4); a tensor may have n = 0.
+ * mimose_op_adamw_table lays the list out in device memory of mimose_op_adamw_table_bytes (0: the list is
+ * refused) and waits for the copy; the table holds the addresses, not the tensors.  step counts from 1.
+ */
+typedef struct {
+  float* master; void* lowp; const float* grad;
+  void* m; void* v; float* m_scale; float* v_scale;   /* scales: state_bits 8 only */
+  int64_t n;
+  int32_t decay;
+  int32_t reserved_;                                  /* keep zero */
+} mimose_adamw_tensor;
+typedef struct {                                      /* plain data, filled by mimose_op_adamw_table */
+  void* device;
+  int32_t tensors, chunks, state_bits, reserved_;
+} mimose_adamw_table;
+uint64_t mimose_op_adamw_table_bytes(const mimose_adamw_tensor* tensors, int32_t count, int32_t state_bits);
+int mimose_op_adamw_table(const mimose_adamw_tensor* tensors, int32_t count, int32_t state_bits,
+                          void* device, uint64_t bytes, mimose_adamw_table* out, void* stream);
+int mimose_op_adamw_step(const mimose_adamw_table* table, const mimose_adamw_cfg* cfg, int64_t step,
+                         void* stream);
 /* sum_out (may be NULL when has_ln = 0) = tok_emb[id] + pos_emb[pos]; y = LN(sum) or sum. */
 int mimose_op_embed_fwd(int32_t dtype, const int32_t* ids, const void* tok_emb, const void* pos_emb,
                         const void* gamma, const void* beta, void* sum_out, void* y, int32_t B,

@@ -49,6 +49,15 @@ class mimose_adamw_cfg(C.Structure):
     _fields_ = [(n, C.c_float) for n in ("lr", "beta1", "beta2", "eps", "weight_decay")]
 
 
+class mimose_adamw_tensor(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("master", "lowp", "grad", "m", "v", "m_scale", "v_scale")] + \
+               [("n", C.c_int64), ("decay", C.c_int32), ("reserved_", C.c_int32)]
+
+
+class mimose_adamw_table(C.Structure):
+    _fields_ = [("device", C.c_void_p)] + [(n, C.c_int32) for n in ("tensors", "chunks", "state_bits", "reserved_")]
+
+
 class MimoseError(RuntimeError):
     def __init__(self, code: int, msg: str):
         super().__init__(f"libmimose: {ERR_NAMES.get(code, code)}: {msg}")
@@ -109,6 +118,15 @@ SIGNATURES = {
     "mimose_op_attention_bwd": (C.c_int, [_i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _i32, _f32,
                                           _u64, C.c_uint32, C.c_uint32, _vp]),
     "mimose_op_softmax_xent": (C.c_int, [_i32, _vp, _i64, _vp, _vp, _vp, _i32, _i32, _i32, _vp]),
+    "mimose_op_token_loss_workspace_bytes": (_u64, [_i32]),
+    "mimose_op_token_logprob": (C.c_int, [_i32, _vp, _i64, _vp, _vp, _i32, _i32, _vp, _u64, _vp]),
+    "mimose_op_preference_loss": (C.c_int, [_i32, _vp, _i64, _vp, _vp, _i32, _i32, _vp, _f32, _f32, _vp, _vp, _vp, _vp, _vp, _i32,
+                                            _i32, _vp, _u64, _vp]),
+    "mimose_op_policy_loss": (C.c_int, [_i32, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _f32, _f32, _f32, _f32, _vp, _vp, _vp, _i32, _i32,
+                                        _vp, _u64, _vp]),
+    "mimose_op_adamw_table_bytes": (_u64, [_vp, _i32, _i32]),
+    "mimose_op_adamw_table": (C.c_int, [_vp, _i32, _i32, _vp, _u64, C.POINTER(mimose_adamw_table), _vp]),
+    "mimose_op_adamw_step": (C.c_int, [C.POINTER(mimose_adamw_table), C.POINTER(mimose_adamw_cfg), _i64, _vp]),
     "mimose_op_embed_fwd": (C.c_int, [_i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _f32, _i32, _vp]),
     "mimose_op_embed_bwd": (C.c_int, [_i32, _vp, _vp, _vp, _vp, _i32, _vp, _vp, _i32, _i32, _i32, _i32, _vp]),
 }
@@ -408,6 +426,49 @@ def mimose_op_softmax_xent(dtype, logits, ld, labels, row_loss, loss, T, V, n_va
                                                  T, V, n_valid, _ptr(stream)))
 
 
+def mimose_op_token_loss_workspace_bytes(T: int) -> int:
+    return load_library().mimose_op_token_loss_workspace_bytes(T)
+
+
+def mimose_op_token_logprob(dtype, logits, ld, labels, logp, T, V, workspace=None, workspace_bytes=0, stream=None):
+    _check(load_library().mimose_op_token_logprob(dtype, _ptr(logits), ld, _ptr(labels), _ptr(logp), T, V, _ptr(workspace),
+                                                  workspace_bytes, _ptr(stream)))
+
+
+def mimose_op_preference_loss(dtype, logits, ld, labels, ends, pairs, L, ref_logp, beta, smoothing, dlogits, logp, seq_logp, margin,
+                              loss, T, V, workspace, workspace_bytes, stream=None):
+    _check(load_library().mimose_op_preference_loss(dtype, _ptr(logits), ld, _ptr(labels), _ptr(ends), pairs, L, _ptr(ref_logp), beta,
+                                                    smoothing, _ptr(dlogits), _ptr(logp), _ptr(seq_logp), _ptr(margin), _ptr(loss),
+                                                    T, V, _ptr(workspace), workspace_bytes, _ptr(stream)))
+
+
+def mimose_op_policy_loss(dtype, logits, ld, labels, old_logp, ref_logp, advantage, weight, scale, clip_low, clip_high, kl_weight,
+                          dlogits, rows, stats, T, V, workspace=None, workspace_bytes=0, stream=None):
+    _check(load_library().mimose_op_policy_loss(dtype, _ptr(logits), ld, _ptr(labels), _ptr(old_logp), _ptr(ref_logp),
+                                                _ptr(advantage), _ptr(weight), scale, clip_low, clip_high, kl_weight, _ptr(dlogits),
+                                                _ptr(rows), _ptr(stats), T, V, _ptr(workspace), workspace_bytes, _ptr(stream)))
+
+
+def mimose_op_adamw_table_bytes(tensors, state_bits: int) -> int:
+    """tensors: a ctypes array of mimose_adamw_tensor; raises where the library refuses the list."""
+    n = load_library().mimose_op_adamw_table_bytes(tensors, len(tensors), state_bits)
+    if not n:
+        _check(MIMOSE_ERR_INVALID_ARG)
+    return n
+
+
+def mimose_op_adamw_table(tensors, state_bits: int, device, nbytes: int, stream=None) -> mimose_adamw_table:
+    out = mimose_adamw_table()
+    _check(load_library().mimose_op_adamw_table(tensors, len(tensors), state_bits, _ptr(device), nbytes, C.byref(out), _ptr(stream)))
+    return out
+
+
+def mimose_op_adamw_step(table, step, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, stream=None):
+    """table: a mimose_adamw_table, or the AdamWTable that owns one."""
+    cfg = mimose_adamw_cfg(lr, beta1, beta2, eps, weight_decay)
+    _check(load_library().mimose_op_adamw_step(C.byref(getattr(table, "table", table)), C.byref(cfg), step, _ptr(stream)))
+
+
 def mimose_op_embed_fwd(dtype, ids, tok, pos, gamma, beta, sum_out, y, B, L, H, eps, has_ln, stream=None):
     _check(load_library().mimose_op_embed_fwd(dtype, _ptr(ids), _ptr(tok), _ptr(pos), _ptr(gamma), _ptr(beta),
                                               _ptr(sum_out), _ptr(y), B, L, H, eps, has_ln, _ptr(stream)))
@@ -418,7 +479,41 @@ def mimose_op_embed_bwd(dtype, d, ids, order, seg, n_seg, dtok, dpos, B, L, H, m
                                               _ptr(dpos), B, L, H, max_seq, _ptr(stream)))
 
 
-# ---------------------------------------------------------------- convenience wrapper
+# ---------------------------------------------------------------- convenience wrappers
+class AdamWTable:
+    """The device table of a list of tensors, for mimose_op_adamw_step; keeps the tensors alive.
+
+    tensors: dicts of device tensors master (fp32), grad (fp32), m, v (fp32, or one byte an element with state_bits 8), lowp
+    (bf16 or None), m_scale and v_scale (fp32, one entry for each 256 elements; state_bits 8), and decay (0 or 1)."""
+
+    BLOCK = 256   # elements that share a scale
+
+    def __init__(self, tensors, state_bits: int = 32, stream=None):
+        import torch
+        self.tensors = [dict(t) for t in tensors]
+        entries = (mimose_adamw_tensor * len(self.tensors))()
+        for e, t in zip(entries, self.tensors):
+            n = t["master"].numel()
+            sizes = {"master": (n, 4), "grad": (n, 4), "m": (n, state_bits // 8), "v": (n, state_bits // 8), "lowp": (n, 2)}
+            if state_bits == 8:
+                blocks = -(-n // self.BLOCK)
+                sizes.update(m_scale=(blocks, 4), v_scale=(blocks, 4))
+            for name, (count, size) in sizes.items():
+                x = t.get(name)
+                if x is None and name == "lowp":
+                    continue
+                if x is None or x.numel() != count or x.element_size() != size or not x.is_contiguous() or not x.is_cuda:
+                    raise ValueError(f"{name}: a contiguous device tensor of {count} elements of {size} bytes is required")
+                setattr(e, name, x.data_ptr() or None)
+            e.n, e.decay = n, int(bool(t.get("decay", 0)))
+        nbytes = mimose_op_adamw_table_bytes(entries, state_bits)
+        device = self.tensors[0]["master"].device
+        if stream is None:
+            stream = torch.cuda.current_stream(device).cuda_stream
+        self.memory = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        self.table = mimose_op_adamw_table(entries, state_bits, self.memory, nbytes, stream)
+
+
 class Mimose:
     """Owns a context and (optionally) the torch-allocated device arena behind it."""
 
@@ -513,4 +608,4 @@ class Mimose:
 
 
 __all__ = [n for n in dir() if n.startswith("mimose_") or n.startswith("MIMOSE_") or n.startswith("Q_")] + \
-          ["Mimose", "MimoseError", "make_cfg", "load_library", "LIB_PATH", "SIGNATURES", "ERR_NAMES", "KERNEL_CLASSES", "PLAN_MODES", "COLLECTORS"]
+          ["Mimose", "AdamWTable", "MimoseError", "make_cfg", "load_library", "LIB_PATH", "SIGNATURES", "ERR_NAMES", "KERNEL_CLASSES", "PLAN_MODES", "COLLECTORS"]

@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <cmath>
+
 namespace mk {
 
 enum DType : int { F32 = 0, BF16 = 1 };
@@ -146,6 +148,26 @@ void attention_bwd(int dtype, const void* qkv, const void* ctx, const void* dctx
                    const DropDesc& drop, hipStream_t st, hipEvent_t done = nullptr, int64_t rule_rows = 0);
 void softmax_xent(int dtype, void* logits, int64_t ld, const int32_t* labels, float* row_loss,
                   float* loss, int T, int V, int n_valid, hipStream_t st);
+// Losses on the log-probabilities of given tokens (token_loss.hip): rows of logits, a label for each; a label
+// outside [0, V) leaves its row out.  dlogits: the logits themselves, or memory that does not overlap them, or null.
+struct PreferenceArgs {
+  const int32_t* ends = nullptr;   // [2 * pairs] (device): sequence s has rows ends[s-1] .. ends[s] - 1; null: L rows each
+  int pairs = 0, L = 0;            // sequence 2p is the chosen one of pair p, 2p + 1 the rejected one
+  const float* ref_logp = nullptr; // [2 * pairs]
+  float beta = 0.f, smoothing = 0.f;
+  float *seq_logp = nullptr, *margin = nullptr, *loss = nullptr;   // [2 * pairs], [pairs], [1]
+};
+struct PolicyArgs {
+  const float *old_logp = nullptr, *ref_logp = nullptr, *advantage = nullptr, *weight = nullptr;   // [T]; ref_logp, weight may be null
+  float scale = 1.f, ratio_low = 0.f, ratio_high = 0.f, kl_weight = 0.f;
+  float *rows = nullptr, *stats = nullptr;                         // [T, 4], [3]
+};
+size_t token_loss_workspace_bytes(int T);
+void token_logprob(int dtype, const void* logits, int64_t ldl, const int32_t* labels, float* logp, int T, int V, void* workspace, hipStream_t st);
+void preference_loss(int dtype, const void* logits, int64_t ldl, const int32_t* labels, const PreferenceArgs& a, void* dlogits, float* logp,
+                     int T, int V, void* workspace, hipStream_t st);
+void policy_loss(int dtype, const void* logits, int64_t ldl, const int32_t* labels, const PolicyArgs& a, void* dlogits, int T, int V,
+                 void* workspace, hipStream_t st);
 // T: rows (B * L, or the real ones when rows.ends is given)
 void embed_fwd(int dtype, const int32_t* ids, const void* tok, const void* pos, const void* gamma,
                const void* beta, void* sum_out, void* y, const Rows& rows, int T, int B, int L, int H, float eps, int has_ln,
@@ -168,6 +190,21 @@ struct AdamChunk { int32_t tensor; int32_t pad; int64_t start; };
 struct AdamHyper { float lr, beta1, beta2, eps, weight_decay, inv_c1, inv_c2; };   // inv_c = 1 / (1 - beta^t)
 void adamw_update(int lowp_dtype, const AdamTensor* tensors, const AdamChunk* chunks, int n_chunks, AdamHyper h,
                   hipStream_t st);
+// numbers of update t >= 1, and what is wrong with the settings, or null
+inline AdamHyper adamw_hyper(float lr, float beta1, float beta2, float eps, float weight_decay, int64_t t) {
+  return {lr, beta1, beta2, eps, weight_decay, (float)(1.0 / (1.0 - std::pow((double)beta1, (double)t))),
+          (float)(1.0 / (1.0 - std::pow((double)beta2, (double)t)))};
+}
+inline const char* bad_adamw(float lr, float beta1, float beta2, float eps, float weight_decay) {
+  return !(lr >= 0.f) || !(beta1 >= 0.f && beta1 < 1.f) || !(beta2 >= 0.f && beta2 < 1.f) || !(eps >= 0.f) || !(weight_decay >= 0.f)
+             ? "hyper-parameters out of range" : nullptr;
+}
+// The same with moments in 8 bits (adamw8.hip): m and sqrt(v) as e4m3 codes, one fp32 scale for each kAdamBlock elements.
+constexpr int kAdamBlock = 256;
+struct Adam8Tensor {
+  float* master; void* lowp; const float* grad; uint8_t* m; uint8_t* v; float* m_scale; float* v_scale; int64_t n; int32_t decay; int32_t pad;
+};
+void adamw8_update(const Adam8Tensor* tensors, const AdamChunk* chunks, int n_chunks, AdamHyper h, int64_t step, hipStream_t st);
 // dst[n] = (resid ? resid[n] : 0) + mask * d.scale * src[n] with the mask of d (element i: word i % 4
 // of block i / 4).  dst and src have the storage type, or fp32 when io_f32; resid has the storage
 // type; dst may be src.  With rows.ends: element e of row r is the mask's element of that token in

@@ -1380,9 +1380,7 @@ int mimose_optimizer_init(mimose_ctx* c, const mimose_adamw_cfg* o) {
   if (!c || !o) return fail(c, MIMOSE_ERR_INVALID_ARG, "ctx and cfg must be given");
   if (c->opt_on) return fail(c, MIMOSE_ERR_INVALID_ARG, "the optimizer is already initialised");
   if (c->stats.steps != 0) return fail(c, MIMOSE_ERR_NOT_READY, "initialise the optimizer before the first step");
-  if (!(o->lr >= 0.f) || !(o->beta1 >= 0.f && o->beta1 < 1.f) || !(o->beta2 >= 0.f && o->beta2 < 1.f) || !(o->eps >= 0.f) ||
-      !(o->weight_decay >= 0.f))
-    return fail(c, MIMOSE_ERR_INVALID_ARG, "hyper-parameters out of range");
+  if (const char* why = mk::bad_adamw(o->lr, o->beta1, o->beta2, o->eps, o->weight_decay)) return fail(c, MIMOSE_ERR_INVALID_ARG, why);
   const bool narrow = c->cfg.dtype != mk::F32;
   std::vector<mk::AdamTensor> tens;
   std::vector<mk::AdamChunk> chunks;
@@ -1435,10 +1433,7 @@ int mimose_optimizer_step(mimose_ctx* c) {
   if (!c->has_device) return fail(c, MIMOSE_ERR_NOT_READY, "host-only context");
   if (c->stats.steps == 0) return fail(c, MIMOSE_ERR_NOT_READY, "no gradients yet: run a training step first");
   c->opt_t += 1;
-  mk::AdamHyper h;
-  h.lr = c->opt.lr; h.beta1 = c->opt.beta1; h.beta2 = c->opt.beta2; h.eps = c->opt.eps; h.weight_decay = c->opt.weight_decay;
-  h.inv_c1 = (float)(1.0 / (1.0 - std::pow((double)c->opt.beta1, (double)c->opt_t)));
-  h.inv_c2 = (float)(1.0 / (1.0 - std::pow((double)c->opt.beta2, (double)c->opt_t)));
+  const mk::AdamHyper h = mk::adamw_hyper(c->opt.lr, c->opt.beta1, c->opt.beta2, c->opt.eps, c->opt.weight_decay, (int64_t)c->opt_t);
   mk::adamw_update(c->cfg.dtype, c->opt_tensors, c->opt_chunks, c->opt_n_chunks, h, c->stream);
   if (hipGetLastError() != hipSuccess) return fail(c, MIMOSE_ERR_HIP, "update launch failed");
   return MIMOSE_OK;

@@ -1,7 +1,10 @@
 // C ABI of the kernel-level entry points: argument checks, then the launcher.
 #include <hip/hip_runtime.h>
 
+#include <cmath>
 #include <cstdio>
+#include <new>
+#include <vector>
 
 #include "../../include/mimose.h"
 #include "kernels.h"
@@ -13,6 +16,25 @@ namespace {
 inline bool bad_dtype(int d) { return d != 0 && d != 1; }
 inline int done() { return hipGetLastError() == hipSuccess ? MIMOSE_OK : MIMOSE_ERR_HIP; }
 inline bool bad_head(int d) { return d != 32 && d != 64; }
+// refuses a call: what mimose_last_error(NULL) returns says why
+int refuse(const char* op, const char* why) {
+  char buf[256];
+  snprintf(buf, sizeof buf, "%s: %s", op, why);
+  mimose_set_thread_error(buf);
+  return MIMOSE_ERR_INVALID_ARG;
+}
+// what is wrong with rows of logits and the gradient beside them, or null
+const char* bad_logits(int dtype, const void* logits, int64_t ld, const int32_t* labels, const void* dlogits, int T, int V) {
+  if (bad_dtype(dtype)) return "dtype must be 0 (fp32) or 1 (bf16)";
+  if (T < 0 || V < 1 || ld < V) return "T >= 0, V >= 1 and ld >= V required";
+  if (T > 0 && (!logits || !labels)) return "logits and labels must be given";
+  const uintptr_t es = mk::elt_size(dtype), a = (uintptr_t)logits, b = (uintptr_t)dlogits;
+  if (ld > INT64_MAX / 8 / (T > 0 ? T : 1)) return "ld too large";
+  if (a % es || b % es || (uintptr_t)labels % 4) return "a pointer is not aligned to its elements";
+  const uintptr_t bytes = T > 0 ? ((uintptr_t)(T - 1) * ld + ld) * es : 0;
+  if (b && a != b && a < b + bytes && b < a + bytes) return "dlogits overlaps the logits without being them";
+  return nullptr;
+}
 }  // namespace
 
 extern "C" {
@@ -157,6 +179,140 @@ int mimose_op_softmax_xent(int32_t dtype, void* logits, int64_t ld, const int32_
                            float* loss, int32_t T, int32_t V, int32_t n_valid, void* stream) {
   if (bad_dtype(dtype) || !logits || !labels || !row_loss || !loss || T < 0 || V < 1 || ld < V) return MIMOSE_ERR_INVALID_ARG;
   mk::softmax_xent(dtype, logits, ld, labels, row_loss, loss, T, V, n_valid, (hipStream_t)stream);
+  return done();
+}
+
+uint64_t mimose_op_token_loss_workspace_bytes(int32_t T) { return mk::token_loss_workspace_bytes(T); }
+
+int mimose_op_token_logprob(int32_t dtype, const void* logits, int64_t ld, const int32_t* labels, float* logp, int32_t T, int32_t V,
+                            void* workspace, uint64_t workspace_bytes, void* stream) {
+  const char* const op = "mimose_op_token_logprob";
+  if (const char* why = bad_logits(dtype, logits, ld, labels, nullptr, T, V)) return refuse(op, why);
+  if (T == 0) return MIMOSE_OK;
+  if (!logp) return refuse(op, "logp must be given");
+  if (workspace && ((uintptr_t)workspace & 15)) return refuse(op, "workspace must be 16-byte aligned");
+  if (workspace && workspace_bytes < mk::token_loss_workspace_bytes(T)) return refuse(op, "workspace smaller than mimose_op_token_loss_workspace_bytes");
+  mk::token_logprob(dtype, logits, ld, labels, logp, T, V, workspace, (hipStream_t)stream);
+  return done();
+}
+
+int mimose_op_preference_loss(int32_t dtype, const void* logits, int64_t ld, const int32_t* labels, const int32_t* ends, int32_t pairs,
+                              int32_t L, const float* ref_logp, float beta, float smoothing, void* dlogits, float* logp, float* seq_logp,
+                              float* margin, float* loss, int32_t T, int32_t V, void* workspace, uint64_t workspace_bytes, void* stream) {
+  const char* const op = "mimose_op_preference_loss";
+  if (const char* why = bad_logits(dtype, logits, ld, labels, dlogits, T, V)) return refuse(op, why);
+  if (pairs < 1 || pairs > (1 << 24)) return refuse(op, "1 to 2^24 pairs required");
+  if (!ends && (L < 0 || (int64_t)2 * pairs * L != T)) return refuse(op, "without ends, T must be 2 * pairs * L");
+  if (!ref_logp || !seq_logp || !margin || !loss || (T > 0 && !logp)) return refuse(op, "ref_logp, logp, seq_logp, margin and loss must be given");
+  if (!std::isfinite(beta) || !(smoothing >= 0.f && smoothing <= 1.f)) return refuse(op, "beta must be finite, smoothing in [0, 1]");
+  if (T > 0 && (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < mk::token_loss_workspace_bytes(T)))
+    return refuse(op, "workspace must be 16-byte aligned and of mimose_op_token_loss_workspace_bytes");
+  mk::PreferenceArgs a;
+  a.ends = ends; a.pairs = pairs; a.L = L; a.ref_logp = ref_logp; a.beta = beta; a.smoothing = smoothing;
+  a.seq_logp = seq_logp; a.margin = margin; a.loss = loss;
+  mk::preference_loss(dtype, logits, ld, labels, a, dlogits, logp, T, V, workspace, (hipStream_t)stream);
+  return done();
+}
+
+int mimose_op_policy_loss(int32_t dtype, const void* logits, int64_t ld, const int32_t* labels, const float* old_logp,
+                          const float* ref_logp, const float* advantage, const float* weight, float scale, float clip_low,
+                          float clip_high, float kl_weight, void* dlogits, float* rows, float* stats, int32_t T, int32_t V,
+                          void* workspace, uint64_t workspace_bytes, void* stream) {
+  const char* const op = "mimose_op_policy_loss";
+  if (const char* why = bad_logits(dtype, logits, ld, labels, dlogits, T, V)) return refuse(op, why);
+  if (!stats || (T > 0 && (!old_logp || !advantage || !rows))) return refuse(op, "old_logp, advantage, rows and stats must be given");
+  if ((uintptr_t)rows & 15) return refuse(op, "rows must be 16-byte aligned");
+  if (!std::isfinite(scale)) return refuse(op, "scale must be finite");
+  if (!(clip_low >= 0.f && clip_low <= 1.f) || !(clip_high >= 0.f)) return refuse(op, "clip_low must lie in [0, 1], clip_high must be 0 or more");
+  if (!std::isfinite(kl_weight) || kl_weight < 0.f) return refuse(op, "kl_weight must be finite and 0 or more");
+  if (kl_weight > 0.f && !ref_logp) return refuse(op, "the KL term needs ref_logp");
+  if (workspace && ((uintptr_t)workspace & 15)) return refuse(op, "workspace must be 16-byte aligned");
+  if (workspace && workspace_bytes < mk::token_loss_workspace_bytes(T)) return refuse(op, "workspace smaller than mimose_op_token_loss_workspace_bytes");
+  mk::PolicyArgs a;
+  a.old_logp = old_logp; a.ref_logp = ref_logp; a.advantage = advantage; a.weight = weight;
+  a.scale = scale; a.ratio_low = 1.f - clip_low; a.ratio_high = 1.f + clip_high; a.kl_weight = kl_weight;
+  a.rows = rows; a.stats = stats;
+  mk::policy_loss(dtype, logits, ld, labels, a, dlogits, T, V, workspace, (hipStream_t)stream);
+  return done();
+}
+
+// chunks of a list of tensors, or -1 with what is wrong with it
+static int64_t adamw_chunks(const mimose_adamw_tensor* t, int32_t count, int32_t state_bits, const char** why) {
+  *why = nullptr;
+  if (!t || count < 1) *why = "at least one tensor required";
+  else if (state_bits != 8 && state_bits != 32) *why = "state_bits must be 8 or 32";
+  if (*why) return -1;
+  int64_t chunks = 0;
+  for (int32_t i = 0; i < count; ++i) {
+    if (t[i].n < 0) *why = "a tensor has a negative element count";
+    else if (t[i].n == 0) continue;
+    else if (!t[i].master || !t[i].grad || !t[i].m || !t[i].v) *why = "master, grad, m and v of a tensor must be given";
+    else if (((uintptr_t)t[i].master | (uintptr_t)t[i].grad | (uintptr_t)t[i].m | (uintptr_t)t[i].v | (uintptr_t)t[i].lowp) & 15)
+      *why = "master, lowp, grad, m and v of a tensor must be 16-byte aligned";
+    else if (state_bits == 8 && (!t[i].m_scale || !t[i].v_scale || (((uintptr_t)t[i].m_scale | (uintptr_t)t[i].v_scale) & 3)))
+      *why = "states in 8 bits need m_scale and v_scale, aligned to their elements";
+    if (*why) return -1;
+    chunks += (t[i].n + mk::kAdamChunk - 1) / mk::kAdamChunk;
+    if (chunks >= (1 << 20)) { *why = "too many elements: 2^34 at most"; return -1; }   // a grid's threads are counted in 32 bits
+  }
+  return chunks;
+}
+static uint64_t adamw_entries_bytes(int32_t count, int32_t state_bits) {
+  const uint64_t e = state_bits == 8 ? sizeof(mk::Adam8Tensor) : sizeof(mk::AdamTensor);
+  return (e * (uint64_t)count + 255) / 256 * 256;
+}
+
+uint64_t mimose_op_adamw_table_bytes(const mimose_adamw_tensor* tensors, int32_t count, int32_t state_bits) {
+  const char* why;
+  const int64_t chunks = adamw_chunks(tensors, count, state_bits, &why);
+  if (chunks < 0) { refuse("mimose_op_adamw_table_bytes", why); return 0; }
+  return adamw_entries_bytes(count, state_bits) + (uint64_t)(chunks > 0 ? chunks : 1) * sizeof(mk::AdamChunk);
+}
+
+int mimose_op_adamw_table(const mimose_adamw_tensor* tensors, int32_t count, int32_t state_bits, void* device, uint64_t bytes,
+                          mimose_adamw_table* out, void* stream) {
+  const char* const op = "mimose_op_adamw_table";
+  const char* why;
+  const int64_t chunks = adamw_chunks(tensors, count, state_bits, &why);
+  if (chunks < 0) return refuse(op, why);
+  const uint64_t entries = adamw_entries_bytes(count, state_bits), need = entries + (uint64_t)(chunks > 0 ? chunks : 1) * sizeof(mk::AdamChunk);
+  if (!out || !device || ((uintptr_t)device & 15) || bytes < need)
+    return refuse(op, "out and 16-byte aligned device memory of mimose_op_adamw_table_bytes must be given");
+  try {
+    std::vector<char> host(need, 0);
+    mk::AdamChunk* c = (mk::AdamChunk*)(host.data() + entries);
+    for (int32_t i = 0; i < count; ++i) {
+      const mimose_adamw_tensor& t = tensors[i];
+      if (state_bits == 8)
+        ((mk::Adam8Tensor*)host.data())[i] = {t.master, t.lowp, t.grad, (uint8_t*)t.m, (uint8_t*)t.v, t.m_scale, t.v_scale, t.n, t.decay != 0, 0};
+      else
+        ((mk::AdamTensor*)host.data())[i] = {t.master, t.lowp, t.grad, (float*)t.m, (float*)t.v, t.n, t.decay != 0, 0};
+      for (int64_t s = 0; s < t.n; s += mk::kAdamChunk) *c++ = mk::AdamChunk{i, 0, s};
+    }
+    if (hipMemcpyAsync(device, host.data(), need, hipMemcpyHostToDevice, (hipStream_t)stream) != hipSuccess ||
+        hipStreamSynchronize((hipStream_t)stream) != hipSuccess) {
+      (void)hipGetLastError();
+      mimose_set_thread_error("mimose_op_adamw_table: copy to the device failed");
+      return MIMOSE_ERR_HIP;
+    }
+  } catch (const std::bad_alloc&) {
+    return refuse(op, "no host memory for the table");
+  }
+  out->device = device; out->tensors = count; out->chunks = (int32_t)chunks; out->state_bits = state_bits; out->reserved_ = 0;
+  return MIMOSE_OK;
+}
+
+int mimose_op_adamw_step(const mimose_adamw_table* table, const mimose_adamw_cfg* cfg, int64_t step, void* stream) {
+  const char* const op = "mimose_op_adamw_step";
+  if (!table || !table->device || table->tensors < 1 || table->chunks < 0 || table->chunks >= (1 << 20) ||
+      (table->state_bits != 8 && table->state_bits != 32) || !cfg)
+    return refuse(op, "a table of mimose_op_adamw_table and cfg must be given");
+  if (const char* why = mk::bad_adamw(cfg->lr, cfg->beta1, cfg->beta2, cfg->eps, cfg->weight_decay)) return refuse(op, why);
+  if (step < 1) return refuse(op, "updates are numbered from 1");
+  const mk::AdamHyper h = mk::adamw_hyper(cfg->lr, cfg->beta1, cfg->beta2, cfg->eps, cfg->weight_decay, step);
+  const mk::AdamChunk* chunks = (const mk::AdamChunk*)((const char*)table->device + adamw_entries_bytes(table->tensors, table->state_bits));
+  if (table->state_bits == 8) mk::adamw8_update((const mk::Adam8Tensor*)table->device, chunks, table->chunks, h, step, (hipStream_t)stream);
+  else mk::adamw_update(mk::BF16, (const mk::AdamTensor*)table->device, chunks, table->chunks, h, (hipStream_t)stream);
   return done();
 }
 

@@ -1,0 +1,193 @@
+"""The update over a caller's tensors, moments in 8 bits or in 32, against the fp64 oracles."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2209_02478_amd as mi
+from gpu_util import DEV, sync
+from oracle import optimizer8 as o8
+from oracle import model as om
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+HYPER = dict(lr=2e-3, beta1=0.9, beta2=0.98, eps=1e-7, weight_decay=0.05)
+HYPER32 = {k: float(np.float32(v)) for k, v in HYPER.items()}          # as the library receives them
+
+
+def tensors(counts, seed, lowp, special=False):
+    rng = np.random.default_rng(seed)
+    out = []
+    for k, n in enumerate(counts):
+        nb = -(-n // 256)
+        size = np.repeat(np.exp(rng.standard_normal(nb) * 3 - 6), 256)[:n]
+        t = dict(p=rng.standard_normal(n) * 0.02, g=rng.standard_normal(n) * size, m=rng.integers(0, 127, n), v=rng.integers(0, 127, n),
+                 ms=np.exp(rng.standard_normal(nb) - 12), vs=np.exp(rng.standard_normal(nb) - 10), decay=k % 2)
+        t["m"] = t["m"] + 128 * (rng.random(n) < 0.5)
+        if k % 3 == 1:                             # before the first update, and blocks without a gradient
+            t["m"][:], t["v"][:], t["ms"][:], t["vs"][:] = 0, 0, 0, 0
+            t["g"][:256] = 0
+        if special and n > 600:
+            t["g"][[3, 300, 301]] = np.inf, -np.inf, np.nan
+            t["g"][512:520] = 1e-15                # beside values of ordinary size: no code but the smallest
+        out.append({key: (np.asarray(val, np.uint8) if key in "mv" else np.asarray(val, np.float32) if key != "decay" else val)
+                    for key, val in t.items()})
+    return out
+
+
+def device(ts, lowp):
+    out = []
+    for t in ts:
+        d = {k: torch.tensor(t[a], device=DEV) for k, a in (("master", "p"), ("grad", "g"), ("m", "m"), ("v", "v"), ("m_scale", "ms"),
+                                                           ("v_scale", "vs"))}
+        d["lowp"] = torch.full((len(t["p"]),), 9.0, dtype=torch.bfloat16, device=DEV) if lowp else None
+        d["decay"] = t["decay"]
+        out.append(d)
+    return out
+
+
+def check(t, d, step, lowp):
+    n = len(t["p"])
+    with np.errstate(all="ignore"):
+        want = o8.step(*(t[k].astype(np.float64) for k in "pg"), t["m"], t["v"], t["ms"], t["vs"], step, **HYPER32)
+        if not t["decay"]:
+            want["p"] = o8.step(*(t[k].astype(np.float64) for k in "pg"), t["m"], t["v"], t["ms"], t["vs"], step,
+                                **dict(HYPER32, weight_decay=0.0))["p"]
+    fine = np.isfinite(want["p"])
+    got = d["master"].cpu().numpy()
+    # the moments lose a few roundings each (the first may cancel: relative to its terms), the step a dozen
+    terms = np.abs(o8.decode(t["m"]) * np.repeat(t["ms"].astype(np.float64), 256)[:n]) + np.abs(t["g"])
+    size = HYPER["lr"] * terms / (1 - HYPER32["beta1"] ** step) / (want["root"] / np.sqrt(1 - HYPER32["beta2"] ** step) + HYPER["eps"])
+    with np.errstate(invalid="ignore"):
+        err = np.abs(got - want["p"])
+        assert np.all(err[fine] <= (16 * U * size + 2 * U * np.abs(t["p"]))[fine] + 1e-30)
+    assert np.array_equal(np.isnan(got), np.isnan(want["p"]))
+    if lowp:
+        assert np.array_equal(d["lowp"].float().cpu().numpy()[fine], om.round_to_bf16(got)[fine])
+    for name, raw in (("m", "moment"), ("v", "root")):
+        codes, s = d[name].cpu().numpy(), d[name + "_scale"].cpu().numpy().astype(np.float64)
+        # a scale is one of the moments and two roundings; a code may fall to the other side where q is within its error of a whole number
+        blocks = np.repeat(s, 256)[:n]
+        np.testing.assert_allclose(s, want[name + "_scale"], rtol=16 * U if name == "v" else 1e-4)
+        x = want[raw]
+        ok = np.isfinite(x)
+        assert np.all((codes[~ok] & 127) == 127)
+        a = np.abs(x[ok])
+        with np.errstate(divide="ignore"):
+            space = 2.0 ** (np.floor(np.log2(np.clip(a / blocks[ok], 2.0 ** -6, 448))) - 3)
+        u = o8.dither(n, o8.K_M if name == "m" else o8.K_V, step)[ok]
+        # (twice that, because below a power of two the spacing is half of the one above it)
+        rel = 2 * (16 * U * (terms[ok] if name == "m" else a) + 8 * U * a) / blocks[ok] / space
+        low, high = (np.minimum(np.floor(a / blocks[ok] / space + u + sign * rel) * space, 448) for sign in (-1, 1))
+        held = np.abs(o8.decode(codes[ok]))
+        if name == "v":
+            low, high = (np.where((z == 0) & (a > 0), 2.0 ** -9, z) for z in (low, high))
+        assert np.all((held >= low) & (held <= high)), name
+        moved = held > 0
+        assert np.array_equal(np.signbit(o8.decode(codes[ok]))[moved], (x[ok] < 0)[moved])
+
+
+@pytest.mark.parametrize("lowp", [False, True])
+@pytest.mark.parametrize("step", [1, 2, 1000, 2 ** 31 + 7])
+def test_8_bits_against_the_oracle(lowp, step):
+    counts = [1, 3, 4, 255, 256, 257, 0, 1023, 16384, 16385, 40001, 65536, 5]
+    ts = tensors(counts, step % 97, lowp)
+    ds = device(ts, lowp)
+    mi.mimose_op_adamw_step(mi.AdamWTable(ds, 8), step, **HYPER)
+    sync()
+    for t, d in zip(ts, ds):
+        if len(t["p"]):
+            check(t, d, step, lowp)
+
+
+def test_8_bits_with_gradients_that_are_not_finite():
+    ts = tensors([700, 5000], 7, True, special=True)
+    ds = device(ts, True)
+    mi.mimose_op_adamw_step(mi.AdamWTable(ds, 8), 5, **HYPER)
+    sync()
+    for t, d in zip(ts, ds):
+        check(t, d, 5, True)
+        assert np.isnan(d["master"].cpu().numpy()[[3, 300, 301]]).all()
+        assert torch.isfinite(d["m_scale"]).all() and torch.isfinite(d["v_scale"]).all()
+        assert (d["v"][512:520] > 0).all()
+
+
+def test_memory_around_the_tensors_is_left_alone():
+    n, guard = 16384 + 300, 64
+    for bits in (8, 32):
+        bufs = {k: torch.full((n + 2 * guard,), 7, dtype=dt, device=DEV)
+                for k, dt in (("master", torch.float32), ("grad", torch.float32), ("lowp", torch.bfloat16),
+                              ("m", torch.uint8 if bits == 8 else torch.float32), ("v", torch.uint8 if bits == 8 else torch.float32))}
+        sc = {k: torch.full((66 + 2 * guard,), 7.0, device=DEV) for k in ("m_scale", "v_scale")}
+        part = {k: b[guard:guard + n] for k, b in bufs.items()}
+        part |= {k: b[guard:guard + 66] for k, b in sc.items()} if bits == 8 else {}
+        mi.mimose_op_adamw_step(mi.AdamWTable([part], bits), 3, **HYPER)
+        sync()
+        for k, b in list(bufs.items()) + list(sc.items()):
+            inner = 66 if k in sc else n
+            assert (b[:guard] == 7).all() and (b[guard + inner:] == 7).all(), k
+        assert (part["master"] != 7).all()
+
+
+@pytest.mark.parametrize("lowp", [False, True])
+def test_32_bits_against_the_formula(lowp):
+    rng = np.random.default_rng(3)
+    counts = [1, 5, 16384, 16390, 70001]
+    host = [dict(p=rng.standard_normal(n), g=rng.standard_normal(n), m=rng.standard_normal(n) * 0.1, v=rng.random(n)) for n in counts]
+    host = [{k: a.astype(np.float32) for k, a in t.items()} for t in host]
+    ds = [dict(master=torch.tensor(t["p"], device=DEV), grad=torch.tensor(t["g"], device=DEV), m=torch.tensor(t["m"], device=DEV),
+               v=torch.tensor(t["v"], device=DEV), lowp=torch.empty(len(t["p"]), dtype=torch.bfloat16, device=DEV) if lowp else None,
+               decay=k % 2) for k, t in enumerate(host)]
+    mi.mimose_op_adamw_step(mi.AdamWTable(ds, 32), 7, **HYPER)
+    sync()
+    h = HYPER32
+    for k, (t, d) in enumerate(zip(host, ds)):
+        p, g, m, v = (t[x].astype(np.float64) for x in "pgmv")
+        m = h["beta1"] * m + (1 - h["beta1"]) * g
+        v = h["beta2"] * v + (1 - h["beta2"]) * g * g
+        q = p - h["lr"] * (m / (1 - h["beta1"] ** 7) / (np.sqrt(v / (1 - h["beta2"] ** 7)) + h["eps"]) + (k % 2) * h["weight_decay"] * p)
+        np.testing.assert_allclose(d["m"].cpu().numpy(), m, rtol=0, atol=4 * U * (np.abs(g).max() + 1))
+        np.testing.assert_allclose(d["v"].cpu().numpy(), v, rtol=8 * U)
+        np.testing.assert_allclose(d["master"].cpu().numpy(), q, rtol=2 * U, atol=1e-6 * h["lr"] * 100)
+        if lowp:
+            assert np.array_equal(d["lowp"].float().cpu().numpy(), om.round_to_bf16(d["master"].cpu().numpy()))
+
+
+def test_8_bits_follows_32_over_many_updates():
+    """300 updates of a noisy quadratic bowl: the two end at losses within a tenth of the distance they came."""
+    n = 4096
+    rng = np.random.default_rng(11)
+    goal = torch.tensor(rng.standard_normal(n).astype(np.float32), device=DEV)
+    curve = torch.tensor(np.exp(rng.standard_normal(n) * 2).astype(np.float32), device=DEV)
+    noise = torch.tensor(rng.standard_normal((300, n)).astype(np.float32) * 0.05, device=DEV)
+    ends = {}
+    for bits in (8, 32):
+        z = lambda k, dt: torch.zeros(k, dtype=dt, device=DEV)  # noqa: E731
+        dt = torch.uint8 if bits == 8 else torch.float32
+        t = dict(master=z(n, torch.float32), grad=z(n, torch.float32), m=z(n, dt), v=z(n, dt), m_scale=z(16, torch.float32),
+                 v_scale=z(16, torch.float32))
+        table = mi.AdamWTable([t], bits)
+        for k in range(300):
+            t["grad"].copy_(curve * (t["master"] - goal + noise[k]))
+            mi.mimose_op_adamw_step(table, k + 1, lr=1e-2, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0)
+        ends[bits] = float((t["master"] - goal).square().mean())
+    start = float(goal.square().mean())
+    assert ends[32] < 0.1 * start and abs(ends[8] - ends[32]) < 0.1 * (start - ends[32]), (start, ends)
+
+
+def test_calls_in_a_graph_and_repeated_are_the_same():
+    ts = tensors([5000, 70001], 21, True)
+    a, b = device(ts, True), device(ts, True)
+    ta, tb = mi.AdamWTable(a, 8), mi.AdamWTable(b, 8)
+    graph = torch.cuda.CUDAGraph()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=side):
+        mi.mimose_op_adamw_step(ta, 4, **HYPER, stream=side.cuda_stream)
+    for _ in range(4):
+        graph.replay()
+        mi.mimose_op_adamw_step(tb, 4, **HYPER)
+        sync()
+        for x, y in zip(a, b):
+            for k in ("master", "lowp", "m", "v", "m_scale", "v_scale"):
+                assert torch.equal(x[k], y[k]), k
