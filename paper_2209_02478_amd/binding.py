@@ -149,13 +149,10 @@ def load_library():
 
 def _ptr(x) -> Optional[int]:
     """Address of a torch tensor (device or host), numpy array, int, or None."""
-    if x is None:
-        return None
-    if isinstance(x, int):
-        return x
-    if isinstance(x, np.ndarray):
-        return x.ctypes.data
-    return x.data_ptr()
+    try:                               # (tensors first: a call has up to a dozen, and small ones are bound by this)
+        return x.data_ptr()
+    except AttributeError:
+        return x.ctypes.data if isinstance(x, np.ndarray) else x
 
 
 def _check(code: int, ctx=None):
