@@ -163,11 +163,11 @@ struct PolicyArgs {
   float *rows = nullptr, *stats = nullptr;                         // [T, 4], [3]
 };
 size_t token_loss_workspace_bytes(int T);
-void token_logprob(int dtype, const void* logits, int64_t ldl, const int32_t* labels, float* logp, int T, int V, void* workspace, hipStream_t st);
+void token_logprob(int dtype, const void* logits, int64_t ldl, const int32_t* labels, float* logp, int T, int V, hipStream_t st);
 void preference_loss(int dtype, const void* logits, int64_t ldl, const int32_t* labels, const PreferenceArgs& a, void* dlogits, float* logp,
                      int T, int V, void* workspace, hipStream_t st);
 void policy_loss(int dtype, const void* logits, int64_t ldl, const int32_t* labels, const PolicyArgs& a, void* dlogits, int T, int V,
-                 void* workspace, hipStream_t st);
+                 hipStream_t st);
 // T: rows (B * L, or the real ones when rows.ends is given)
 void embed_fwd(int dtype, const int32_t* ids, const void* tok, const void* pos, const void* gamma,
                const void* beta, void* sum_out, void* y, const Rows& rows, int T, int B, int L, int H, float eps, int has_ln,

@@ -192,7 +192,7 @@ int mimose_op_token_logprob(int32_t dtype, const void* logits, int64_t ld, const
   if (!logp) return refuse(op, "logp must be given");
   if (workspace && ((uintptr_t)workspace & 15)) return refuse(op, "workspace must be 16-byte aligned");
   if (workspace && workspace_bytes < mk::token_loss_workspace_bytes(T)) return refuse(op, "workspace smaller than mimose_op_token_loss_workspace_bytes");
-  mk::token_logprob(dtype, logits, ld, labels, logp, T, V, workspace, (hipStream_t)stream);
+  mk::token_logprob(dtype, logits, ld, labels, logp, T, V, (hipStream_t)stream);
   return done();
 }
 
@@ -232,7 +232,7 @@ int mimose_op_policy_loss(int32_t dtype, const void* logits, int64_t ld, const i
   a.old_logp = old_logp; a.ref_logp = ref_logp; a.advantage = advantage; a.weight = weight;
   a.scale = scale; a.ratio_low = 1.f - clip_low; a.ratio_high = 1.f + clip_high; a.kl_weight = kl_weight;
   a.rows = rows; a.stats = stats;
-  mk::policy_loss(dtype, logits, ld, labels, a, dlogits, T, V, workspace, (hipStream_t)stream);
+  mk::policy_loss(dtype, logits, ld, labels, a, dlogits, T, V, (hipStream_t)stream);
   return done();
 }
 

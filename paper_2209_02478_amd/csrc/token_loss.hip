@@ -57,11 +57,6 @@ __device__ __forceinline__ float policy_token(const PolicyArgs& a, int row, floa
   return w * d;
 }
 
-template <typename T>
-__device__ __forceinline__ void zero_row(T* g, int64_t ldl) {
-  for (int64_t c = threadIdx.x; c < ldl; c += blockDim.x) st<T>(g + c, 0.f);
-}
-
 // 16 bytes of a row, as they are stored
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 template <typename T> struct Chunk;
@@ -75,15 +70,6 @@ template <> struct Chunk<bf16_t> {
   static __device__ __forceinline__ u32x4 bits(const float (&v)[8]) {
     return u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
   }
-  // element e on: -inf
-  static __device__ __forceinline__ u32x4 cut(u32x4 u, int e) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (2 * i >= e) u[i] = kNone;
-      else if (2 * i + 1 >= e) u[i] = (u[i] & 0xFFFFu) | (kNone & 0xFFFF0000u);
-    }
-    return u;
-  }
 };
 template <> struct Chunk<float> {
   static constexpr int N = 4;
@@ -95,19 +81,71 @@ template <> struct Chunk<float> {
   static __device__ __forceinline__ u32x4 bits(const float (&v)[4]) {
     return u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
   }
-  static __device__ __forceinline__ u32x4 cut(u32x4 u, int e) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) if (i >= e) u[i] = kNone;
-    return u;
-  }
 };
-
 constexpr float kLog2e = 1.44269504088896340736f;
 
-// Rows of whole 16-byte chunks on 16-byte addresses, held in registers as they are stored: read once, and with their
-// gradient written once.  WAVES waves share a row (one: a block has four rows and no barrier), NCH chunks a lane.
-template <typename T, int WAVES, int NCH, int MODE>
-__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES, WAVES == 16 && NCH <= 8 ? 8 : 4)
+// elements from e on are -inf
+template <typename T>
+__device__ __forceinline__ u32x4 cut_chunk(u32x4 u, int e) {
+  constexpr int per = 4 / (int)sizeof(T);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (per * i >= e) u[i] = Chunk<T>::kNone;
+    else if (per == 2 && 2 * i + 1 == e) u[i] = (u[i] & 0xFFFFu) | (Chunk<T>::kNone & 0xFFFF0000u);
+  }
+  return u;
+}
+// Chunks lie on 16-byte addresses whatever the row's own: chunk c of row x has the columns from c * N - shift(x) on.  A
+// row's first and last chunk may reach beyond it: there elements are read and written one by one, and none outside.
+template <typename T>
+__device__ __forceinline__ int shift_of(const T* x) { return (int)(((uintptr_t)x & 15) / sizeof(T)); }
+// a chunk from column `col` on that reaches beyond [0, V), where it is -inf
+template <typename T>
+__device__ __forceinline__ u32x4 load_edge(const T* x, int64_t col, int V) {
+  constexpr int N = Chunk<T>::N;
+  float v[N];
+#pragma unroll
+  for (int e = 0; e < N; ++e) v[e] = col + e >= 0 && col + e < V ? ld<T>(x + col + e) : -INFINITY;
+  return Chunk<T>::bits(v);
+}
+// columns of [V, ldl) are written as zeros, none outside [0, ldl)
+template <typename T>
+__device__ __forceinline__ void store_edge(T* g, int64_t col, int V, int64_t ldl, const float (&v)[Chunk<T>::N]) {
+#pragma unroll
+  for (int e = 0; e < Chunk<T>::N; ++e)
+    if (col + e >= 0 && col + e < ldl) st<T>(g + col + e, col + e < V ? v[e] : 0.f);
+}
+// gradient of a chunk: softmax times k, and d on the label, element `in` (any other number: not in this chunk)
+template <typename T>
+__device__ __forceinline__ void chunk_gradient(u32x4 u, float m, float k, float d, int64_t in, float (&v)[Chunk<T>::N]) {
+  constexpr int N = Chunk<T>::N;
+  Chunk<T>::values(u, v);
+#pragma unroll
+  for (int e = 0; e < N; ++e) v[e] = __builtin_amdgcn_exp2f((v[e] - m) * kLog2e) * k;
+  if (in >= 0 && in < N) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) if (e == in) v[e] += d;
+  }
+}
+// columns [from, to) of a row are zeros, by `threads` threads
+template <typename T>
+__device__ __forceinline__ void zero_columns(T* g, int64_t from, int64_t to, int tid, int threads) {
+  constexpr int N = Chunk<T>::N;
+  const int64_t body = min(to, from + (N - shift_of(g + from)) % N), end = body + (to - body) / N * N;
+  if (from + tid < body) st<T>(g + from + tid, 0.f);     // (fewer than N columns)
+  for (int64_t c = body + (int64_t)tid * N; c < end; c += (int64_t)threads * N)
+    __builtin_nontemporal_store(u32x4{0u, 0u, 0u, 0u}, (u32x4*)(g + c));
+  if (end + tid < to) st<T>(g + end + tid, 0.f);
+}
+// the next pass over held chunks converts them anew: kept as floats they would take twice the registers
+__device__ __forceinline__ void keep_packed(u32x4& u) { asm volatile("" : "+v"(u)); }
+
+// A row is held in registers as it is stored: read once, and with its gradient written once.  WAVES waves share a row
+// (one: a block has four rows and no barrier), NCH chunks a lane.  EVEN: every row, and that of the gradient, begins and
+// ends on a chunk.  PAST: the row is read past the caches.  Gradients always are written past them: what reads them next is
+// a matrix product over all rows.
+template <typename T, int WAVES, int NCH, int MODE, bool PAST, bool EVEN>
+__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES, (WAVES == 16 && NCH <= 9) || (WAVES == 1 && NCH <= 4) ? 8 : 4)
 void token_rows_held_kernel(const T* logits, int64_t ldl, const int32_t* __restrict__ labels, float* __restrict__ logp,
                             float2* __restrict__ stat, float* __restrict__ slope, T* dlogits, PolicyArgs pa, int rows, int V) {
   constexpr int N = Chunk<T>::N, TPR = 64 * WAVES;
@@ -116,49 +154,70 @@ void token_rows_held_kernel(const T* logits, int64_t ldl, const int32_t* __restr
   const int tid = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
   if (row >= rows) return;                              // (a wave with a row to itself)
   const T* x = logits + (int64_t)row * ldl;
-  u32x4* g = dlogits ? (u32x4*)(dlogits + (int64_t)row * ldl) : nullptr;
-  const int label = labels[row], chunks = (V + N - 1) / N;
-  const int64_t wide = ldl / N;
-  const u32x4 zero = {0u, 0u, 0u, 0u};
+  T* g = dlogits ? dlogits + (int64_t)row * ldl : nullptr;
+  const int label = labels[row];
   if (MODE == 0 && slope && tid == 0) slope[row] = 0.f;
   if (!is_scored(label, V)) {
     if (MODE == 0) {
       if (tid == 0) logp[row] = 0.f;
     } else {
       if (tid == 0) ((float4*)pa.rows)[row] = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (g) for (int64_t c = tid; c < wide; c += TPR) g[c] = zero;
+      if (g) zero_columns(g, 0, ldl, tid, TPR);
     }
     return;
   }
   const float picked = ld<T>(x + label);
+  // chunks [whole0, whole1) lie inside [0, V); chunk 0 where whole0 is 1, and chunk whole1 (tail), where there is one, reach
+  // beyond it; a row inside one chunk is its tail alone
+  const int shift = EVEN ? 0 : shift_of(x), whole1 = (shift + V) / N, whole0 = shift && whole1 ? 1 : 0;
+  const int tail = (shift + V) % N ? whole1 : -1, chunks = whole1 + (tail >= 0);
+  const int loaded = EVEN ? chunks : whole1;
+  const u32x4* xc = (const u32x4*)(x - shift);
+  constexpr uint32_t none = Chunk<T>::kNone;
   u32x4 raw[NCH];
 #pragma unroll
   for (int i = 0; i < NCH; ++i) {
     const int c = tid + TPR * i;
-    raw[i] = u32x4{Chunk<T>::kNone, Chunk<T>::kNone, Chunk<T>::kNone, Chunk<T>::kNone};
-    if (c < chunks) raw[i] = ((const u32x4*)x)[c];
+    raw[i] = u32x4{none, none, none, none};
+    if (c >= whole0 && c < loaded) raw[i] = PAST ? __builtin_nontemporal_load(xc + c) : xc[c];
   }
-  if (V % N) {
+  if (EVEN) {
+    if (tail >= 0) {
 #pragma unroll
-    for (int i = 0; i < NCH; ++i)
-      if (tid + TPR * i == chunks - 1) raw[i] = Chunk<T>::cut(raw[i], V % N);
+      for (int i = 0; i < NCH; ++i)
+        if (tid + TPR * i == tail) raw[i] = cut_chunk<T>(raw[i], V % N);
+    }
+  } else {
+    if (whole0 && tid == 0) raw[0] = load_edge(x, -shift, V);
+    if (tail >= 0 && tail % TPR == tid) {
+      const u32x4 edge = load_edge(x, (int64_t)tail * N - shift, V);
+#pragma unroll
+      for (int i = 0; i < NCH; ++i) if (tid + TPR * i == tail) raw[i] = edge;
+    }
   }
+  // a wave leaves out chunks that none of its lanes has
+  const int wave_first = WAVES == 1 ? 0 : __builtin_amdgcn_readfirstlane(tid & ~63);
   float m = -INFINITY;
 #pragma unroll
   for (int i = 0; i < NCH; ++i) {
-    float v[N];
-    Chunk<T>::values(raw[i], v);
+    if (wave_first + TPR * i < chunks) {
+      float v[N];
+      Chunk<T>::values(raw[i], v);
 #pragma unroll
-    for (int e = 0; e < N; ++e) m = fmaxf(m, v[e]);
+      for (int e = 0; e < N; ++e) m = fmaxf(m, v[e]);
+    }
   }
   m = WAVES == 1 ? wave_max(m) : block_max<WAVES>(m, sm);
   float s = 0.f;
 #pragma unroll
   for (int i = 0; i < NCH; ++i) {
-    float v[N];
-    Chunk<T>::values(raw[i], v);
+    keep_packed(raw[i]);
+    if (wave_first + TPR * i < chunks) {
+      float v[N];
+      Chunk<T>::values(raw[i], v);
 #pragma unroll
-    for (int e = 0; e < N; ++e) s += __builtin_amdgcn_exp2f((v[e] - m) * kLog2e);
+      for (int e = 0; e < N; ++e) s += __builtin_amdgcn_exp2f((v[e] - m) * kLog2e);
+    }
   }
   s = WAVES == 1 ? wave_sum(s) : block_sum<WAVES>(s, ss);
   const float lp = (picked - m) - logf(s);
@@ -173,35 +232,58 @@ void token_rows_held_kernel(const T* logits, int64_t ldl, const int32_t* __restr
   const float d = policy_token(pa, row, lp, &kept), k = -d / s;
   if (tid == 0) ((float4*)pa.rows)[row] = kept;
   if (!g) return;
+  const int at = label + shift;                         // the label's element, counted from chunk 0
+  float v[N];
+  if (EVEN) {
+    u32x4* gc = (u32x4*)g;
 #pragma unroll
-  for (int i = 0; i < NCH; ++i) {
-    const int c = tid + TPR * i;
-    if (c >= chunks) break;
-    float v[N];
-    Chunk<T>::values(raw[i], v);
+    for (int i = 0; i < NCH; ++i) {
+      const int c = tid + TPR * i;
+      keep_packed(raw[i]);
+      if (c < chunks) {
+        chunk_gradient<T>(raw[i], m, k, d, at - c * N, v);
+        if (c == tail) {
 #pragma unroll
-    for (int e = 0; e < N; ++e) v[e] = __builtin_amdgcn_exp2f((v[e] - m) * kLog2e) * k;
-    if (label / N == c) {
-#pragma unroll
-      for (int e = 0; e < N; ++e) if (label % N == e) v[e] += d;
+          for (int e = 0; e < N; ++e) if (e >= V % N) v[e] = 0.f;
+        }
+        __builtin_nontemporal_store(Chunk<T>::bits(v), gc + c);
+      }
     }
-    g[c] = Chunk<T>::bits(v);
+  } else {
+    const bool aligned = shift_of(g) == shift;          // else the gradient's chunks are not the logits': element by element
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) {
+      const int c = tid + TPR * i;
+      keep_packed(raw[i]);
+      if (c < chunks) {
+        chunk_gradient<T>(raw[i], m, k, d, at - c * N, v);
+        if (aligned && c >= whole0 && c < whole1) __builtin_nontemporal_store(Chunk<T>::bits(v), (u32x4*)(g - shift) + c);
+        else store_edge(g, (int64_t)c * N - shift, V, ldl, v);
+      }
+    }
   }
-  for (int64_t c = chunks + tid; c < wide; c += TPR) g[c] = zero;
+  const int64_t behind = (int64_t)chunks * N - shift;
+  if (behind < ldl) zero_columns(g, behind, ldl, tid, TPR);
 }
 
-// chunks a lane and waves a row that hold a row of `chunks`, or none
-#define HELD_ROWS(CHUNKS, M)                     \
-  if ((CHUNKS) <= 64) { M(1, 1); }               \
-  else if ((CHUNKS) <= 128) { M(1, 2); }         \
-  else if ((CHUNKS) <= 256) { M(1, 4); }         \
-  else if ((CHUNKS) <= 512) { M(4, 2); }         \
-  else if ((CHUNKS) <= 1024) { M(4, 4); }        \
-  else if ((CHUNKS) <= 2048) { M(8, 4); }        \
-  else if ((CHUNKS) <= 4096) { M(16, 4); }       \
-  else if ((CHUNKS) <= 7168) { M(16, 7); }       \
-  else if ((CHUNKS) <= 8192) { M(16, 8); }       \
-  else if ((CHUNKS) <= 16384) { M(16, 16); }
+// WAVES and NCH by the chunks of a row: at least seven chunks a lane where the row has them, because fewer leave too few bytes
+// on the way to memory (policy loss, 16384 rows of 4000 in bf16: 79 us with 4 x 4, 54 with 1 x 9; of 15000: 259 with 8 x 4, 174
+// with 4 x 9), and registers of no more than 64 a lane, for two rows of 16 waves a unit.  Reading alone, 8 x 13 is ahead of 16 x
+// 7 (12288 rows of 50257: 183 us against 190); with the gradient behind it, it is not (550 against 517).
+#define HELD_ROWS(CHUNKS, M)                                 \
+  if ((CHUNKS) <= 64) { M(1, 1) }                            \
+  else if ((CHUNKS) <= 128) { M(1, 2) }                      \
+  else if ((CHUNKS) <= 256) { M(1, 4) }                      \
+  else if ((CHUNKS) <= 576) { M(1, 9) }                      \
+  else if ((CHUNKS) <= 1152) { M(2, 9) }                     \
+  else if ((CHUNKS) <= 2304) { M(4, 9) }                     \
+  else if ((CHUNKS) <= 4608) { M(8, 9) }                     \
+  else if (MODE == 0 && (CHUNKS) <= 6656) { M(8, 13) }       \
+  else if ((CHUNKS) <= 7168) { M(16, 7) }                    \
+  else if ((CHUNKS) <= 9216) { M(16, 9) }                    \
+  else if ((CHUNKS) <= 13312) { M(16, 13) }                  \
+  else { M(16, 16) }
+constexpr int kMostChunks = 16384;
 
 // One block for a row, whatever its length and alignment.
 // MODE 0: logp[row]; stat[row] (optional), the row's maximum and the reciprocal of its sum of exponentials; slope[row]
@@ -223,7 +305,7 @@ __global__ __launch_bounds__(kRowThreads) void token_rows_kernel(const T* logits
       if (tid == 0) logp[row] = 0.f;
     } else {
       if (tid == 0) ((float4*)pa.rows)[row] = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (g) zero_row(g, ldl);
+      if (g) zero_columns(g, 0, ldl, tid, kRowThreads);
     }
     return;
   }
@@ -272,42 +354,37 @@ __device__ __forceinline__ float pair_slope(float z, const PreferenceArgs& a) {
   return -a.beta / (float)a.pairs * ((1.f - a.smoothing) / (1.f + expf(z)) - a.smoothing / (1.f + expf(-z)));
 }
 
-// One block for a pair: the sums of both sequences, in fp64 because the margin is the small difference of four sums
-// over a thousand rows; the margin; and d loss / d logp of each of the pair's rows.
-constexpr int kPairThreads = 512;
+// One block for a pair, half of its threads for each sequence: the sums, in fp64 because the margin is the small difference
+// of four sums over a thousand rows; the margin; and d loss / d logp of each of the pair's rows.
+constexpr int kPairThreads = 1024;
 __global__ __launch_bounds__(kPairThreads) void pair_sums_kernel(PreferenceArgs a, const float* __restrict__ logp, float* __restrict__ slope,
-                                                                 int first, int T) {
-  __shared__ double red[kPairThreads];
-  const int p = first + blockIdx.x, tid = threadIdx.x;
-  const int2 r[2] = {sequence_rows(a.ends, 2 * p, a.L, T), sequence_rows(a.ends, 2 * p + 1, a.L, T)};
-  double h = 0.0;
-  for (int k = 0; k < 2; ++k) {
-    double s = 0.0;
-    for (int i = r[k].x + tid; i < r[k].y; i += kPairThreads) s += (double)logp[i];
-    red[tid] = s;
+                                                                 int T) {
+  constexpr int half = kPairThreads / 2;
+  __shared__ double red[2][half];
+  const int p = blockIdx.x, k = threadIdx.x / half, tid = threadIdx.x % half;
+  const int2 r = sequence_rows(a.ends, 2 * p + k, a.L, T);
+  double s = 0.0;
+  for (int i = r.x + tid; i < r.y; i += half) s += (double)logp[i];
+  red[k][tid] = s;
+  __syncthreads();
+  for (int o = half / 2; o > 0; o >>= 1) {
+    if (tid < o) red[k][tid] += red[k][tid + o];
     __syncthreads();
-    for (int o = kPairThreads / 2; o > 0; o >>= 1) {
-      if (tid < o) red[tid] += red[tid + o];
-      __syncthreads();
-    }
-    s = red[0];
-    __syncthreads();
-    if (tid == 0) a.seq_logp[2 * p + k] = (float)s;
-    s -= (double)a.ref_logp[2 * p + k];
-    h = k ? h - s : s;
   }
+  if (tid == 0) a.seq_logp[2 * p + k] = (float)red[k][0];
+  const double h = (red[0][0] - (double)a.ref_logp[2 * p]) - (red[1][0] - (double)a.ref_logp[2 * p + 1]);
   const float z = (float)((double)a.beta * h);
-  if (tid == 0) a.margin[p] = z;
+  if (threadIdx.x == 0) a.margin[p] = z;
   if (!slope) return;
   const float d = pair_slope(z, a);
-  for (int k = 0; k < 2; ++k)
-    for (int i = r[k].x + tid; i < r[k].y; i += kPairThreads) slope[i] = k ? -d : d;
+  for (int i = r.x + tid; i < r.y; i += half) slope[i] = k ? -d : d;
 }
 
 // mean loss of the pairs, by one block
 __device__ __forceinline__ void mean_pair_loss(const PreferenceArgs& a) {
   __shared__ double red[256];
   const int tid = threadIdx.x;
+  if (tid >= 256) return;
   double s = 0.0;
   for (int p = tid; p < a.pairs; p += 256) s += (double)pair_loss(a.margin[p], a.smoothing);
   red[tid] = s;
@@ -320,72 +397,56 @@ __device__ __forceinline__ void mean_pair_loss(const PreferenceArgs& a) {
 }
 __global__ __launch_bounds__(256) void pair_loss_kernel(PreferenceArgs a) { mean_pair_loss(a); }
 
-// Gradient from what the pass before left of each row, any alignment: one block for a row, and one more, of 256 threads
-// like the others, for the mean loss (with_loss).
-template <typename T>
+// Gradient from what the pass before left of each row: grad_chunks() chunks a thread, `parts` blocks a row, the last row first, because the pass
+// before has read it last.  One more block, behind all rows, for the mean loss.
+constexpr int grad_chunks(bool past) { return past ? 1 : 2; }
+template <typename T, bool PAST>
 __global__ __launch_bounds__(kRowThreads) void pair_grad_kernel(const T* logits, int64_t ldl, const int32_t* __restrict__ labels,
                                                                 const float2* __restrict__ stat, const float* __restrict__ slope,
-                                                                T* dlogits, PreferenceArgs a, int rows, int V) {
-  const int row = rows - 1 - (int)blockIdx.x, tid = threadIdx.x;
-  if (row < 0) { mean_pair_loss(a); return; }
-  const T* x = logits + (int64_t)row * ldl;
-  T* g = dlogits + (int64_t)row * ldl;
-  const int label = labels[row];
-  const float d = slope[row];
-  if (!is_scored(label, V) || d == 0.f) {
-    zero_row(g, ldl);
-    return;
-  }
-  const float2 ms = stat[row];
-  const float k = -d * ms.y;
-  for (int64_t c = tid; c < ldl; c += kRowThreads)
-    st<T>(g + c, c < V ? __expf(ld<T>(x + c) - ms.x) * k + (c == label ? d : 0.f) : 0.f);
-}
-
-// The same for rows of whole 16-byte chunks: kGradChunks chunks a thread, `parts` blocks a row, the last row first, which
-// the pass before has read last.
-constexpr int kGradChunks = 4;
-template <typename T>
-__global__ __launch_bounds__(kRowThreads) void pair_grad_chunk_kernel(const T* logits, int64_t ldl, const int32_t* __restrict__ labels,
-                                                                      const float2* __restrict__ stat, const float* __restrict__ slope,
-                                                                      T* dlogits, PreferenceArgs a, int rows, int V, int parts) {
-  constexpr int N = Chunk<T>::N;
+                                                                T* dlogits, PreferenceArgs a, int rows, int V, int parts) {
+  constexpr int N = Chunk<T>::N, CH = grad_chunks(PAST);
   const int row = rows - 1 - (int)(blockIdx.x / (unsigned)parts);
   if (row < 0) { mean_pair_loss(a); return; }
-  const int c0 = (int)(blockIdx.x % (unsigned)parts) * (kRowThreads * kGradChunks) + threadIdx.x, chunks = (V + N - 1) / N, wide = (int)(ldl / N);
-  const u32x4* x = (const u32x4*)(logits + (int64_t)row * ldl);
-  u32x4* g = (u32x4*)(dlogits + (int64_t)row * ldl);
-  const int label = labels[row];
+  const int part = (int)(blockIdx.x % (unsigned)parts);
+  const T* x = logits + (int64_t)row * ldl;
+  T* g = dlogits + (int64_t)row * ldl;
+  const int shift = shift_of(x), label = labels[row];
+  const bool aligned = shift_of(g) == shift;
   const float d = slope[row];
-  const u32x4 zero = {0u, 0u, 0u, 0u};
+  const int64_t first = (int64_t)part * (kRowThreads * CH) * N - shift;     // column
   if (!is_scored(label, V) || d == 0.f) {
-#pragma unroll
-    for (int i = 0; i < kGradChunks; ++i)
-      if (c0 + kRowThreads * i < wide) g[c0 + kRowThreads * i] = zero;
+    const int64_t to = min(ldl, first + (int64_t)kRowThreads * CH * N);
+    if (first < to) zero_columns(g, max(first, (int64_t)0), to, threadIdx.x, kRowThreads);
     return;
   }
-  u32x4 raw[kGradChunks];
+  u32x4 raw[CH];
 #pragma unroll
-  for (int i = 0; i < kGradChunks; ++i)
-    if (c0 + kRowThreads * i < chunks) raw[i] = x[c0 + kRowThreads * i];
+  for (int i = 0; i < CH; ++i) {
+    const int64_t col = first + (int64_t)(threadIdx.x + kRowThreads * i) * N;
+    if (col >= 0 && col + N <= ldl) {
+      const u32x4* p = (const u32x4*)(x + col);
+      raw[i] = PAST ? __builtin_nontemporal_load(p) : *p;
+      if (col + N > V) raw[i] = cut_chunk<T>(raw[i], (int)max(V - col, (int64_t)0));
+    } else {
+      raw[i] = load_edge(x, col, V);
+    }
+  }
   const float2 ms = stat[row];
   const float k = -d * ms.y;
 #pragma unroll
-  for (int i = 0; i < kGradChunks; ++i) {
-    const int c = c0 + kRowThreads * i;
-    if (c < chunks) {
-      if (c == chunks - 1 && V % N) raw[i] = Chunk<T>::cut(raw[i], V % N);
-      float v[N];
-      Chunk<T>::values(raw[i], v);
+  for (int i = 0; i < CH; ++i) {
+    const int64_t col = first + (int64_t)(threadIdx.x + kRowThreads * i) * N;
+    if (col >= ldl) break;
+    float v[N];
+    chunk_gradient<T>(raw[i], ms.x, k, d, label - col, v);
+    if (aligned && col >= 0 && col + N <= ldl) {
+      if (col + N > V) {
 #pragma unroll
-      for (int e = 0; e < N; ++e) v[e] = __builtin_amdgcn_exp2f((v[e] - ms.x) * kLog2e) * k;
-      if (label / N == c) {
-#pragma unroll
-        for (int e = 0; e < N; ++e) if (label % N == e) v[e] += d;
+        for (int e = 0; e < N; ++e) if (col + e >= V) v[e] = 0.f;
       }
-      g[c] = Chunk<T>::bits(v);
-    } else if (c < wide) {
-      g[c] = zero;
+      __builtin_nontemporal_store(Chunk<T>::bits(v), (u32x4*)(g + col));
+    } else {
+      store_edge(g, col, V, ldl, v);
     }
   }
 }
@@ -395,9 +456,12 @@ __global__ __launch_bounds__(1024) void policy_stats_kernel(const float4* __rest
   __shared__ double red[3][1024];
   const int tid = threadIdx.x;
   double s[3] = {0.0, 0.0, 0.0};
-  for (int i = tid; i < T; i += 1024) {
-    const float4 r = rows[i];
-    s[0] += (double)r.y; s[1] += (double)r.z; s[2] += (double)r.w;
+  for (int i = tid; i < T; i += 8 * 1024) {
+    float4 r[8];                                        // (eight loads on their way at a time)
+#pragma unroll
+    for (int u = 0; u < 8; ++u) r[u] = i + 1024 * u < T ? rows[i + 1024 * u] : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int u = 0; u < 8; ++u) { s[0] += (double)r[u].y; s[1] += (double)r[u].z; s[2] += (double)r[u].w; }
   }
   for (int k = 0; k < 3; ++k) red[k][tid] = s[k];
   __syncthreads();
@@ -415,16 +479,24 @@ constexpr int kRowsPerLaunch = 1 << 20;
 // of each row its maximum and the reciprocal of its sum of exponentials, and d loss / d logp
 size_t token_loss_workspace_bytes(int T) { return (size_t)(T > 0 ? T : 0) * (sizeof(float2) + sizeof(float)); }
 
-template <typename T>
-static bool whole_chunks(const void* a, const void* b, int64_t ldl) {
-  return ldl % Chunk<T>::N == 0 && ldl / Chunk<T>::N <= INT32_MAX && (((uintptr_t)a | (uintptr_t)b) & 15) == 0;
+template <typename T, int MODE, bool PAST, bool EVEN>
+static void held_t(const T* x, int64_t ldl, const int32_t* labels, float* logp, float2* stat, float* slope, T* g, const PolicyArgs& a, int rows,
+                   int V, int chunks, hipStream_t st) {
+#define H_(WAVES, NCH)                                                                                                           \
+  hipLaunchKernelGGL((token_rows_held_kernel<T, WAVES, NCH, MODE, PAST, EVEN>), dim3(WAVES == 1 ? (rows + 3) / 4 : rows),           \
+                     dim3(WAVES == 1 ? 256 : 64 * WAVES), 0, st, x, ldl, labels, logp, stat, slope, g, a, rows, V);
+  HELD_ROWS(chunks, H_)
+#undef H_
 }
 
+// past: rows are read past the caches
 template <typename T, int MODE>
 static void rows_t(const void* logits, int64_t ldl, const int32_t* labels, float* logp, float2* stat, float* slope, void* dlogits,
-                   const PolicyArgs& pa, int rows, int V, hipStream_t st) {
-  const int chunks = (V + Chunk<T>::N - 1) / Chunk<T>::N;
-  const bool held = whole_chunks<T>(logits, dlogits, ldl) && chunks <= 16384;
+                   const PolicyArgs& pa, int rows, int V, bool past, hipStream_t st) {
+  constexpr int N = Chunk<T>::N;
+  const bool even = ldl % N == 0 && (((uintptr_t)logits | (uintptr_t)dlogits) & 15) == 0;
+  const int64_t chunks = ((even ? 0 : N - 1) + (int64_t)V + N - 1) / N;
+  const bool held = chunks <= kMostChunks;
   for (int r = 0; r < rows; r += kRowsPerLaunch) {
     const int n = std::min(rows - r, kRowsPerLaunch);
     PolicyArgs a = pa;
@@ -437,48 +509,53 @@ static void rows_t(const void* logits, int64_t ldl, const int32_t* labels, float
     T* g = dlogits ? (T*)dlogits + r * ldl : nullptr;
     float *lp = logp ? logp + r : nullptr, *sl = slope ? slope + r : nullptr;
     float2* sta = stat ? stat + r : nullptr;
-    if (held) {
-#define H_(WAVES, NCH)                                                                                                               \
-  hipLaunchKernelGGL((token_rows_held_kernel<T, WAVES, NCH, MODE>), dim3(WAVES == 1 ? (n + 3) / 4 : n), dim3(WAVES == 1 ? 256 : 64 * WAVES), \
-                     0, st, x, ldl, labels + r, lp, sta, sl, g, a, n, V)
-      HELD_ROWS(chunks, H_)
-#undef H_
-    } else {
+    if (held && even && (past || MODE == 1))
+      held_t<T, MODE, true, true>(x, ldl, labels + r, lp, sta, sl, g, a, n, V, (int)chunks, st);
+    else if (held && even)
+      held_t<T, 0, false, true>(x, ldl, labels + r, lp, sta, sl, g, a, n, V, (int)chunks, st);
+    else if (held)
+      held_t<T, MODE, true, false>(x, ldl, labels + r, lp, sta, sl, g, a, n, V, (int)chunks, st);
+    else
       hipLaunchKernelGGL((token_rows_kernel<T, MODE>), dim3(n), dim3(kRowThreads), 0, st, x, ldl, labels + r, lp, sta, sl, g, a, V);
-    }
   }
 }
 
-void token_logprob(int dtype, const void* logits, int64_t ldl, const int32_t* labels, float* logp, int T, int V, void* workspace, hipStream_t st) {
-  (void)workspace;
-  if (dtype == BF16) rows_t<bf16_t, 0>(logits, ldl, labels, logp, nullptr, nullptr, nullptr, PolicyArgs(), T, V, st);
-  else rows_t<float, 0>(logits, ldl, labels, logp, nullptr, nullptr, nullptr, PolicyArgs(), T, V, st);
+void token_logprob(int dtype, const void* logits, int64_t ldl, const int32_t* labels, float* logp, int T, int V, hipStream_t st) {
+  if (dtype == BF16) rows_t<bf16_t, 0>(logits, ldl, labels, logp, nullptr, nullptr, nullptr, PolicyArgs(), T, V, true, st);
+  else rows_t<float, 0>(logits, ldl, labels, logp, nullptr, nullptr, nullptr, PolicyArgs(), T, V, true, st);
 }
 
 template <typename T>
 static void preference_t(const void* logits, int64_t ldl, const int32_t* labels, const PreferenceArgs& a, void* dlogits, float* logp, int rows,
                          int V, void* workspace, hipStream_t st) {
+  constexpr int N = Chunk<T>::N;
   float2* stat = (float2*)workspace;
-  float* slope = dlogits ? (float*)(stat + rows) : nullptr;
-  rows_t<T, 0>(logits, ldl, labels, logp, stat, slope, nullptr, PolicyArgs(), rows, V, st);
-  hipLaunchKernelGGL(pair_sums_kernel, dim3(a.pairs), dim3(kPairThreads), 0, st, a, logp, slope, 0, rows);
   if (!dlogits || rows <= 0) {
+    rows_t<T, 0>(logits, ldl, labels, logp, nullptr, nullptr, nullptr, PolicyArgs(), rows, V, true, st);
+    hipLaunchKernelGGL(pair_sums_kernel, dim3(a.pairs), dim3(kPairThreads), 0, st, a, logp, (float*)nullptr, rows);
     hipLaunchKernelGGL(pair_loss_kernel, dim3(1), dim3(256), 0, st, a);
     return;
   }
-  const bool vec = whole_chunks<T>(logits, dlogits, ldl);
-  const int64_t per_block = (int64_t)kRowThreads * kGradChunks, parts = vec ? (ldl / Chunk<T>::N + per_block - 1) / per_block : 1;
+  float* slope = (float*)(stat + rows);
+  // The gradient reads the rows a second time.  Where they are few, what the first pass has read is still in the last cache
+  // (256 MB), where many are it is not, and loads past the caches are faster.  Labels say what is read of them, and they are on
+  // the device: the bound is of all rows, 640 MB, of which some hundred are prompts.  6352 rows of 50257, 0.4 of them prompts
+  // (639 MB): 223 us through the caches, 249 past them; 8192 of 30522, no prompts (500 MB): 255 and 249; 16384 of 50257: 849 and
+  // 778.  Chunks a thread: 2 and 1, 788 and 749 in the last of these, 143 and 151 for 4200 rows (422 MB).
+  const bool few = rows * ldl * (int64_t)sizeof(T) <= (int64_t)640 << 20;
+  const int64_t per_block = (int64_t)kRowThreads * grad_chunks(!few) * N, parts = (ldl + (N - 1) + per_block - 1) / per_block;
   const int most = (int)std::max<int64_t>(1, ((int64_t)kRowsPerLaunch * 8) / parts);
-  for (int r = 0; r < rows; r += most) {
-    const int n = std::min(rows - r, most);
-    const int extra = r + n == rows;                    // the mean loss, once
+  rows_t<T, 0>(logits, ldl, labels, logp, stat, slope, nullptr, PolicyArgs(), rows, V, !few, st);
+  hipLaunchKernelGGL(pair_sums_kernel, dim3(a.pairs), dim3(kPairThreads), 0, st, a, logp, slope, rows);
+  for (int end = rows; end > 0; end -= std::min(end, most)) {
+    const int n = std::min(end, most), r = end - n, extra = r == 0;     // (with the mean loss behind everything)
     const T* x = (const T*)logits + r * ldl;
     T* g = (T*)dlogits + r * ldl;
-    if (vec)
-      hipLaunchKernelGGL(pair_grad_chunk_kernel<T>, dim3((unsigned)(n * parts + extra)), dim3(kRowThreads), 0, st, x, ldl, labels + r, stat + r,
-                         slope + r, g, a, n, V, (int)parts);
-    else
-      hipLaunchKernelGGL(pair_grad_kernel<T>, dim3(n + extra), dim3(kRowThreads), 0, st, x, ldl, labels + r, stat + r, slope + r, g, a, n, V);
+#define G_(PAST)                                                                                                                     \
+  hipLaunchKernelGGL((pair_grad_kernel<T, PAST>), dim3((unsigned)(n * parts + extra)), dim3(kRowThreads), 0, st, x, ldl, labels + r, stat + r, \
+                     slope + r, g, a, n, V, (int)parts)
+    if (few) G_(false); else G_(true);
+#undef G_
   }
 }
 
@@ -489,10 +566,9 @@ void preference_loss(int dtype, const void* logits, int64_t ldl, const int32_t* 
 }
 
 void policy_loss(int dtype, const void* logits, int64_t ldl, const int32_t* labels, const PolicyArgs& a, void* dlogits, int T, int V,
-                 void* workspace, hipStream_t st) {
-  (void)workspace;
-  if (dtype == BF16) rows_t<bf16_t, 1>(logits, ldl, labels, nullptr, nullptr, nullptr, dlogits, a, T, V, st);
-  else rows_t<float, 1>(logits, ldl, labels, nullptr, nullptr, nullptr, dlogits, a, T, V, st);
+                 hipStream_t st) {
+  if (dtype == BF16) rows_t<bf16_t, 1>(logits, ldl, labels, nullptr, nullptr, nullptr, dlogits, a, T, V, true, st);
+  else rows_t<float, 1>(logits, ldl, labels, nullptr, nullptr, nullptr, dlogits, a, T, V, true, st);
   hipLaunchKernelGGL(policy_stats_kernel, dim3(1), dim3(1024), 0, st, (const float4*)a.rows, T, a.stats);
 }
 
