@@ -68,6 +68,11 @@ __device__ __forceinline__ int padded_row(const Rows& r, int row, int B, int L) 
   return lo * L + row - (lo ? r.ends[lo - 1] : 0);
 }
 
+// A pointer that comes out of a table in memory could point anywhere: said to point into device memory it is accessed by
+// global instructions, not by flat ones, which also count as accesses of the LDS.
+template <typename T> using global_ptr = T __attribute__((address_space(1)))*;
+template <typename T> __device__ __forceinline__ global_ptr<T> in_global(T* p) { return (global_ptr<T>)p; }
+
 template <typename T> __device__ __forceinline__ float ld(const T* p);
 template <> __device__ __forceinline__ float ld<float>(const float* p) { return *p; }
 template <> __device__ __forceinline__ float ld<bf16_t>(const bf16_t* p) { return bf16_to_f32(*p); }

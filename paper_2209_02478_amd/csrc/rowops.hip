@@ -831,8 +831,10 @@ __global__ __launch_bounds__(kAdamThreads) void adamw_kernel(const AdamTensor* _
   bf16_t* lowp = (bf16_t*)t.lowp;
   const int64_t i = ck.start + 4 * ((int64_t)(blockIdx.x % kAdamBlocks) * kAdamThreads + threadIdx.x);
   if (i + 4 <= t.n) {                                 // (tensor starts are 256-byte aligned)
-    const f32x4 g4 = __builtin_nontemporal_load((const f32x4*)(t.grad + i)), m4 = __builtin_nontemporal_load((const f32x4*)(t.m + i)),
-                v4 = __builtin_nontemporal_load((const f32x4*)(t.v + i)), p4 = __builtin_nontemporal_load((const f32x4*)(t.master + i));
+    const f32x4 g4 = __builtin_nontemporal_load(in_global((const f32x4*)(t.grad + i))),
+                m4 = __builtin_nontemporal_load(in_global((const f32x4*)(t.m + i))),
+                v4 = __builtin_nontemporal_load(in_global((const f32x4*)(t.v + i))),
+                p4 = __builtin_nontemporal_load(in_global((const f32x4*)(t.master + i)));
     const float gs[4] = {g4[0], g4[1], g4[2], g4[3]};
     float ms[4] = {m4[0], m4[1], m4[2], m4[3]}, vs[4] = {v4[0], v4[1], v4[2], v4[3]}, ps[4] = {p4[0], p4[1], p4[2], p4[3]};
 #pragma unroll
@@ -841,17 +843,16 @@ __global__ __launch_bounds__(kAdamThreads) void adamw_kernel(const AdamTensor* _
       vs[e] = h.beta2 * vs[e] + (1.f - h.beta2) * gs[e] * gs[e];
       ps[e] -= h.lr * ((ms[e] * h.inv_c1) / (sqrtf(vs[e] * h.inv_c2) + h.eps) + wd * ps[e]);
     }
-    const f32x4 m = {ms[0], ms[1], ms[2], ms[3]}, v = {vs[0], vs[1], vs[2], vs[3]}, p = {ps[0], ps[1], ps[2], ps[3]};
-    __builtin_nontemporal_store(m, (f32x4*)(t.m + i));
-    __builtin_nontemporal_store(v, (f32x4*)(t.v + i));
+    f32x4 m = {ms[0], ms[1], ms[2], ms[3]}, v = {vs[0], vs[1], vs[2], vs[3]}, p = {ps[0], ps[1], ps[2], ps[3]};
+    __builtin_nontemporal_store(m, in_global((f32x4*)(t.m + i)));
+    __builtin_nontemporal_store(v, in_global((f32x4*)(t.v + i)));
     if (lowp) {
-      __builtin_nontemporal_store(p, (f32x4*)(t.master + i));
-      uint2 w;
-      w.x = pack_bf16x2(p[0], p[1]);
-      w.y = pack_bf16x2(p[2], p[3]);
-      *(uint2*)(lowp + i) = w;
+      __builtin_nontemporal_store(p, in_global((f32x4*)(t.master + i)));
+      typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+      *in_global((u32x2*)(lowp + i)) = u32x2{pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3])};
     } else {
-      *(f32x4*)(t.master + i) = p;                    // (fp32: the master is what the next forward reads)
+      asm volatile("" : "+v"(p));                     // (else the compiler makes one ordinary store of the two)
+      *in_global((f32x4*)(t.master + i)) = p;         // fp32: the master is what the next forward reads
     }
   } else {
     for (int64_t j = i; j < t.n; ++j) {
