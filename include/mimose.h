@@ -162,6 +162,43 @@ int mimose_train_step_padded(mimose_ctx* ctx, const int32_t* tokens_host, const 
                              uint64_t* peak_bytes, uint64_t* plan_id);
 
 /*
+ * The same iteration with another loss in place of the cross-entropy, for fine-tuning after the first
+ * training: plan, memory, recomputation, dropout, queueing and errors are those of mimose_train_step
+ * (mimose_train_step_padded where lengths is given; NULL: every sample has L tokens).  What the loss
+ * needs beside the logits comes out of the same arena, as part of the head's transient.  Labels say
+ * which positions are scored (-1: none, as for the tokens of a prompt).
+ *
+ * mimose_train_step_preference: samples 2p and 2p+1 are the preferred and the other answer of pair p
+ * (B even); the loss of mimose_op_preference_loss.
+ *   ref_logp   host fp32 [B]: sum of the reference model's log-probabilities over a sample's scored
+ *              positions (mimose_score)
+ *   margin     host fp32 [B/2], or NULL; needs loss
+ * mimose_train_step_policy: the loss of mimose_op_policy_loss over the scored positions.
+ *   old_logp, ref_logp (NULL without a KL term), advantage, weight (NULL: the mean over the scored
+ *              positions)   host fp32 [B,L], positions that are not scored may hold anything finite
+ *   stats      host fp32 [3]: loss, KL term, clipped share; or NULL; needs loss
+ * Errors: as mimose_train_step, plus INVALID_ARG for settings out of range and an odd B.
+ */
+typedef struct { float beta, smoothing; } mimose_preference_cfg;
+typedef struct { float clip_low, clip_high, kl_weight; } mimose_policy_cfg;
+int mimose_train_step_preference(mimose_ctx* ctx, const int32_t* tokens_host, const int32_t* labels_host,
+                                 const int32_t* lengths_host, const float* ref_logp, int32_t B, int32_t L,
+                                 const mimose_preference_cfg* cfg, float* loss, float* margin,
+                                 uint64_t* peak_bytes, uint64_t* plan_id);
+int mimose_train_step_policy(mimose_ctx* ctx, const int32_t* tokens_host, const int32_t* labels_host,
+                             const int32_t* lengths_host, const float* old_logp, const float* ref_logp,
+                             const float* advantage, const float* weight, int32_t B, int32_t L,
+                             const mimose_policy_cfg* cfg, float* loss, float* stats,
+                             uint64_t* peak_bytes, uint64_t* plan_id);
+
+/* Log-probability of every label under the model as it is: forward alone, without dropout, layers keeping
+ * nothing but their outputs; waits.  logp: host fp32 [B,L], 0 where nothing is scored.  No iteration:
+ * gradients, planner, statistics and dropout's numbering stay as they are.  peak_bytes may be NULL.
+ * Errors: as mimose_train_step_padded. */
+int mimose_score(mimose_ctx* ctx, const int32_t* tokens_host, const int32_t* labels_host,
+                 const int32_t* lengths_host, int32_t B, int32_t L, float* logp, uint64_t* peak_bytes);
+
+/*
  * Dropout, as the fine-tuning tasks of Section 6.1 train with it.  p_hidden acts on the
  * embedding output, on the attention block's output projection and on the feed-forward block's
  * output (each before its residual sum); kept elements are scaled by 1/(1-p).  The masks come
@@ -206,6 +243,10 @@ typedef struct {
   float lr, beta1, beta2, eps, weight_decay;
 } mimose_adamw_cfg;
 int mimose_optimizer_init(mimose_ctx* ctx, const mimose_adamw_cfg* cfg);
+/* The same with moments of state_bits per element: 32 (mimose_optimizer_init), or 8, as mimose_op_adamw_step
+ * describes: 6 bytes less per parameter among the input-independent memory, which leaves that much of the
+ * budget to activations.  Errors: also INVALID_ARG for another state_bits. */
+int mimose_optimizer_init_states(mimose_ctx* ctx, const mimose_adamw_cfg* cfg, int32_t state_bits);
 int mimose_optimizer_step(mimose_ctx* ctx);
 
 /* Test hook: plan >= 0 forces that bitmask on every following step (0 = keep everything)
@@ -393,9 +434,9 @@ int mimose_op_softmax_xent(int32_t dtype, void* logits, int64_t ld, const int32_
  * A label outside [0, V) leaves its row out: the logits are not read (they may hold anything), logp is
  * 0, the gradient 0.  dlogits (optional, storage type, leading dimension ld): the gradient, zeros in
  * columns >= V; NULL: the loss alone; logits itself: in place; any other overlap is INVALID_ARG.
- * Logits of any alignment and ld; rows of whole 16-byte chunks on 16-byte addresses run fastest.
- * workspace: device scratch of mimose_op_token_loss_workspace_bytes(T), 16-byte aligned; only the preference
- * loss needs it, the others then split long rows where there are few (NULL: they do not).
+ * Logits of any alignment and ld (dlogits too; fastest where every row begins and ends on a 16-byte address).
+ * workspace: device scratch of mimose_op_token_loss_workspace_bytes(T), 16-byte aligned, which a caller can
+ * hand to all three; the preference loss needs it, the other two use none and take NULL as well.
  * mimose_last_error(NULL) says why a call was refused.
  */
 uint64_t mimose_op_token_loss_workspace_bytes(int32_t T);

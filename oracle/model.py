@@ -285,7 +285,7 @@ def layer_backward(cfg: Cfg, P, l: int, S, dout, G: Dict[str, np.ndarray]):
 # --------------------------------------------------------------------------
 def train_step(cfg: Cfg, params: Dict[str, np.ndarray], tokens: np.ndarray,
                labels: np.ndarray, plan: int = 0, dtype=np.float64,
-               return_logits: bool = False, lengths=None, dropout: "Dropout" = None):
+               return_logits: bool = False, lengths=None, dropout: "Dropout" = None, loss_fn=None):
     """Loss and gradients for one mini-batch.
 
     plan: bitmask, bit l set = layer l drops its activations after its forward
@@ -293,6 +293,7 @@ def train_step(cfg: Cfg, params: Dict[str, np.ndarray], tokens: np.ndarray,
     lengths (optional, [B]): real tokens per sample of a batch padded to L; padded keys are
     masked in every attention and padded positions carry no label.
     dropout (optional): see Dropout; None or zero probabilities leave every value as it is.
+    loss_fn (optional): (logits[T, V], labels[T]) -> loss, dlogits in place of the mean cross-entropy.
     """
     P = {k: np.asanyarray(v, dtype=dtype) for k, v in params.items()}
     B, L = tokens.shape
@@ -338,7 +339,7 @@ def train_step(cfg: Cfg, params: Dict[str, np.ndarray], tokens: np.ndarray,
     else:
         t = hs
         logits = t @ P["tok_emb"].T
-    loss, dlogits = cross_entropy(logits, lab)
+    loss, dlogits = (loss_fn or cross_entropy)(logits, lab)
 
     G: Dict[str, np.ndarray] = {}
     # head backward (the tied decoder's contribution to tok_emb comes first)

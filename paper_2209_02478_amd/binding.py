@@ -49,6 +49,14 @@ class mimose_adamw_cfg(C.Structure):
     _fields_ = [(n, C.c_float) for n in ("lr", "beta1", "beta2", "eps", "weight_decay")]
 
 
+class mimose_preference_cfg(C.Structure):
+    _fields_ = [(n, C.c_float) for n in ("beta", "smoothing")]
+
+
+class mimose_policy_cfg(C.Structure):
+    _fields_ = [(n, C.c_float) for n in ("clip_low", "clip_high", "kl_weight")]
+
+
 class mimose_adamw_tensor(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("master", "lowp", "grad", "m", "v", "m_scale", "v_scale")] + \
                [("n", C.c_int64), ("decay", C.c_int32), ("reserved_", C.c_int32)]
@@ -76,6 +84,11 @@ SIGNATURES = {
     "mimose_train_step": (C.c_int, [_vp, _vp, _vp, _i32, _i32, C.POINTER(_f32), C.POINTER(_u64), C.POINTER(_u64)]),
     "mimose_train_step_padded": (C.c_int, [_vp, _vp, _vp, _vp, _i32, _i32, C.POINTER(_f32), C.POINTER(_u64),
                                            C.POINTER(_u64)]),
+    "mimose_train_step_preference": (C.c_int, [_vp, _vp, _vp, _vp, _vp, _i32, _i32, C.POINTER(mimose_preference_cfg), C.POINTER(_f32),
+                                               _vp, C.POINTER(_u64), C.POINTER(_u64)]),
+    "mimose_train_step_policy": (C.c_int, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, C.POINTER(mimose_policy_cfg),
+                                           C.POINTER(_f32), _vp, C.POINTER(_u64), C.POINTER(_u64)]),
+    "mimose_score": (C.c_int, [_vp, _vp, _vp, _vp, _i32, _i32, _vp, C.POINTER(_u64)]),
     "mimose_sync_loss": (C.c_int, [_vp, C.POINTER(_f32)]),
     "mimose_set_collector": (C.c_int, [_vp, _i32]),
     "mimose_set_dropout": (C.c_int, [_vp, _f32, _f32, _u64, _u64]),
@@ -84,6 +97,7 @@ SIGNATURES = {
     "mimose_get_grad": (C.c_int, [_vp, _i32, _vp, _u64]),
     "mimose_get_param": (C.c_int, [_vp, _i32, _vp, _u64]),
     "mimose_optimizer_init": (C.c_int, [_vp, _vp]),
+    "mimose_optimizer_init_states": (C.c_int, [_vp, _vp, _i32]),
     "mimose_optimizer_step": (C.c_int, [_vp]),
     "mimose_force_plan": (C.c_int, [_vp, _i64]),
     "mimose_set_plan_mode": (C.c_int, [_vp, _i32]),
@@ -236,6 +250,63 @@ def mimose_train_step_padded(ctx, tokens: np.ndarray, labels: np.ndarray, length
     return (loss.value if wait else None), peak.value, plan.value
 
 
+def _batch(tokens, labels, lengths):
+    t = np.ascontiguousarray(tokens, dtype=np.int32)
+    l = np.ascontiguousarray(labels, dtype=np.int32)
+    n = None if lengths is None else np.ascontiguousarray(lengths, dtype=np.int32)
+    if l.shape != t.shape or t.ndim != 2:
+        raise ValueError("tokens and labels must be of one shape [B, L]")
+    if n is not None and n.shape != (t.shape[0],):
+        raise ValueError("lengths must have one entry per sample")
+    return t, l, n
+
+
+def _floats(a, shape, name):
+    if a is None:
+        return None
+    a = np.ascontiguousarray(a, dtype=np.float32)
+    if a.shape != shape:
+        raise ValueError(f"{name} must have the shape {shape}")
+    return a
+
+
+def mimose_train_step_preference(ctx, tokens, labels, ref_logp, beta=0.1, smoothing=0.0, lengths=None, wait=True):
+    """Returns loss, margins, peak bytes and plan; wait=False queues the iteration, loss and margins are None."""
+    t, l, n = _batch(tokens, labels, lengths)
+    B, L = t.shape
+    ref = _floats(ref_logp, (B,), "ref_logp")
+    margin = np.empty(B // 2, dtype=np.float32) if wait else None
+    loss, peak, plan = _f32(), _u64(), _u64()
+    cfg = mimose_preference_cfg(beta, smoothing)
+    _check(load_library().mimose_train_step_preference(ctx, _ptr(t), _ptr(l), _ptr(n), _ptr(ref), B, L, C.byref(cfg),
+                                                       C.byref(loss) if wait else None, _ptr(margin), C.byref(peak), C.byref(plan)), ctx)
+    return (loss.value if wait else None), margin, peak.value, plan.value
+
+
+def mimose_train_step_policy(ctx, tokens, labels, old_logp, advantage, ref_logp=None, weight=None, clip_low=0.2, clip_high=0.2,
+                             kl_weight=0.0, lengths=None, wait=True):
+    """Returns loss, stats (loss, KL term, clipped share), peak bytes and plan; wait=False: loss and stats are None."""
+    t, l, n = _batch(tokens, labels, lengths)
+    B, L = t.shape
+    old, adv, ref, w = (_floats(a, (B, L), name) for a, name in ((old_logp, "old_logp"), (advantage, "advantage"), (ref_logp, "ref_logp"),
+                                                                (weight, "weight")))
+    stats = np.empty(3, dtype=np.float32) if wait else None
+    loss, peak, plan = _f32(), _u64(), _u64()
+    cfg = mimose_policy_cfg(clip_low, clip_high, kl_weight)
+    _check(load_library().mimose_train_step_policy(ctx, _ptr(t), _ptr(l), _ptr(n), _ptr(old), _ptr(ref), _ptr(adv), _ptr(w), B, L,
+                                                   C.byref(cfg), C.byref(loss) if wait else None, _ptr(stats), C.byref(peak),
+                                                   C.byref(plan)), ctx)
+    return (loss.value if wait else None), stats, peak.value, plan.value
+
+
+def mimose_score(ctx, tokens, labels, lengths=None) -> np.ndarray:
+    """Log-probability of each label, [B, L]; 0 where nothing is scored."""
+    t, l, n = _batch(tokens, labels, lengths)
+    logp = np.empty(t.shape, dtype=np.float32)
+    _check(load_library().mimose_score(ctx, _ptr(t), _ptr(l), _ptr(n), t.shape[0], t.shape[1], _ptr(logp), None), ctx)
+    return logp
+
+
 def mimose_dry_step(ctx, B: int, L: int) -> Tuple[int, int]:
     peak, plan = _u64(), _u64()
     _check(load_library().mimose_dry_step(ctx, B, L, C.byref(peak), C.byref(plan)), ctx)
@@ -257,6 +328,11 @@ def mimose_get_param(ctx, i: int, n_elems: int) -> np.ndarray:
 def mimose_optimizer_init(ctx, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01):
     cfg = mimose_adamw_cfg(lr, beta1, beta2, eps, weight_decay)
     _check(load_library().mimose_optimizer_init(ctx, C.addressof(cfg)), ctx)
+
+
+def mimose_optimizer_init_states(ctx, state_bits, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01):
+    cfg = mimose_adamw_cfg(lr, beta1, beta2, eps, weight_decay)
+    _check(load_library().mimose_optimizer_init_states(ctx, C.addressof(cfg), state_bits), ctx)
 
 
 def mimose_optimizer_step(ctx):
@@ -551,6 +627,15 @@ class Mimose:
             return mimose_train_step_padded(self.ctx, tokens, labels, lengths, wait)
         return mimose_train_step(self.ctx, tokens, labels, wait)
 
+    def train_step_preference(self, tokens, labels, ref_logp, **kw):
+        return mimose_train_step_preference(self.ctx, tokens, labels, ref_logp, **kw)
+
+    def train_step_policy(self, tokens, labels, old_logp, advantage, **kw):
+        return mimose_train_step_policy(self.ctx, tokens, labels, old_logp, advantage, **kw)
+
+    def score(self, tokens, labels, lengths=None) -> np.ndarray:
+        return mimose_score(self.ctx, tokens, labels, lengths)
+
     def sync_loss(self) -> float:
         return mimose_sync_loss(self.ctx)
 
@@ -567,8 +652,8 @@ class Mimose:
     def force_plan(self, plan: int):
         mimose_force_plan(self.ctx, plan)
 
-    def optimizer_init(self, **hyper):
-        mimose_optimizer_init(self.ctx, **hyper)
+    def optimizer_init(self, state_bits=32, **hyper):
+        mimose_optimizer_init_states(self.ctx, state_bits, **hyper)
 
     def optimizer_step(self):
         mimose_optimizer_step(self.ctx)

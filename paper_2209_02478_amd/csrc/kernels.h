@@ -162,6 +162,15 @@ struct PolicyArgs {
   float scale = 1.f, ratio_low = 0.f, ratio_high = 0.f, kl_weight = 0.f;
   float *rows = nullptr, *stats = nullptr;                         // [T, 4], [3]
 };
+// what is wrong with the settings of a loss, or null
+inline const char* bad_preference(float beta, float smoothing) {
+  return !std::isfinite(beta) || !(smoothing >= 0.f && smoothing <= 1.f) ? "beta must be finite, smoothing in [0, 1]" : nullptr;
+}
+inline const char* bad_policy(float clip_low, float clip_high, float kl_weight, bool has_ref) {
+  if (!(clip_low >= 0.f && clip_low <= 1.f) || !(clip_high >= 0.f)) return "clip_low must lie in [0, 1], clip_high must be 0 or more";
+  if (!std::isfinite(kl_weight) || kl_weight < 0.f) return "kl_weight must be finite and 0 or more";
+  return kl_weight > 0.f && !has_ref ? "the KL term needs ref_logp" : nullptr;
+}
 size_t token_loss_workspace_bytes(int T);
 void token_logprob(int dtype, const void* logits, int64_t ldl, const int32_t* labels, float* logp, int T, int V, hipStream_t st);
 void preference_loss(int dtype, const void* logits, int64_t ldl, const int32_t* labels, const PreferenceArgs& a, void* dlogits, float* logp,

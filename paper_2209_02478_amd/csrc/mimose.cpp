@@ -14,6 +14,7 @@
 #include <cmath>
 #include <cstring>
 #include <memory>
+#include <new>
 #include <string>
 #include <utility>
 #include <vector>
@@ -61,11 +62,18 @@ struct Param {
   int64_t n = 0;
   void* w = nullptr;    // storage dtype
   float* g = nullptr;   // fp32 gradient
-  // optimizer state (after mimose_optimizer_init): moments, and an fp32 master copy when the
-  // storage type is narrower than fp32 (for fp32 storage the parameter itself is the master)
-  float* m = nullptr;
-  float* v = nullptr;
+  // after mimose_optimizer_init: the fp32 master copy when the storage type is narrower than fp32 (for
+  // fp32 storage the parameter itself)
   float* master = nullptr;
+};
+
+// what an iteration minimises; pointers are host memory, borrowed for the call
+struct Objective {
+  enum Kind { CROSS_ENTROPY, PREFERENCE, POLICY, SCORE } kind = CROSS_ENTROPY;   // (SCORE: forward alone)
+  const float *old = nullptr, *ref = nullptr, *advantage = nullptr, *weight = nullptr;
+  mimose_preference_cfg preference = {0.f, 0.f};
+  mimose_policy_cfg policy = {0.f, 0.f, 0.f};
+  float *margin = nullptr, *stats = nullptr, *logp = nullptr;                    // results, optional
 };
 
 struct LayerIdx { int wqkv, bqkv, wo, bo, ln1g, ln1b, w1, b1, w2, b2, ln2g, ln2b; };
@@ -120,6 +128,8 @@ struct mimose_ctx {
   mk::AdamTensor* opt_tensors = nullptr;   // device tables
   mk::AdamChunk* opt_chunks = nullptr;
   int opt_n_chunks = 0;
+  int opt_bits = 32;                       // of a moment's element
+  mk::Adam8Tensor* opt_tensors8 = nullptr; // the table where that is 8
   mimose_stats stats;
   std::string err;
   // pinned host staging for ids / labels / sort order / segments and the loss
@@ -226,8 +236,8 @@ double attention_pairs(int B, int L, const int32_t* lengths) {
 // ------------------------------------------------------------------ step executor
 class Step {
  public:
-  Step(mimose_ctx* c, int B, int L, uint64_t plan, bool collect)
-      : c_(c), f_(c->cfg), B_(B), L_(L), T_(B * L), Tpad_(B * L), plan_(plan), collect_(collect), dry_(c->dry),
+  Step(mimose_ctx* c, const Objective& objective, int B, int L, uint64_t plan, bool collect)
+      : c_(c), f_(c->cfg), obj_(objective), B_(B), L_(L), T_(B * L), Tpad_(B * L), plan_(plan), collect_(collect), dry_(c->dry),
         st_(c->stream), dt_(c->cfg.dtype), es_(c->elt()) {}
 
   void run(const int32_t* tokens, const int32_t* labels, float* loss_out, bool wait);
@@ -261,6 +271,7 @@ class Step {
  private:
   mimose_ctx* c_;
   const mimose_model_cfg& f_;
+  const Objective& obj_;
   const int32_t* lens_host = nullptr;
   int B_, L_;
   int T_, Tpad_;        // rows of the step; rows its tensors are allocated for (B * L)
@@ -285,6 +296,32 @@ class Step {
   bool wide_ = false;   // fp32 residual sums and gradient carriers
   int stage_turn_ = 0;  // which pinned staging buffer this step uses
   int n_seg_ = 0, n_valid_ = 0;
+  // The objective's numbers pass through the staging buffer: per row (policy) or per sample (preference) on the way in,
+  // per pair (preference) or per row (score) on the way out.
+  size_t extra_at_ = 0;                   // where they begin, in ints
+  int64_t extra_in() const {
+    if (obj_.kind == Objective::PREFERENCE) return B_;
+    return obj_.kind == Objective::POLICY ? (2 + (obj_.ref != nullptr) + (obj_.weight != nullptr)) * (int64_t)T_ : 0;
+  }
+  int64_t extra_out() const {
+    if (obj_.kind == Objective::PREFERENCE) return B_ / 2;
+    return obj_.kind == Objective::SCORE ? T_ : 0;
+  }
+  float* extra_host() const { return (float*)(c_->stage + extra_at_); }
+  // the staged numbers in device memory, behind everything the step has queued
+  const float* extra_to_device(float* dev) {
+    HIPCHK(c_, hipMemcpyAsync(dev, extra_host(), (size_t)extra_in() * 4, hipMemcpyHostToDevice, st_));
+    mark_stage();
+    return dev;
+  }
+  void extra_from_device(const float* dev) {
+    HIPCHK(c_, hipMemcpyAsync(extra_host() + extra_in(), dev, (size_t)extra_out() * 4, hipMemcpyDeviceToHost, st_));
+    mark_stage();
+  }
+  void mark_stage() {                     // the last copy out of, or into, this staging buffer so far
+    HIPCHK(c_, hipEventRecord(c_->ev_stage[stage_turn_], st_));
+    c_->stage_busy[stage_turn_] = true;
+  }
 
   // times everything enqueued during its lifetime as one launch of kernel class `cls`
   struct Timed {
@@ -528,6 +565,7 @@ class Step {
   bool split_forward() const;
   void cross_sync();
   void layer_backward(int l, LayerActs& A);
+  void objective(void* logits, int64_t ldv, float* per_row, float* loss_dev);
   void head(float* loss_dev);
   void embed_backward();
 };
@@ -561,7 +599,8 @@ void Step::embed_stage(const int32_t* tokens, const int32_t* labels) {
 
   // host side: stable sort of positions by token id, run boundaries of equal ids
   const int64_t n_tables = packed_ ? n_table_ints() : B_;
-  const size_t need = (size_t)(4 * TP + 1 + n_tables);
+  extra_at_ = (size_t)(4 * TP + 1 + n_tables);
+  const size_t need = extra_at_ + (size_t)(extra_in() + extra_out());
   const int turn = c_->stage_turn;
   c_->stage_turn ^= 1;
   if (c_->stage_busy[turn]) {               // copies of the step before last out of this buffer: long done
@@ -594,6 +633,18 @@ void Step::embed_stage(const int32_t* tokens, const int32_t* labels) {
   } else {
     std::memcpy(s, tokens, (size_t)T_ * 4);
     std::memcpy(s + TP, labels, (size_t)T_ * 4);
+  }
+  if (obj_.kind == Objective::PREFERENCE) std::memcpy(extra_host(), obj_.ref, (size_t)B_ * 4);
+  if (obj_.kind == Objective::POLICY) {
+    float* to = extra_host();
+    for (const float* from : {obj_.old, obj_.advantage, obj_.ref, obj_.weight}) {
+      if (!from) continue;
+      for (int b = 0; b < B_; ++b) {
+        const int64_t t = first_row(b), n = first_row(b + 1) - t;
+        std::memcpy(to + t, from + (size_t)b * L_, (size_t)n * 4);
+      }
+      to += T_;
+    }
   }
   HIPCHK(c_, hipMemcpyAsync(ints, s, 2 * (size_t)TP * 4, hipMemcpyHostToDevice, st_));
   Timed t(this, MIMOSE_K_EMBED_FWD, (f_.pre_ln ? 3.0 : 4.0) * T_ * H * es_d());
@@ -821,13 +872,50 @@ void Step::layer_backward(int l, LayerActs& A) {
   }
 }
 
+// The loss and its gradient in place of the logits; log-probabilities alone where the step scores.  Memory that only an
+// objective needs is taken here, as part of the head's transient.
+void Step::objective(void* logits, int64_t ldv, float* per_row, float* loss_dev) {
+  const int V = f_.vocab;
+  auto floats = [&](int64_t n) { return (float*)c_->arena.alloc((uint64_t)n * 4); };
+  if (obj_.kind == Objective::CROSS_ENTROPY) {
+    if (!dry_) mk::softmax_xent(dt_, logits, ldv, labels_, per_row, loss_dev, T_, V, n_valid_, st_);
+  } else if (obj_.kind == Objective::SCORE) {
+    if (dry_) return;
+    mk::token_logprob(dt_, logits, ldv, labels_, per_row, T_, V, st_);
+    extra_from_device(per_row);
+  } else if (obj_.kind == Objective::PREFERENCE) {
+    float* ref = floats(B_);
+    mk::PreferenceArgs a;
+    a.seq_logp = floats(B_); a.margin = floats(B_ / 2); a.loss = loss_dev;
+    void* workspace = c_->arena.alloc(mk::token_loss_workspace_bytes(Tpad_));
+    if (dry_) return;
+    a.ends = ends_; a.pairs = B_ / 2; a.L = L_; a.ref_logp = extra_to_device(ref);
+    a.beta = obj_.preference.beta; a.smoothing = obj_.preference.smoothing;
+    mk::preference_loss(dt_, logits, ldv, labels_, a, logits, per_row, T_, V, workspace, st_);
+    if (obj_.margin) extra_from_device(a.margin);
+  } else {
+    const int arrays = 2 + (obj_.ref != nullptr) + (obj_.weight != nullptr);
+    float* in = floats(arrays * (int64_t)Tpad_);
+    mk::PolicyArgs a;
+    a.rows = floats(4 * (int64_t)Tpad_); a.stats = loss_dev;
+    if (dry_) return;
+    const float* p = extra_to_device(in);
+    a.old_logp = p; a.advantage = p += T_;
+    if (obj_.ref) a.ref_logp = p += T_;
+    if (obj_.weight) a.weight = p += T_;
+    a.scale = obj_.weight ? 1.f : 1.f / (float)(n_valid_ > 0 ? n_valid_ : 1);
+    a.ratio_low = 1.f - obj_.policy.clip_low; a.ratio_high = 1.f + obj_.policy.clip_high; a.kl_weight = obj_.policy.kl_weight;
+    mk::policy_loss(dt_, logits, ldv, labels_, a, logits, T_, V, st_);
+  }
+}
+
 // Head forward, loss, head backward.  Leaves the gradient of the last layer's output in gA_.
 void Step::head(float* loss_dev) {
   const int H = f_.hidden, V = f_.vocab;
   const int64_t TH = (int64_t)Tpad_ * H, ldv = c_->ldv();
   const int gelu = f_.gelu_tanh ? mk::GELU_TANH : mk::GELU_ERF;
   const void* hlast = f_.n_layers ? c_->acts[f_.n_layers - 1].out : h0_;
-  reserve_workspace({{V, H}, {H, H}});
+  if (obj_.kind != Objective::SCORE) reserve_workspace({{V, H}, {H, H}});
   const void* hs = hlast;
   void* hs_buf = nullptr;
   if (f_.pre_ln) { hs_buf = talloc(TH); ln_fwd(hlast, c_->i_fg, c_->i_fb, hs_buf); hs = hs_buf; }
@@ -847,9 +935,10 @@ void Step::head(float* loss_dev) {
     gemm(a);
   }
   {
-    Timed t(this, MIMOSE_K_XENT, 2.0 * T_ * ldv * es_d());
-    if (!dry_) mk::softmax_xent(dt_, logits, ldv, labels_, row_loss, loss_dev, T_, V, n_valid_, st_);
+    Timed t(this, MIMOSE_K_XENT, (obj_.kind == Objective::SCORE ? 1.0 : 2.0) * T_ * ldv * es_d());
+    objective(logits, ldv, row_loss, loss_dev);
   }
+  if (obj_.kind == Objective::SCORE) return;
   // tied decoder: its weight gradient overwrites the embedding gradient, the embedding
   // backward adds onto it later
   {
@@ -910,8 +999,7 @@ void Step::embed_sort() {
   int32_t* order = s + 2 * (size_t)Tpad_;
   each_position([&](int t) { order[count[ids[t]]++] = t; });
   HIPCHK(c_, hipMemcpyAsync(order_, order, (2 * (size_t)Tpad_ + 1) * 4, hipMemcpyHostToDevice, st_));
-  HIPCHK(c_, hipEventRecord(c_->ev_stage[stage_turn_], st_));     // the last copy out of this staging buffer
-  c_->stage_busy[stage_turn_] = true;
+  mark_stage();
 }
 
 void Step::embed_backward() {
@@ -937,7 +1025,8 @@ void Step::run(const int32_t* tokens, const int32_t* labels, float* loss_out, bo
     }
   }
   const uint64_t base = ar.top();
-  float* loss_dev = (float*)ar.alloc(4);
+  const size_t loss_bytes = obj_.kind == Objective::POLICY ? 12 : 4;    // (with the KL term and the clipped share)
+  float* loss_dev = (float*)ar.alloc(loss_bytes);
   embed_stage(tokens, labels);
   e_bytes = ar.top() - base;
 
@@ -989,10 +1078,23 @@ void Step::run(const int32_t* tokens, const int32_t* labels, float* loss_out, bo
       throw StepError{MIMOSE_ERR_HIP, "join of the forward streams failed"};
   }
 
-  embed_sort();                           // host work hidden behind the queued forward
+  if (obj_.kind != Objective::SCORE) embed_sort();          // host work hidden behind the queued forward
   const uint64_t m_head = ar.top();
   ar.begin_section();
   head(loss_dev);
+  if (obj_.kind == Objective::SCORE) {
+    HIPCHK(c_, hipStreamSynchronize(st_));
+    HIPCHK(c_, hipGetLastError());
+    const float* got = extra_host() + extra_in();
+    for (int b = 0; b < B_; ++b) {
+      const int64_t t = first_row(b), n = first_row(b + 1) - t;
+      std::memcpy(obj_.logp + (size_t)b * L_, got + t, (size_t)n * 4);
+      std::fill(obj_.logp + (size_t)b * L_ + n, obj_.logp + (size_t)(b + 1) * L_, 0.f);
+    }
+    c_->prof_pending.clear();
+    c_->ev_used = 0;
+    return;
+  }
   g_bytes = ar.section_high() - m_head;
   ar.pop_to(m_head);
 
@@ -1011,7 +1113,7 @@ void Step::run(const int32_t* tokens, const int32_t* labels, float* loss_out, bo
   join();
   embed_backward();
   if (!dry_) {
-    HIPCHK(c_, hipMemcpyAsync(c_->loss_host, loss_dev, 4, hipMemcpyDeviceToHost, st_));
+    HIPCHK(c_, hipMemcpyAsync(c_->loss_host, loss_dev, loss_bytes, hipMemcpyDeviceToHost, st_));
     c_->loss_pending = true;
     // the caller does not want the loss now: the step stays queued and the host runs ahead
     // (collecting steps read their layer timers, profiled steps their events: they wait)
@@ -1020,6 +1122,8 @@ void Step::run(const int32_t* tokens, const int32_t* labels, float* loss_out, bo
     HIPCHK(c_, hipGetLastError());
     c_->loss_pending = false;
     *loss_out = *c_->loss_host;
+    if (obj_.margin) std::memcpy(obj_.margin, extra_host() + extra_in(), (size_t)(B_ / 2) * 4);
+    if (obj_.stats) std::memcpy(obj_.stats, c_->loss_host, 12);
     for (auto& p : c_->prof_pending) {
       float ms = 0.f;
       if (hipEventElapsedTime(&ms, p.a, p.b) == hipSuccess) {
@@ -1052,8 +1156,8 @@ void flops(const mimose_model_cfg& f, int B, int L, const int32_t* lengths, uint
   *useful = 3.0 * (layers + T * head);
 }
 
-int do_step(mimose_ctx* c, const int32_t* tokens, const int32_t* labels, const int32_t* lengths, int32_t B, int32_t L,
-            bool dry, float* loss, uint64_t* peak, uint64_t* plan_id) {
+// the batch of a step, or of a score: what is wrong with it is left in the context
+int check_batch(mimose_ctx* c, const int32_t* tokens, const int32_t* labels, const int32_t* lengths, int32_t B, int32_t L, bool dry) {
   const auto& f = c->cfg;
   if (B < 1 || L < 1 || L > f.max_seq) return fail(c, MIMOSE_ERR_INVALID_ARG, "B >= 1 and 1 <= L <= max_seq required");
   if ((int64_t)B * L > (int64_t)1 << 28) return fail(c, MIMOSE_ERR_INVALID_ARG, "B*L too large");
@@ -1069,6 +1173,27 @@ int do_step(mimose_ctx* c, const int32_t* tokens, const int32_t* labels, const i
       for (int b = 0; b < B; ++b)
         if (lengths[b] < 1 || lengths[b] > L) return fail(c, MIMOSE_ERR_INVALID_ARG, "sample length outside [1, L]");
   }
+  return MIMOSE_OK;
+}
+
+// an abandoned step: the arena is reset, nothing of it is left on the device
+void abandon(mimose_ctx* c, bool dry) {
+  c->prof_pending.clear(); c->ev_used = 0;
+  c->arena.pop_to(c->fixed_top);
+  if (!dry && c->has_device) { if (c->side) (void)hipStreamSynchronize(c->side); (void)hipStreamSynchronize(c->stream); }
+}
+int fail_oom(mimose_ctx* c, const OomError& e) {
+  char buf[160];
+  snprintf(buf, sizeof buf, "allocation of %llu bytes at %llu exceeds the budget of %llu bytes",
+           (unsigned long long)e.want, (unsigned long long)e.top, (unsigned long long)e.cap);
+  return fail(c, MIMOSE_ERR_OOM_BUDGET, buf);
+}
+
+int do_step(mimose_ctx* c, const int32_t* tokens, const int32_t* labels, const int32_t* lengths, int32_t B, int32_t L,
+            bool dry, float* loss, uint64_t* peak, uint64_t* plan_id, const Objective& objective = Objective()) {
+  const auto& f = c->cfg;
+  const int bad = check_batch(c, tokens, labels, lengths, B, L, dry);
+  if (bad != MIMOSE_OK) return bad;
   const int64_t x = (int64_t)B * L;
   const uint64_t all = f.n_layers >= 64 ? ~(uint64_t)0 : (((uint64_t)1 << f.n_layers) - 1);
   // ---- plan (host only, on the critical path of every iteration)
@@ -1106,20 +1231,18 @@ int do_step(mimose_ctx* c, const int32_t* tokens, const int32_t* labels, const i
                           std::chrono::steady_clock::now() - t0).count();
   // ---- run
   c->dry = dry;
-  Step s(c, B, L, plan, collect);
+  Step s(c, objective, B, L, plan, collect);
   // A cost-aware planner keeps a layer's forward time at x = B * L (Section 4.1), so its collecting steps
   // run the batch whole: the time of the rows that are left says nothing about that size (2 x 768-wide
   // layers, 32 x 256 with a quarter of the rows real: 0.14 ms against the whole batch's 0.25).  In bf16
   // the bits are those of the steps that leave padding out; fp32 sums are not, so there no step of such
   // a context leaves any out.
-  if (!dry && lengths) s.set_lengths(lengths, f.cost_aware && (collect || f.dtype == mk::F32));
   float lv = 0.f;
   try {
+    if (!dry && lengths) s.set_lengths(lengths, f.cost_aware && (collect || f.dtype == mk::F32));
     s.run(tokens, labels, &lv, dry || loss != nullptr);
   } catch (const OomError& e) {
-    c->prof_pending.clear(); c->ev_used = 0;
-    c->arena.pop_to(c->fixed_top);
-    if (!dry && c->has_device) { if (c->side) (void)hipStreamSynchronize(c->side); (void)hipStreamSynchronize(c->stream); }
+    abandon(c, dry);
     // A plan of the planner's own that does not fit means the estimator under-predicted (the paper
     // keeps 0.5-1 GB free for that, Section 6.4).  The cached plan would fail again on every batch
     // of this size, so it is dropped and the key planned anew against what was missing; the
@@ -1128,17 +1251,15 @@ int do_step(mimose_ctx* c, const int32_t* tokens, const int32_t* labels, const i
       mimose::PlanOut po;
       if (c->planner->replan(xq_planned, (int64_t)(e.top + e.want - e.cap), plan, &po)) {
         c->stats.replans++;
-        return do_step(c, tokens, labels, lengths, B, L, dry, loss, peak, plan_id);
+        return do_step(c, tokens, labels, lengths, B, L, dry, loss, peak, plan_id, objective);
       }
     }
-    char buf[160];
-    snprintf(buf, sizeof buf, "allocation of %llu bytes at %llu exceeds the budget of %llu bytes",
-             (unsigned long long)e.want, (unsigned long long)e.top, (unsigned long long)e.cap);
-    return fail(c, MIMOSE_ERR_OOM_BUDGET, buf);
+    return fail_oom(c, e);
+  } catch (const std::bad_alloc&) {
+    abandon(c, dry);
+    return fail(c, MIMOSE_ERR_INVALID_ARG, "no host memory for a batch of this size");
   } catch (const StepError& e) {
-    c->prof_pending.clear(); c->ev_used = 0;
-    c->arena.pop_to(c->fixed_top);
-    if (!dry && c->has_device) { if (c->side) (void)hipStreamSynchronize(c->side); (void)hipStreamSynchronize(c->stream); }
+    abandon(c, dry);
     if (e.code == MIMOSE_ERR_HIP) (void)hipGetLastError();        // reported here, not by the next step too
     return fail(c, e.code, e.msg);
   }
@@ -1312,6 +1433,68 @@ int mimose_train_step_padded(mimose_ctx* c, const int32_t* tokens, const int32_t
   return do_step(c, tokens, labels, lengths, B, L, false, loss, peak, plan_id);
 }
 
+int mimose_train_step_preference(mimose_ctx* c, const int32_t* tokens, const int32_t* labels, const int32_t* lengths,
+                                 const float* ref_logp, int32_t B, int32_t L, const mimose_preference_cfg* cfg, float* loss,
+                                 float* margin, uint64_t* peak, uint64_t* plan_id) {
+  if (!c) return MIMOSE_ERR_INVALID_ARG;
+  if (!cfg || !ref_logp) return fail(c, MIMOSE_ERR_INVALID_ARG, "cfg and ref_logp must be given");
+  if (const char* why = mk::bad_preference(cfg->beta, cfg->smoothing)) return fail(c, MIMOSE_ERR_INVALID_ARG, why);
+  if (B < 2 || B % 2) return fail(c, MIMOSE_ERR_INVALID_ARG, "a batch of pairs has an even number of samples");
+  if (margin && !loss) return fail(c, MIMOSE_ERR_INVALID_ARG, "margins are there once the step has been waited for: loss must be given");
+  Objective o;
+  o.kind = Objective::PREFERENCE; o.ref = ref_logp; o.preference = *cfg; o.margin = margin;
+  return do_step(c, tokens, labels, lengths, B, L, false, loss, peak, plan_id, o);
+}
+
+int mimose_train_step_policy(mimose_ctx* c, const int32_t* tokens, const int32_t* labels, const int32_t* lengths, const float* old_logp,
+                             const float* ref_logp, const float* advantage, const float* weight, int32_t B, int32_t L,
+                             const mimose_policy_cfg* cfg, float* loss, float* stats, uint64_t* peak, uint64_t* plan_id) {
+  if (!c) return MIMOSE_ERR_INVALID_ARG;
+  if (!cfg || !old_logp || !advantage) return fail(c, MIMOSE_ERR_INVALID_ARG, "cfg, old_logp and advantage must be given");
+  if (const char* why = mk::bad_policy(cfg->clip_low, cfg->clip_high, cfg->kl_weight, ref_logp != nullptr))
+    return fail(c, MIMOSE_ERR_INVALID_ARG, why);
+  if (stats && !loss) return fail(c, MIMOSE_ERR_INVALID_ARG, "stats are there once the step has been waited for: loss must be given");
+  Objective o;
+  o.kind = Objective::POLICY; o.old = old_logp; o.ref = ref_logp; o.advantage = advantage; o.weight = weight;
+  o.policy = *cfg; o.stats = stats;
+  return do_step(c, tokens, labels, lengths, B, L, false, loss, peak, plan_id, o);
+}
+
+int mimose_score(mimose_ctx* c, const int32_t* tokens, const int32_t* labels, const int32_t* lengths, int32_t B, int32_t L,
+                 float* logp, uint64_t* peak) {
+  if (!c) return MIMOSE_ERR_INVALID_ARG;
+  if (!logp) return fail(c, MIMOSE_ERR_INVALID_ARG, "logp must be given");
+  const int bad = check_batch(c, tokens, labels, lengths, B, L, false);
+  if (bad != MIMOSE_OK) return bad;
+  Objective o;
+  o.kind = Objective::SCORE; o.logp = logp;
+  // a model is scored without dropout, and keeps nothing of a layer but its output
+  const float p_hidden = c->p_hidden, p_attn = c->p_attn;
+  c->p_hidden = c->p_attn = 0.f;
+  c->dry = false;
+  int rc = MIMOSE_OK;
+  try {
+    Step s(c, o, B, L, ~(uint64_t)0, false);
+    if (lengths) s.set_lengths(lengths, false);
+    s.run(tokens, labels, nullptr, true);
+  } catch (const OomError& e) {
+    abandon(c, false);
+    rc = fail_oom(c, e);
+  } catch (const StepError& e) {
+    abandon(c, false);
+    if (e.code == MIMOSE_ERR_HIP) (void)hipGetLastError();
+    rc = fail(c, e.code, e.msg);
+  } catch (const std::bad_alloc&) {
+    abandon(c, false);
+    rc = fail(c, MIMOSE_ERR_INVALID_ARG, "no host memory for a batch of this size");
+  }
+  c->p_hidden = p_hidden; c->p_attn = p_attn;
+  if (rc != MIMOSE_OK) return rc;
+  if (peak) *peak = c->arena.high();
+  c->arena.pop_to(c->fixed_top);
+  return MIMOSE_OK;
+}
+
 int mimose_sync_loss(mimose_ctx* c, float* loss) {
   if (!c) return MIMOSE_ERR_INVALID_ARG;
   if (!c->has_device) return fail(c, MIMOSE_ERR_NOT_READY, "host-only context");
@@ -1376,46 +1559,65 @@ int mimose_get_param(mimose_ctx* c, int32_t i, float* host, uint64_t n) {
   return MIMOSE_OK;
 }
 
-int mimose_optimizer_init(mimose_ctx* c, const mimose_adamw_cfg* o) {
+int mimose_optimizer_init(mimose_ctx* c, const mimose_adamw_cfg* o) { return mimose_optimizer_init_states(c, o, 32); }
+
+int mimose_optimizer_init_states(mimose_ctx* c, const mimose_adamw_cfg* o, int32_t state_bits) {
   if (!c || !o) return fail(c, MIMOSE_ERR_INVALID_ARG, "ctx and cfg must be given");
+  if (state_bits != 8 && state_bits != 32) return fail(c, MIMOSE_ERR_INVALID_ARG, "state_bits must be 8 or 32");
   if (c->opt_on) return fail(c, MIMOSE_ERR_INVALID_ARG, "the optimizer is already initialised");
   if (c->stats.steps != 0) return fail(c, MIMOSE_ERR_NOT_READY, "initialise the optimizer before the first step");
   if (const char* why = mk::bad_adamw(o->lr, o->beta1, o->beta2, o->eps, o->weight_decay)) return fail(c, MIMOSE_ERR_INVALID_ARG, why);
-  const bool narrow = c->cfg.dtype != mk::F32;
+  const bool narrow = c->cfg.dtype != mk::F32, eight = state_bits == 8;
   std::vector<mk::AdamTensor> tens;
+  std::vector<mk::Adam8Tensor> tens8;
   std::vector<mk::AdamChunk> chunks;
   const uint64_t mark = c->arena.top();
+  void* table = nullptr;                   // behind the states
+  const void* host_table = nullptr;
+  size_t table_bytes = 0;
+  void* first = nullptr;
   try {
-    for (auto& p : c->params) {
-      p.m = (float*)c->arena.alloc((uint64_t)p.n * 4);
-      p.v = (float*)c->arena.alloc((uint64_t)p.n * 4);
-      p.master = narrow ? (float*)c->arena.alloc((uint64_t)p.n * 4) : (float*)p.w;
-    }
     for (size_t i = 0; i < c->params.size(); ++i) {
-      const Param& p = c->params[i];
-      mk::AdamTensor t;
-      t.master = p.master; t.lowp = narrow ? p.w : nullptr; t.grad = p.g; t.m = p.m; t.v = p.v; t.n = p.n;
-      t.decay = p.ndim >= 2 ? 1 : 0; t.pad = 0;
-      tens.push_back(t);
+      Param& p = c->params[i];
+      const uint64_t state_bytes = (uint64_t)p.n * (eight ? 1 : 4), scales = eight ? (uint64_t)(p.n + mk::kAdamBlock - 1) / mk::kAdamBlock * 4 : 0;
+      void* m = c->arena.alloc(state_bytes);
+      void* v = c->arena.alloc(state_bytes);
+      if (!first) first = m;
+      float* ms = eight ? (float*)c->arena.alloc(scales) : nullptr;
+      float* vs = eight ? (float*)c->arena.alloc(scales) : nullptr;
+      p.master = narrow ? (float*)c->arena.alloc((uint64_t)p.n * 4) : (float*)p.w;
+      const int32_t decay = p.ndim >= 2 ? 1 : 0;
+      void* lowp = narrow ? p.w : nullptr;
+      if (eight) tens8.push_back(mk::Adam8Tensor{p.master, lowp, p.g, (uint8_t*)m, (uint8_t*)v, ms, vs, p.n, decay, 0});
+      else tens.push_back(mk::AdamTensor{p.master, lowp, p.g, (float*)m, (float*)v, p.n, decay, 0});
       for (int64_t s0 = 0; s0 < p.n; s0 += mk::kAdamChunk) chunks.push_back(mk::AdamChunk{(int32_t)i, 0, s0});
     }
-    c->opt_tensors = (mk::AdamTensor*)c->arena.alloc(tens.size() * sizeof(mk::AdamTensor));
+    table_bytes = eight ? tens8.size() * sizeof(mk::Adam8Tensor) : tens.size() * sizeof(mk::AdamTensor);
+    host_table = eight ? (const void*)tens8.data() : (const void*)tens.data();
+    table = c->arena.alloc(table_bytes);
     c->opt_chunks = (mk::AdamChunk*)c->arena.alloc(chunks.size() * sizeof(mk::AdamChunk));
   } catch (const OomError&) {
     c->arena.pop_to(mark);
-    for (auto& p : c->params) p.m = p.v = p.master = nullptr;
+    for (auto& p : c->params) p.master = nullptr;
     return fail(c, MIMOSE_ERR_OOM_BUDGET, "optimizer state does not fit in the budget");
+  } catch (const std::bad_alloc&) {
+    c->arena.pop_to(mark);
+    for (auto& p : c->params) p.master = nullptr;
+    return fail(c, MIMOSE_ERR_INVALID_ARG, "no host memory for the optimizer's table");
   }
   c->opt_n_chunks = (int)chunks.size();
+  c->opt_bits = state_bits;
+  c->opt_tensors = eight ? nullptr : (mk::AdamTensor*)table;
+  c->opt_tensors8 = eight ? (mk::Adam8Tensor*)table : nullptr;
   if (c->has_device) {
-    mk::fill_zero(c->params.front().m, (int64_t)((char*)c->opt_tensors - (char*)c->params.front().m), c->stream);
+    mk::fill_zero(first, (int64_t)((char*)table - (char*)first), c->stream);
     if (narrow)
       for (auto& p : c->params) mk::convert_to_f32(c->cfg.dtype, p.w, p.master, p.n, c->stream);
-    if (hipMemcpyAsync(c->opt_tensors, tens.data(), tens.size() * sizeof(mk::AdamTensor), hipMemcpyHostToDevice, c->stream) != hipSuccess ||
+    if (hipMemcpyAsync(table, host_table, table_bytes, hipMemcpyHostToDevice, c->stream) != hipSuccess ||
         hipMemcpyAsync(c->opt_chunks, chunks.data(), chunks.size() * sizeof(mk::AdamChunk), hipMemcpyHostToDevice, c->stream) != hipSuccess ||
         hipStreamSynchronize(c->stream) != hipSuccess) {
       c->arena.pop_to(mark);
-      for (auto& p : c->params) p.m = p.v = p.master = nullptr;
+      for (auto& p : c->params) p.master = nullptr;
       return fail(c, MIMOSE_ERR_HIP, "optimizer initialisation failed");
     }
   }
@@ -1434,7 +1636,8 @@ int mimose_optimizer_step(mimose_ctx* c) {
   if (c->stats.steps == 0) return fail(c, MIMOSE_ERR_NOT_READY, "no gradients yet: run a training step first");
   c->opt_t += 1;
   const mk::AdamHyper h = mk::adamw_hyper(c->opt.lr, c->opt.beta1, c->opt.beta2, c->opt.eps, c->opt.weight_decay, (int64_t)c->opt_t);
-  mk::adamw_update(c->cfg.dtype, c->opt_tensors, c->opt_chunks, c->opt_n_chunks, h, c->stream);
+  if (c->opt_bits == 8) mk::adamw8_update(c->opt_tensors8, c->opt_chunks, c->opt_n_chunks, h, (int64_t)c->opt_t, c->stream);
+  else mk::adamw_update(c->cfg.dtype, c->opt_tensors, c->opt_chunks, c->opt_n_chunks, h, c->stream);
   if (hipGetLastError() != hipSuccess) return fail(c, MIMOSE_ERR_HIP, "update launch failed");
   return MIMOSE_OK;
 }

@@ -204,7 +204,7 @@ int mimose_op_preference_loss(int32_t dtype, const void* logits, int64_t ld, con
   if (pairs < 1 || pairs > (1 << 24)) return refuse(op, "1 to 2^24 pairs required");
   if (!ends && (L < 0 || (int64_t)2 * pairs * L != T)) return refuse(op, "without ends, T must be 2 * pairs * L");
   if (!ref_logp || !seq_logp || !margin || !loss || (T > 0 && !logp)) return refuse(op, "ref_logp, logp, seq_logp, margin and loss must be given");
-  if (!std::isfinite(beta) || !(smoothing >= 0.f && smoothing <= 1.f)) return refuse(op, "beta must be finite, smoothing in [0, 1]");
+  if (const char* why = mk::bad_preference(beta, smoothing)) return refuse(op, why);
   if (T > 0 && (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < mk::token_loss_workspace_bytes(T)))
     return refuse(op, "workspace must be 16-byte aligned and of mimose_op_token_loss_workspace_bytes");
   mk::PreferenceArgs a;
@@ -223,9 +223,7 @@ int mimose_op_policy_loss(int32_t dtype, const void* logits, int64_t ld, const i
   if (!stats || (T > 0 && (!old_logp || !advantage || !rows))) return refuse(op, "old_logp, advantage, rows and stats must be given");
   if ((uintptr_t)rows & 15) return refuse(op, "rows must be 16-byte aligned");
   if (!std::isfinite(scale)) return refuse(op, "scale must be finite");
-  if (!(clip_low >= 0.f && clip_low <= 1.f) || !(clip_high >= 0.f)) return refuse(op, "clip_low must lie in [0, 1], clip_high must be 0 or more");
-  if (!std::isfinite(kl_weight) || kl_weight < 0.f) return refuse(op, "kl_weight must be finite and 0 or more");
-  if (kl_weight > 0.f && !ref_logp) return refuse(op, "the KL term needs ref_logp");
+  if (const char* why = mk::bad_policy(clip_low, clip_high, kl_weight, ref_logp != nullptr)) return refuse(op, why);
   if (workspace && ((uintptr_t)workspace & 15)) return refuse(op, "workspace must be 16-byte aligned");
   if (workspace && workspace_bytes < mk::token_loss_workspace_bytes(T)) return refuse(op, "workspace smaller than mimose_op_token_loss_workspace_bytes");
   mk::PolicyArgs a;
