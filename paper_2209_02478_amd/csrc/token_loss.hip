@@ -285,15 +285,17 @@ void token_rows_held_kernel(const T* logits, int64_t ldl, const int32_t* __restr
   else { M(16, 16) }
 constexpr int kMostChunks = 16384;
 
-// One block for a row, whatever its length and alignment.
+// Rows too long to be held: one block for a row, a running maximum and sum in each thread over its chunks, and for the gradient a
+// second pass over them, out of the last cache.
 // MODE 0: logp[row]; stat[row] (optional), the row's maximum and the reciprocal of its sum of exponentials; slope[row]
 // (optional) = 0, until pair_sums_kernel writes the rows of a pair.
 // MODE 1: the policy loss's numbers of the row, and its gradient where dlogits is given (it may be logits).
+constexpr int kLongThreads = 1024, kLongAhead = 4;
 template <typename T, int MODE>
-__global__ __launch_bounds__(kRowThreads) void token_rows_kernel(const T* logits, int64_t ldl, const int32_t* __restrict__ labels,
-                                                                 float* __restrict__ logp, float2* __restrict__ stat,
-                                                                 float* __restrict__ slope, T* dlogits, PolicyArgs pa, int V) {
-  constexpr int NW = kRowThreads / 64;
+__global__ __launch_bounds__(kLongThreads) void token_rows_long_kernel(const T* logits, int64_t ldl, const int32_t* __restrict__ labels,
+                                                                       float* __restrict__ logp, float2* __restrict__ stat,
+                                                                       float* __restrict__ slope, T* dlogits, PolicyArgs pa, int V) {
+  constexpr int N = Chunk<T>::N, NW = kLongThreads / 64;
   __shared__ float sm[NW], ss[NW];
   const int row = blockIdx.x, tid = threadIdx.x;
   const T* x = logits + (int64_t)row * ldl;
@@ -305,17 +307,39 @@ __global__ __launch_bounds__(kRowThreads) void token_rows_kernel(const T* logits
       if (tid == 0) logp[row] = 0.f;
     } else {
       if (tid == 0) ((float4*)pa.rows)[row] = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (g) zero_columns(g, 0, ldl, tid, kRowThreads);
+      if (g) zero_columns(g, 0, ldl, tid, kLongThreads);
     }
     return;
   }
-  float m = -INFINITY;
-  for (int c = tid; c < V; c += kRowThreads) m = fmaxf(m, ld<T>(x + c));
+  const float picked = ld<T>(x + label);
+  const int shift = shift_of(x);
+  const int64_t step = (int64_t)kLongThreads * N, first = (int64_t)tid * N - shift;   // columns
+  u32x4 raw[kLongAhead];
+  auto load = [&](int64_t col) {
+#pragma unroll
+    for (int i = 0; i < kLongAhead; ++i) {
+      const int64_t c = col + i * step;
+      raw[i] = c >= 0 && c + N <= V ? *(const u32x4*)(x + c) : load_edge(x, c, V);
+    }
+  };
+  float m = -INFINITY, s = 0.f;
+  for (int64_t col = first; col < V; col += kLongAhead * step) {
+    load(col);
+#pragma unroll
+    for (int i = 0; i < kLongAhead; ++i) {
+      float v[N], top = m;
+      Chunk<T>::values(raw[i], v);
+#pragma unroll
+      for (int e = 0; e < N; ++e) top = fmaxf(top, v[e]);
+      if (top > m) { s *= __builtin_amdgcn_exp2f((m - top) * kLog2e); m = top; }
+#pragma unroll
+      for (int e = 0; e < N; ++e) s += v[e] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((v[e] - m) * kLog2e);
+    }
+  }
+  const float own = m;
   m = block_max<NW>(m, sm);
-  float s = 0.f;
-  for (int c = tid; c < V; c += kRowThreads) s += __expf(ld<T>(x + c) - m);
-  s = block_sum<NW>(s, ss);
-  const float lp = (ld<T>(x + label) - m) - logf(s);
+  s = block_sum<NW>(own == -INFINITY && s == 0.f ? 0.f : s * __builtin_amdgcn_exp2f((own - m) * kLog2e), ss);
+  const float lp = (picked - m) - logf(s);
   if (MODE == 0) {
     if (tid == 0) {
       logp[row] = lp;
@@ -324,13 +348,23 @@ __global__ __launch_bounds__(kRowThreads) void token_rows_kernel(const T* logits
     return;
   }
   float4 kept;
-  const float d = policy_token(pa, row, lp, &kept);
+  const float d = policy_token(pa, row, lp, &kept), k = -d / s;
   if (tid == 0) ((float4*)pa.rows)[row] = kept;
   if (!g) return;
-  const float k = -d / s;
-  __syncthreads();                                      // (in place: every thread has read the label's logit)
-  for (int64_t c = tid; c < ldl; c += kRowThreads)
-    st<T>(g + c, c < V ? __expf(ld<T>(x + c) - m) * k + (c == label ? d : 0.f) : 0.f);
+  const bool aligned = shift_of(g) == shift;
+  for (int64_t col = first; col < V; col += kLongAhead * step) {
+    load(col);
+#pragma unroll
+    for (int i = 0; i < kLongAhead; ++i) {
+      const int64_t c = col + i * step;
+      float v[N];
+      chunk_gradient<T>(raw[i], m, k, d, label - c, v);
+      if (aligned && c >= 0 && c + N <= V) __builtin_nontemporal_store(Chunk<T>::bits(v), (u32x4*)(g + c));
+      else if (c < V) store_edge(g, c, V, ldl, v);
+    }
+  }
+  const int64_t behind = ((int64_t)shift + V + N - 1) / N * N - shift;
+  if (behind < ldl) zero_columns(g, behind, ldl, tid, kLongThreads);
 }
 
 // first row and end of sequence s, inside [0, T] whatever ends holds
@@ -516,7 +550,7 @@ static void rows_t(const void* logits, int64_t ldl, const int32_t* labels, float
     else if (held)
       held_t<T, MODE, true, false>(x, ldl, labels + r, lp, sta, sl, g, a, n, V, (int)chunks, st);
     else
-      hipLaunchKernelGGL((token_rows_kernel<T, MODE>), dim3(n), dim3(kRowThreads), 0, st, x, ldl, labels + r, lp, sta, sl, g, a, V);
+      hipLaunchKernelGGL((token_rows_long_kernel<T, MODE>), dim3(n), dim3(kLongThreads), 0, st, x, ldl, labels + r, lp, sta, sl, g, a, V);
   }
 }
 
