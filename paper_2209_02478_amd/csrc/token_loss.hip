@@ -36,6 +36,21 @@ __device__ __forceinline__ float block_sum(float v, float* s) {
   return v;
 }
 
+// sum of 64 * WAVES threads' numbers, in the first wave's lanes, by one barrier; red: WAVES * 64 places
+template <int WAVES>
+__device__ __forceinline__ double first_wave_sum(double v, double* red, int tid) {
+  red[tid] = v;
+  __syncthreads();
+  v = 0.0;
+  if (tid < 64) {
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) v += red[64 * w + tid];
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+  }
+  return v;
+}
+
 __device__ __forceinline__ bool is_scored(int label, int V) { return (unsigned)label < (unsigned)V; }
 
 // what the policy loss makes of one token: d loss / d logp, and the four numbers that are kept of its row
@@ -394,19 +409,18 @@ constexpr int kPairThreads = 1024;
 __global__ __launch_bounds__(kPairThreads) void pair_sums_kernel(PreferenceArgs a, const float* __restrict__ logp, float* __restrict__ slope,
                                                                  int T) {
   constexpr int half = kPairThreads / 2;
-  __shared__ double red[2][half];
+  __shared__ double red[2][half], sum[2];
   const int p = blockIdx.x, k = threadIdx.x / half, tid = threadIdx.x % half;
   const int2 r = sequence_rows(a.ends, 2 * p + k, a.L, T);
   double s = 0.0;
   for (int i = r.x + tid; i < r.y; i += half) s += (double)logp[i];
-  red[k][tid] = s;
-  __syncthreads();
-  for (int o = half / 2; o > 0; o >>= 1) {
-    if (tid < o) red[k][tid] += red[k][tid + o];
-    __syncthreads();
+  s = first_wave_sum<half / 64>(s, red[k], tid);
+  if (tid == 0) {
+    sum[k] = s;
+    a.seq_logp[2 * p + k] = (float)s;
   }
-  if (tid == 0) a.seq_logp[2 * p + k] = (float)red[k][0];
-  const double h = (red[0][0] - (double)a.ref_logp[2 * p]) - (red[1][0] - (double)a.ref_logp[2 * p + 1]);
+  __syncthreads();
+  const double h = (sum[0] - (double)a.ref_logp[2 * p]) - (sum[1] - (double)a.ref_logp[2 * p + 1]);
   const float z = (float)((double)a.beta * h);
   if (threadIdx.x == 0) a.margin[p] = z;
   if (!slope) return;
@@ -414,22 +428,15 @@ __global__ __launch_bounds__(kPairThreads) void pair_sums_kernel(PreferenceArgs 
   for (int i = r.x + tid; i < r.y; i += half) slope[i] = k ? -d : d;
 }
 
-// mean loss of the pairs, by one block
+// mean loss of the pairs, by one block of kRowThreads
 __device__ __forceinline__ void mean_pair_loss(const PreferenceArgs& a) {
-  __shared__ double red[256];
-  const int tid = threadIdx.x;
-  if (tid >= 256) return;
+  __shared__ double red[kRowThreads];
   double s = 0.0;
-  for (int p = tid; p < a.pairs; p += 256) s += (double)pair_loss(a.margin[p], a.smoothing);
-  red[tid] = s;
-  __syncthreads();
-  for (int o = 128; o > 0; o >>= 1) {
-    if (tid < o) red[tid] += red[tid + o];
-    __syncthreads();
-  }
-  if (tid == 0) *a.loss = (float)(red[0] / (double)a.pairs);
+  for (int p = threadIdx.x; p < a.pairs; p += kRowThreads) s += (double)pair_loss(a.margin[p], a.smoothing);
+  s = first_wave_sum<kRowThreads / 64>(s, red, threadIdx.x);
+  if (threadIdx.x == 0) *a.loss = (float)(s / (double)a.pairs);
 }
-__global__ __launch_bounds__(256) void pair_loss_kernel(PreferenceArgs a) { mean_pair_loss(a); }
+__global__ __launch_bounds__(kRowThreads) void pair_loss_kernel(PreferenceArgs a) { mean_pair_loss(a); }
 
 // Gradient from what the pass before left of each row: grad_chunks() chunks a thread, `parts` blocks a row, the last row first, because the pass
 // before has read it last.  One more block, behind all rows, for the mean loss.
@@ -499,11 +506,14 @@ __global__ __launch_bounds__(1024) void policy_stats_kernel(const float4* __rest
   }
   for (int k = 0; k < 3; ++k) red[k][tid] = s[k];
   __syncthreads();
-  for (int o = 512; o > 0; o >>= 1) {
-    if (tid < o) for (int k = 0; k < 3; ++k) red[k][tid] += red[k][tid + o];
-    __syncthreads();
-  }
-  if (tid < 3) stats[tid] = (float)red[tid][0];
+  const int k = tid >> 6;                               // a wave for each sum
+  if (k >= 3) return;
+  double v = 0.0;
+#pragma unroll
+  for (int w = 0; w < 16; ++w) v += red[k][64 * w + (tid & 63)];
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+  if ((tid & 63) == 0) stats[k] = (float)v;
 }
 
 // ---------------------------------------------------------------- launchers
@@ -567,7 +577,7 @@ static void preference_t(const void* logits, int64_t ldl, const int32_t* labels,
   if (!dlogits || rows <= 0) {
     rows_t<T, 0>(logits, ldl, labels, logp, nullptr, nullptr, nullptr, PolicyArgs(), rows, V, true, st);
     hipLaunchKernelGGL(pair_sums_kernel, dim3(a.pairs), dim3(kPairThreads), 0, st, a, logp, (float*)nullptr, rows);
-    hipLaunchKernelGGL(pair_loss_kernel, dim3(1), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(pair_loss_kernel, dim3(1), dim3(kRowThreads), 0, st, a);
     return;
   }
   float* slope = (float*)(stat + rows);
