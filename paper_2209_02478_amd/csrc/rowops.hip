@@ -818,10 +818,11 @@ __global__ __launch_bounds__(256) void dropout_kernel(TIO* __restrict__ dst, con
 // Bound by memory: 28 or 30 bytes an element in seven or eight streams, none of which fits a cache until it is
 // touched again, so all but the low-precision copy, which the next forward reads, go past the caches (non-temporal
 // loads and stores; either alone gains nothing).  kAdamBlocks blocks share a chunk of kAdamChunk elements of one
-// tensor, four elements a thread and no loop: stretches of 8 KB that start together.  110 M parameters in bf16, call
-// behind call: a block for a chunk, through the caches, 650 us (5.05 TB/s), so 616 (5.3); behind an iteration's
-// backward, which leaves some of the gradients in the last cache, 645 and 550-570.
-constexpr int kAdamThreads = 512, kAdamBlocks = kAdamChunk / (4 * kAdamThreads);
+// tensor, four elements a thread and no loop: stretches of 1 KB that start together.  109 M parameters in bf16, call behind
+// call: a block for a chunk, through the caches, 650 us (5.05 TB/s), stretches of 8 KB 616, with the master's store past the
+// caches too 595, stretches of 2 KB 564, of 1 KB 546 (6.0; 355 M parameters 2006, 1890 and 1785).  Behind an iteration's
+// backward, iterations of bert_base 7.72 (8 KB), 7.70 (2 KB) and 7.68 ms (1 KB), of gpt2_medium 25.49, 25.65 and 25.43.
+constexpr int kAdamThreads = 64, kAdamBlocks = kAdamChunk / (4 * kAdamThreads);
 __global__ __launch_bounds__(kAdamThreads) void adamw_kernel(const AdamTensor* __restrict__ tensors,
                                                              const AdamChunk* __restrict__ chunks, AdamHyper h) {
   typedef float f32x4 __attribute__((ext_vector_type(4)));
