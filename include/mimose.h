@@ -434,7 +434,8 @@ int mimose_op_softmax_xent(int32_t dtype, void* logits, int64_t ld, const int32_
  * A label outside [0, V) leaves its row out: the logits are not read (they may hold anything), logp is
  * 0, the gradient 0.  dlogits (optional, storage type, leading dimension ld): the gradient, zeros in
  * columns >= V; NULL: the loss alone; logits itself: in place; any other overlap is INVALID_ARG.
- * Logits of any alignment and ld (dlogits too; fastest where every row begins and ends on a 16-byte address).
+ * Logits of any alignment and any ld below 2^31 (dlogits too; fastest where every row begins and ends on a
+ * 16-byte address, slowest where the two lie differently to one).
  * workspace: device scratch of mimose_op_token_loss_workspace_bytes(T), 16-byte aligned, which a caller can
  * hand to all three; the preference loss needs it, the other two use none and take NULL as well.
  * mimose_last_error(NULL) says why a call was refused.
@@ -451,7 +452,7 @@ int mimose_op_token_logprob(int32_t dtype, const void* logits, int64_t ld, const
  *     margin[p]   = beta ((seq_logp[2p] - ref_logp[2p]) - (seq_logp[2p+1] - ref_logp[2p+1]))
  *     loss        = mean over p of (1 - smoothing) log(1 + exp(-margin)) + smoothing log(1 + exp(margin))
  * logp fp32[T], seq_logp fp32[2*pairs], margin fp32[pairs], loss fp32 scalar are written, ref_logp
- * fp32[2*pairs] (the reference model's seq_logp) is read; all on the device. */
+ * fp32[2*pairs] (the reference model's seq_logp) is read; all on the device.  At most 2^21 pairs. */
 int mimose_op_preference_loss(int32_t dtype, const void* logits, int64_t ld, const int32_t* labels,
                               const int32_t* ends, int32_t pairs, int32_t L, const float* ref_logp,
                               float beta, float smoothing, void* dlogits, float* logp,

@@ -162,6 +162,7 @@ struct PolicyArgs {
   float scale = 1.f, ratio_low = 0.f, ratio_high = 0.f, kl_weight = 0.f;
   float *rows = nullptr, *stats = nullptr;                         // [T, 4], [3]
 };
+constexpr int kMostPairs = 1 << 21;   // a block of 1024 threads each, and a grid's threads are counted in 32 bits
 // what is wrong with the settings of a loss, or null
 inline const char* bad_preference(float beta, float smoothing) {
   return !std::isfinite(beta) || !(smoothing >= 0.f && smoothing <= 1.f) ? "beta must be finite, smoothing in [0, 1]" : nullptr;

@@ -1440,6 +1440,7 @@ int mimose_train_step_preference(mimose_ctx* c, const int32_t* tokens, const int
   if (!cfg || !ref_logp) return fail(c, MIMOSE_ERR_INVALID_ARG, "cfg and ref_logp must be given");
   if (const char* why = mk::bad_preference(cfg->beta, cfg->smoothing)) return fail(c, MIMOSE_ERR_INVALID_ARG, why);
   if (B < 2 || B % 2) return fail(c, MIMOSE_ERR_INVALID_ARG, "a batch of pairs has an even number of samples");
+  if (B / 2 > mk::kMostPairs) return fail(c, MIMOSE_ERR_INVALID_ARG, "too many pairs");
   if (margin && !loss) return fail(c, MIMOSE_ERR_INVALID_ARG, "margins are there once the step has been waited for: loss must be given");
   Objective o;
   o.kind = Objective::PREFERENCE; o.ref = ref_logp; o.preference = *cfg; o.margin = margin;

@@ -29,7 +29,7 @@ const char* bad_logits(int dtype, const void* logits, int64_t ld, const int32_t*
   if (T < 0 || V < 1 || ld < V) return "T >= 0, V >= 1 and ld >= V required";
   if (T > 0 && (!logits || !labels)) return "logits and labels must be given";
   const uintptr_t es = mk::elt_size(dtype), a = (uintptr_t)logits, b = (uintptr_t)dlogits;
-  if (ld > INT64_MAX / 8 / (T > 0 ? T : 1)) return "ld too large";
+  if (ld > INT32_MAX) return "ld too large";
   if (a % es || b % es || (uintptr_t)labels % 4) return "a pointer is not aligned to its elements";
   const uintptr_t bytes = T > 0 ? ((uintptr_t)(T - 1) * ld + ld) * es : 0;
   if (b && a != b && a < b + bytes && b < a + bytes) return "dlogits overlaps the logits without being them";
@@ -201,7 +201,7 @@ int mimose_op_preference_loss(int32_t dtype, const void* logits, int64_t ld, con
                               float* margin, float* loss, int32_t T, int32_t V, void* workspace, uint64_t workspace_bytes, void* stream) {
   const char* const op = "mimose_op_preference_loss";
   if (const char* why = bad_logits(dtype, logits, ld, labels, dlogits, T, V)) return refuse(op, why);
-  if (pairs < 1 || pairs > (1 << 24)) return refuse(op, "1 to 2^24 pairs required");
+  if (pairs < 1 || pairs > mk::kMostPairs) return refuse(op, "1 to 2^21 pairs required");
   if (!ends && (L < 0 || (int64_t)2 * pairs * L != T)) return refuse(op, "without ends, T must be 2 * pairs * L");
   if (!ref_logp || !seq_logp || !margin || !loss || (T > 0 && !logp)) return refuse(op, "ref_logp, logp, seq_logp, margin and loss must be given");
   if (const char* why = mk::bad_preference(beta, smoothing)) return refuse(op, why);
