@@ -406,8 +406,54 @@ __device__ __forceinline__ float pair_slope(float z, const PreferenceArgs& a) {
   return -a.beta / (float)a.pairs * ((1.f - a.smoothing) / (1.f + expf(z)) - a.smoothing / (1.f + expf(-z)));
 }
 
-// One block for a pair, half of its threads for each sequence: the sums, in fp64 because the margin is the small difference
-// of four sums over a thousand rows; the margin; and d loss / d logp of each of the pair's rows.
+// Margin of pair p by one wave, in every lane, and the sums of its sequences where seq is given.  Sums are fp64 because the
+// margin is the small difference of four of them over up to a thousand rows.
+__device__ __forceinline__ float wave_margin(const PreferenceArgs& a, const float* logp, int p, int T, float* seq) {
+  const int lane = threadIdx.x & 63;
+  double h = 0.0;
+  for (int k = 0; k < 2; ++k) {
+    const int2 r = sequence_rows(a.ends, 2 * p + k, a.L, T);
+    double s = 0.0;
+    for (int i = r.x + lane; i < r.y; i += 4 * 64) {
+      float v[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) v[u] = i + 64 * u < r.y ? logp[i + 64 * u] : 0.f;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) s += (double)v[u];
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
+    if (seq && lane == 0) seq[2 * p + k] = (float)s;
+    s -= (double)a.ref_logp[2 * p + k];
+    h = k ? h - s : s;
+  }
+  return (float)((double)a.beta * h);
+}
+// the pairs' sums, margins and mean loss, by one block of kRowThreads, a wave for a pair
+__device__ __forceinline__ void few_pairs_loss(const PreferenceArgs& a, const float* logp, int T) {
+  constexpr int NW = kRowThreads / 64;
+  __shared__ double part[NW];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  double s = 0.0;
+  for (int p = wave; p < a.pairs; p += NW) {
+    const float z = wave_margin(a, logp, p, T, a.seq_logp);
+    if (lane == 0) a.margin[p] = z;
+    s += (double)pair_loss(z, a.smoothing);
+  }
+  if (lane == 0) part[wave] = s;
+  __syncthreads();
+  if (threadIdx.x) return;
+  s = 0.0;
+  for (int w = 0; w < NW; ++w) s += part[w];
+  *a.loss = (float)(s / (double)a.pairs);
+}
+__global__ __launch_bounds__(kRowThreads) void few_pairs_kernel(PreferenceArgs a, const float* __restrict__ logp, int T) {
+  few_pairs_loss(a, logp, T);
+}
+constexpr int kFewPairs = 8;                            // (their ends fit the lanes of a wave)
+
+// One block for a pair, half of its threads for each sequence: the sums (fp64, as above), the margin, and d loss / d logp of each
+// of the pair's rows.
 constexpr int kPairThreads = 1024;
 __global__ __launch_bounds__(kPairThreads) void pair_sums_kernel(PreferenceArgs a, const float* __restrict__ logp, float* __restrict__ slope,
                                                                  int T) {
@@ -443,27 +489,32 @@ __global__ __launch_bounds__(kRowThreads) void pair_loss_kernel(PreferenceArgs a
 
 // Gradient from what the pass before left of each row: grad_chunks() chunks a thread, `parts` blocks a row, the last row first,
 // because the pass before has read it last.  One more block, behind all rows, for the mean loss.  Bound by memory: 16384 rows of
-// 50257 in bf16 530-550 us, 6.1 TB/s.
+// 50257 in bf16 530-550 us, 6.1 TB/s.  SUMS: no kernel has summed the pairs; every block makes its pair's margin itself while its
+// logits are on their way, and the block behind all rows writes the pairs' numbers.
 constexpr int grad_chunks(bool past) { return past ? 1 : 2; }
-template <typename T, bool PAST>
+template <typename T, bool PAST, bool SUMS>
 __global__ __launch_bounds__(kRowThreads) void pair_grad_kernel(const T* logits, int64_t ldl, const int32_t* __restrict__ labels,
                                                                 const float2* __restrict__ stat, const float* __restrict__ slope,
-                                                                T* dlogits, PreferenceArgs a, int rows, int V, int parts) {
+                                                                const float* __restrict__ logp, T* dlogits, PreferenceArgs a, int rows,
+                                                                int V, int parts) {
   constexpr int N = Packed<T>::N, CH = grad_chunks(PAST);
   const int row = rows - 1 - (int)(blockIdx.x / (unsigned)parts);
-  if (row < 0) { mean_pair_loss(a); return; }
+  if (row < 0) {
+    if (SUMS) few_pairs_loss(a, logp, rows); else mean_pair_loss(a);
+    return;
+  }
   const int part = (int)(blockIdx.x % (unsigned)parts);
   const T* x = logits + (int64_t)row * ldl;
   T* g = dlogits + (int64_t)row * ldl;
   const int shift = shift_of(x), label = labels[row];
   const bool aligned = shift_of(g) == shift;
-  const float d = slope[row];
+  float d = SUMS ? 1.f : slope[row];
   const int64_t first = (int64_t)part * (kRowThreads * CH) * N - shift;     // column
-  if (!is_scored(label, V) || d == 0.f) {
+  auto zeros = [&] {
     const int64_t to = min(ldl, first + (int64_t)kRowThreads * CH * N);
     if (first < to) zero_columns(g, max(first, (int64_t)0), to, threadIdx.x, kRowThreads);
-    return;
-  }
+  };
+  if (!is_scored(label, V) || d == 0.f) { zeros(); return; }
   u32x4 raw[CH];
 #pragma unroll
   for (int i = 0; i < CH; ++i) {
@@ -477,6 +528,22 @@ __global__ __launch_bounds__(kRowThreads) void pair_grad_kernel(const T* logits,
     }
   }
   const float2 ms = stat[row];
+  if (SUMS) {
+    __shared__ float shared_d;
+    if (threadIdx.x < 64) {
+      // the row's sequence: how many ends are not behind it
+      const int s = a.ends ? __popcll(__ballot((int)threadIdx.x < 2 * a.pairs && a.ends[threadIdx.x] <= row)) : row / a.L;
+      d = 0.f;                                          // (a row behind the last sequence)
+      if (s < 2 * a.pairs) {
+        d = pair_slope(wave_margin(a, logp, s >> 1, rows, nullptr), a);
+        if (s & 1) d = -d;
+      }
+      if (threadIdx.x == 0) shared_d = d;
+    }
+    __syncthreads();
+    d = shared_d;
+    if (d == 0.f) { zeros(); return; }
+  }
   const float k = -d * ms.y;
 #pragma unroll
   for (int i = 0; i < CH; ++i) {
@@ -580,28 +647,42 @@ static void preference_t(const void* logits, int64_t ldl, const int32_t* labels,
   float2* stat = (float2*)workspace;
   if (!dlogits || rows <= 0) {
     rows_t<T, 0>(logits, ldl, labels, logp, nullptr, nullptr, nullptr, PolicyArgs(), rows, V, true, st);
+    if (a.pairs <= kFewPairs) {
+      hipLaunchKernelGGL(few_pairs_kernel, dim3(1), dim3(kRowThreads), 0, st, a, logp, rows);
+      return;
+    }
     hipLaunchKernelGGL(pair_sums_kernel, dim3(a.pairs), dim3(kPairThreads), 0, st, a, logp, (float*)nullptr, rows);
     hipLaunchKernelGGL(pair_loss_kernel, dim3(1), dim3(kRowThreads), 0, st, a);
     return;
   }
-  float* slope = (float*)(stat + rows);
   // The gradient reads the rows a second time.  Where they are few, what the first pass has read is still in the last cache
   // (256 MB), where many are it is not, and loads past the caches are faster.  Labels say what is read of them, and they are on
   // the device: the bound is of all rows, 640 MB, of which some hundred are prompts.  6352 rows of 50257, 0.4 of them prompts
   // (639 MB): 223 us through the caches, 249 past them; 8192 of 30522, no prompts (500 MB): 255 and 249; 16384 of 50257: 849 and
   // 778.  Chunks a thread: 2 and 1, 788 and 749 in the last of these, 143 and 151 for 4200 rows (422 MB).
   const bool few = rows * ldl * (int64_t)sizeof(T) <= (int64_t)640 << 20;
-  const int64_t per_block = (int64_t)kRowThreads * grad_chunks(!few) * N, parts = (ldl + (N - 1) + per_block - 1) / per_block;
+  const int64_t before = ldl % N == 0 && ((uintptr_t)logits & 15) == 0 ? 0 : N - 1;       // of a row, in its first chunk
+  const int64_t per_block = (int64_t)kRowThreads * grad_chunks(!few) * N, parts = (before + ldl + per_block - 1) / per_block;
   const int most = (int)std::max<int64_t>(1, ((int64_t)kRowsPerLaunch * 8) / parts);
+  // A gradient of few blocks makes the pairs' sums itself, a launch less (2.5 us of the host's time): 4 x 33 rows of 1000 in fp32
+  // 16.2 -> 12.8 us, 240 of 50257 17.0 -> 15.3 (3100 blocks), 2400 of 1000 15.8 -> 12.5; but 3600 of 1000 13.9 -> 15.9, 500 of
+  // 50257 27.9 -> 29.7 (6500 blocks).
+  const bool sums = few && a.pairs <= kFewPairs && rows * parts <= 3072;
+  float* slope = sums ? nullptr : (float*)(stat + rows);
   rows_t<T, 0>(logits, ldl, labels, logp, stat, slope, nullptr, PolicyArgs(), rows, V, !few, st);
+  if (sums) {
+    hipLaunchKernelGGL((pair_grad_kernel<T, false, true>), dim3((unsigned)(rows * parts + 1)), dim3(kRowThreads), 0, st, (const T*)logits, ldl,
+                       labels, stat, slope, logp, (T*)dlogits, a, rows, V, (int)parts);
+    return;
+  }
   hipLaunchKernelGGL(pair_sums_kernel, dim3(a.pairs), dim3(kPairThreads), 0, st, a, logp, slope, rows);
   for (int end = rows; end > 0; end -= std::min(end, most)) {
     const int n = std::min(end, most), r = end - n, extra = r == 0;     // (with the mean loss behind everything)
     const T* x = (const T*)logits + r * ldl;
     T* g = (T*)dlogits + r * ldl;
 #define G_(PAST)                                                                                                                     \
-  hipLaunchKernelGGL((pair_grad_kernel<T, PAST>), dim3((unsigned)(n * parts + extra)), dim3(kRowThreads), 0, st, x, ldl, labels + r, stat + r, \
-                     slope + r, g, a, n, V, (int)parts)
+  hipLaunchKernelGGL((pair_grad_kernel<T, PAST, false>), dim3((unsigned)(n * parts + extra)), dim3(kRowThreads), 0, st, x, ldl, labels + r, \
+                     stat + r, slope + r, logp, g, a, n, V, (int)parts)
     if (few) G_(false); else G_(true);
 #undef G_
   }

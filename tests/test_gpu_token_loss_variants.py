@@ -99,3 +99,32 @@ def test_infinities_and_nan_stay_in_their_rows():
         lg[5, V - 1] = 0.0
         run_preference(1, lg, ld, labels, None, 2, 2, zeros[:4], 0.1, 0.0, d, T, V)
         assert np.array_equal(np.isnan(host(d)[:, :V]).any(1), np.arange(T) < 4) and not d[:, V:].any()
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("lengths", [[3, 0], [0, 0, 1, 5], [200, 1, 0, 300] * 4, [1] * 18, [400, 700], [70] * 16 + [2, 3], [64, 65] * 8])
+@pytest.mark.parametrize("grad", [False, True])
+def test_preference_sums(dtype, lengths, grad):
+    """Up to eight pairs and more, few rows and many, sequences without rows, rows behind the last end: the pairs' numbers come out of
+    the gradient's launch, or out of one of their own, and are the oracle's either way."""
+    P, V, ld = len(lengths) // 2, 700, 704
+    ends = np.cumsum(lengths)
+    T = int(ends[-1]) + 3
+    rng, x, labels = inputs(T, T, V, dtype)
+    if sum(lengths) == 0:
+        labels[:] = -1
+    logp = tl.token_logprob(x, labels)[0]
+    sums = np.array([logp[a:b].sum() for a, b in zip(np.concatenate([[0], ends[:-1]]), ends)])
+    ref = (sums + rng.standard_normal(2 * P)).astype(np.float32)
+    want = tl.preference_loss(x, labels, ends, ref, 0.2, 0.1)
+    lg = logits_of(dtype, x, ld)
+    d = torch.full_like(lg, 9.0) if grad else None
+    out = run_preference(dtype, lg, ld, labels, ends, P, 0, ref, 0.2, 0.1, d, T, V)
+    check_logp(host(out["logp"]), want["logp"], V)
+    seq_tol = max(lengths) * lse_tol(V) + 8 * U * np.abs(want["logp"]).sum()
+    assert np.abs(host(out["seq"]) - want["seq_logp"]).max() <= seq_tol
+    z_tol = 0.4 * seq_tol + U * np.abs(want["margin"]).max()
+    assert np.abs(host(out["margin"]) - want["margin"]).max() <= z_tol
+    assert abs(float(out["loss"]) - want["loss"]) <= z_tol + 8 * U * want["loss"]
+    if grad:
+        check_gradient(host(d), want, labels, V, dtype, z_tol + 16 * U)

@@ -12,8 +12,8 @@ SETUP = """
         return launched(lambda: mi.mimose_op_token_logprob(dtype, x, ld, at, at, 64, V))
     def policy(dtype, V, ld, x=at, g=far, T=64):
         return launched(lambda: mi.mimose_op_policy_loss(dtype, x, ld, at, at, None, at, None, 1.0, .2, .2, 0., g, at, at, T, V))
-    def preference(dtype, V, ld, T, g=far):
-        return launched(lambda: mi.mimose_op_preference_loss(dtype, at, ld, at, at, 2, 0, at, .1, 0., g, at, at, at, at, T, V, at, 1 << 40))
+    def preference(dtype, V, ld, T, g=far, pairs=2):
+        return launched(lambda: mi.mimose_op_preference_loss(dtype, at, ld, at, at, pairs, 0, at, .1, 0., g, at, at, at, at, T, V, at, 1 << 40))
 """
 
 
@@ -41,16 +41,23 @@ def test_rows(runtime, dtype, letter):  # noqa: F811
 
 
 def test_preference(runtime):  # noqa: F811
-    """Rows of up to 640 MB through the caches, more past them; three launches, or with the loss alone no gradient's."""
+    """Rows of up to 640 MB through the caches, more past them; three launches, two where the gradient makes the pairs' sums or a
+    block is enough for the loss alone."""
     run(runtime, SETUP + """
     for T, past in ((6670, 0), (6671, 1)):
         names = preference(1, 50257, 50304, T)
         assert len(names) == 3 and "Li8ELi13ELi0ELb%dELb1E" % past in names[0] and "pair_sums" in names[1], names
-        assert "pair_grad_kernelItLb%dE" % past in names[2], names
+        assert "pair_grad_kernelItLb%dELb0E" % past in names[2], names
+    for V, ld, T, pairs, sums in ((4096, 4096, 3071, 8, 1), (4096, 4096, 3072, 8, 1), (4096, 4096, 3073, 8, 0), (4096, 4096, 100, 9, 0),
+                                  (4097, 4104, 1536, 8, 1), (4097, 4104, 1537, 8, 0)):
+        names = preference(1, V, ld, T, far, pairs)
+        assert len(names) == (2 if sums else 3) and "pair_grad_kernelItLb0ELb%dE" % sums in names[-1], (V, T, pairs, names)
     names = preference(1, 50257, 50304, 100, None)
-    assert len(names) == 3 and "pair_loss" in names[2], names
+    assert len(names) == 2 and "few_pairs_kernel" in names[1], names
+    names = preference(1, 50257, 50304, 100, None, 9)
+    assert len(names) == 3 and "pair_sums" in names[1] and "pair_loss" in names[2], names
     names = preference(1, 50257, 50304, 0)
-    assert len(names) == 2 and "pair_sums" in names[0] and "pair_loss" in names[1], names
+    assert len(names) == 1 and "few_pairs_kernel" in names[0], names
     """)
 
 
