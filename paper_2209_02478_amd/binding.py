@@ -556,7 +556,7 @@ def mimose_op_embed_bwd(dtype, d, ids, order, seg, n_seg, dtok, dpos, B, L, H, m
 class AdamWTable:
     """The device table of a list of tensors, for mimose_op_adamw_step; keeps the tensors alive.
 
-    tensors: dicts of device tensors master (fp32), grad (fp32), m, v (fp32, or one byte an element with state_bits 8), lowp
+    tensors: dicts of device tensors master (fp32), grad (fp32), m, v (fp32; uint8 or float8_e4m3fn with state_bits 8), lowp
     (bf16 or None), m_scale and v_scale (fp32, one entry for each 256 elements; state_bits 8), and decay (0 or 1)."""
 
     BLOCK = 256   # elements that share a scale
@@ -567,16 +567,16 @@ class AdamWTable:
         entries = (mimose_adamw_tensor * len(self.tensors))()
         for e, t in zip(entries, self.tensors):
             n = t["master"].numel()
-            sizes = {"master": (n, 4), "grad": (n, 4), "m": (n, state_bits // 8), "v": (n, state_bits // 8), "lowp": (n, 2)}
+            state = (n, (torch.float32,) if state_bits == 32 else (torch.uint8, torch.float8_e4m3fn))
+            wanted = {"master": (n, (torch.float32,)), "grad": (n, (torch.float32,)), "m": state, "v": state, "lowp": (n, (torch.bfloat16,))}
             if state_bits == 8:
-                blocks = -(-n // self.BLOCK)
-                sizes.update(m_scale=(blocks, 4), v_scale=(blocks, 4))
-            for name, (count, size) in sizes.items():
+                wanted["m_scale"] = wanted["v_scale"] = (-(-n // self.BLOCK), (torch.float32,))
+            for name, (count, dtypes) in wanted.items():
                 x = t.get(name)
                 if x is None and name == "lowp":
                     continue
-                if x is None or x.numel() != count or x.element_size() != size or not x.is_contiguous() or not x.is_cuda:
-                    raise ValueError(f"{name}: a contiguous device tensor of {count} elements of {size} bytes is required")
+                if x is None or x.numel() != count or x.dtype not in dtypes or not x.is_contiguous() or not x.is_cuda:
+                    raise ValueError(f"{name}: a contiguous device tensor of {count} elements of {dtypes[0]} is required")
                 setattr(e, name, x.data_ptr() or None)
             e.n, e.decay = n, int(bool(t.get("decay", 0)))
         nbytes = mimose_op_adamw_table_bytes(entries, state_bits)

@@ -191,3 +191,19 @@ def test_calls_in_a_graph_and_repeated_are_the_same():
         for x, y in zip(a, b):
             for k in ("master", "lowp", "m", "v", "m_scale", "v_scale"):
                 assert torch.equal(x[k], y[k]), k
+
+
+def test_tensors_that_are_not_what_a_table_holds():
+    good = device(tensors([300], 1, True), True)[0]
+    for name, bad in (("master", good["master"].double()), ("grad", good["grad"].to(torch.int32)), ("m", good["m"][:-1]), ("v", good["v"].float()),
+                      ("lowp", good["lowp"].half()), ("m_scale", good["m_scale"][:1]), ("v_scale", None), ("grad", good["grad"].cpu()),
+                      ("master", torch.zeros(600, device=DEV)[::2])):
+        with pytest.raises(ValueError, match=name):
+            mi.AdamWTable([dict(good, **{name: bad})], 8)
+    with pytest.raises(mi.MimoseError):
+        mi.AdamWTable([], 8)
+    with pytest.raises(mi.MimoseError, match="16-byte"):
+        mi.AdamWTable([dict(good, grad=torch.zeros(301, device=DEV)[1:])], 8)
+    step = dict(good, m=good["m"].view(torch.float8_e4m3fn), v=good["v"].view(torch.float8_e4m3fn))
+    mi.mimose_op_adamw_step(mi.AdamWTable([step], 8), 1)
+    sync()
