@@ -163,7 +163,9 @@ def load_library():
 
 def _ptr(x) -> Optional[int]:
     """Address of a torch tensor (device or host), numpy array, int, or None."""
-    try:                               # (tensors first: a call has up to a dozen, and small ones are bound by this)
+    if x is None or type(x) is int:    # (small calls are bound by this: an AttributeError costs more than a check)
+        return x
+    try:
         return x.data_ptr()
     except AttributeError:
         return x.ctypes.data if isinstance(x, np.ndarray) else x
