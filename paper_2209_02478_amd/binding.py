@@ -559,7 +559,8 @@ class AdamWTable:
     """The device table of a list of tensors, for mimose_op_adamw_step; keeps the tensors alive.
 
     tensors: dicts of device tensors master (fp32), grad (fp32), m, v (fp32; uint8 or float8_e4m3fn with state_bits 8), lowp
-    (bf16 or None), m_scale and v_scale (fp32, one entry for each 256 elements; state_bits 8), and decay (0 or 1)."""
+    (bf16 or None), m_scale and v_scale (fp32, one entry for each 256 elements; state_bits 8), and decay (0 or 1).  stream (an address; None: torch's current one) is
+    the one that steps run on; a step on another has to have ended before the table is let go."""
 
     BLOCK = 256   # elements that share a scale
 
@@ -585,8 +586,11 @@ class AdamWTable:
         device = self.tensors[0]["master"].device
         if stream is None:
             stream = torch.cuda.current_stream(device).cuda_stream
-        self.memory = torch.empty(nbytes, dtype=torch.uint8, device=device)
-        self.table = mimose_op_adamw_table(entries, state_bits, self.memory, nbytes, stream)
+        # memory of that stream's own: other streams' may still be in use by what was queued there
+        owner = torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)
+        with torch.cuda.stream(owner):
+            self.memory = torch.empty(nbytes, dtype=torch.uint8, device=device)
+            self.table = mimose_op_adamw_table(entries, state_bits, self.memory, nbytes, stream)
 
 
 class Mimose:
