@@ -558,9 +558,10 @@ def mimose_op_embed_bwd(dtype, d, ids, order, seg, n_seg, dtok, dpos, B, L, H, m
 class AdamWTable:
     """The device table of a list of tensors, for mimose_op_adamw_step; keeps the tensors alive.
 
-    tensors: dicts of device tensors master (fp32), grad (fp32), m, v (fp32; uint8 or float8_e4m3fn with state_bits 8), lowp
-    (bf16 or None), m_scale and v_scale (fp32, one entry for each 256 elements; state_bits 8), and decay (0 or 1).  stream (an address; None: torch's current one) is
-    the one that steps run on; a step on another has to have ended before the table is let go."""
+    tensors: dicts of tensors of one device, master (fp32), grad (fp32), m, v (fp32; uint8 or float8_e4m3fn with state_bits 8),
+    lowp (bf16 or None), m_scale and v_scale (fp32, one entry for each 256 elements; state_bits 8), and decay (0 or 1).
+    stream (an address; None: torch's current one) is the one that steps run on; a step on another has to have ended before
+    the table is let go."""
 
     BLOCK = 256   # elements that share a scale
 
@@ -568,6 +569,7 @@ class AdamWTable:
         import torch
         self.tensors = [dict(t) for t in tensors]
         entries = (mimose_adamw_tensor * len(self.tensors))()
+        device = self.tensors[0]["master"].device if self.tensors else None
         for e, t in zip(entries, self.tensors):
             n = t["master"].numel()
             state = (n, (torch.float32,) if state_bits == 32 else (torch.uint8, torch.float8_e4m3fn))
@@ -578,12 +580,11 @@ class AdamWTable:
                 x = t.get(name)
                 if x is None and name == "lowp":
                     continue
-                if x is None or x.numel() != count or x.dtype not in dtypes or not x.is_contiguous() or not x.is_cuda:
-                    raise ValueError(f"{name}: a contiguous device tensor of {count} elements of {dtypes[0]} is required")
+                if x is None or x.numel() != count or x.dtype not in dtypes or not x.is_contiguous() or not x.is_cuda or x.device != device:
+                    raise ValueError(f"{name}: a contiguous tensor of {count} elements of {dtypes[0]} on the list's one device is required")
                 setattr(e, name, x.data_ptr() or None)
             e.n, e.decay = n, int(bool(t.get("decay", 0)))
         nbytes = mimose_op_adamw_table_bytes(entries, state_bits)
-        device = self.tensors[0]["master"].device
         if stream is None:
             stream = torch.cuda.current_stream(device).cuda_stream
         # memory of that stream's own: other streams' may still be in use by what was queued there

@@ -67,3 +67,18 @@ def test_memory_belongs_to_the_stream_that_fills_it(calls, stream, used):
     mi.AdamWTable([entry()], 8, stream=stream)
     assert calls == [("memory", used), ("copy", used)]
     assert torch.cuda.current_stream().cuda_stream == 7
+
+
+@pytest.mark.parametrize("name, tensor", [("grad", Tensor(300, device="cuda:1")), ("m", Tensor(300, torch.uint8, "cuda:1")),
+                                          ("v_scale", Tensor(2, device="cuda:1")), ("lowp", Tensor(300, torch.bfloat16, "cuda:1"))])
+def test_tensors_of_several_devices(calls, name, tensor):
+    with pytest.raises(ValueError, match=name):
+        mi.AdamWTable([entry(), entry(**{name: tensor})], 8)
+    assert not calls
+
+
+def test_lists_of_several_devices(calls):
+    there = {k: Tensor(t.n, t.dtype, "cuda:1") for k, t in entry().items()}
+    with pytest.raises(ValueError, match="master"):
+        mi.AdamWTable([entry(), there], 8)
+    mi.AdamWTable([there], 8)
