@@ -463,7 +463,7 @@ int mimose_op_preference_loss(int32_t dtype, const void* logits, int64_t ld, con
  *     gain = min(r A, clip(r, 1 - clip_low, 1 + clip_high) A),   kl = exp(d) - d - 1
  *     loss = sum of w (kl_weight kl - gain)
  * A token whose gain the clip holds back passes no gradient through r (one on the bound does).  A row
- * with w = 0 is left out of the loss whatever its other numbers are.  ref_logp may be NULL when
+ * with w = 0 is left out of the loss whatever its other numbers and its logits are, its gradient is zeros.  ref_logp may be NULL when
  * kl_weight is 0.  old_logp, ref_logp, advantage, weight: fp32[T]; rows fp32 [T,4] (16-byte aligned)
  * receives logp, w (kl_weight kl - gain), w kl, and w where the clip held the gain back; stats fp32[3]
  * the sums of the last three: loss, KL, clipped share. */

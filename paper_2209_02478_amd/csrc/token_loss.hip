@@ -253,6 +253,7 @@ void token_rows_held_kernel(const T* logits, int64_t ldl, const int32_t* __restr
   const float d = policy_token(pa, row, lp, &kept), k = -d / s;
   if (tid == 0) ((float4*)pa.rows)[row] = kept;
   if (!g) return;
+  if (d == 0.f) { zero_columns(g, 0, ldl, tid, TPR); return; }   // left out, whatever its logits are, or held back by the clip
   const int at = label + shift;                         // the label's element, counted from chunk 0
   float v[N];
   if (EVEN) {
@@ -369,6 +370,7 @@ __global__ __launch_bounds__(kLongThreads) void token_rows_long_kernel(const T* 
   const float d = policy_token(pa, row, lp, &kept), k = -d / s;
   if (tid == 0) ((float4*)pa.rows)[row] = kept;
   if (!g) return;
+  if (d == 0.f) { zero_columns(g, 0, ldl, tid, kLongThreads); return; }
   const bool aligned = shift_of(g) == shift;
   for (int64_t col = first; col < V; col += kLongAhead * step) {
     load(col);
