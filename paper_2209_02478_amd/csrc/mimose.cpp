@@ -1189,6 +1189,14 @@ int fail_oom(mimose_ctx* c, const OomError& e) {
   return fail(c, MIMOSE_ERR_OOM_BUDGET, buf);
 }
 
+// Whether a padded batch runs whole, with nothing left out.
+// A cost-aware planner keeps a layer's forward time at x = B * L (Section 4.1), so its collecting steps
+// run the batch whole: the time of the rows that are left says nothing about that size (2 x 768-wide
+// layers, 32 x 256 with a quarter of the rows real: 0.14 ms against the whole batch's 0.25).  In bf16
+// the bits are those of the steps that leave padding out; fp32 sums are not, so there no step of such
+// a context leaves any out, and no score, whose log-probabilities are compared with a step's.
+bool runs_whole(const mimose_model_cfg& f, bool collect) { return f.cost_aware && (collect || f.dtype == mk::F32); }
+
 int do_step(mimose_ctx* c, const int32_t* tokens, const int32_t* labels, const int32_t* lengths, int32_t B, int32_t L,
             bool dry, float* loss, uint64_t* peak, uint64_t* plan_id, const Objective& objective = Objective()) {
   const auto& f = c->cfg;
@@ -1232,14 +1240,9 @@ int do_step(mimose_ctx* c, const int32_t* tokens, const int32_t* labels, const i
   // ---- run
   c->dry = dry;
   Step s(c, objective, B, L, plan, collect);
-  // A cost-aware planner keeps a layer's forward time at x = B * L (Section 4.1), so its collecting steps
-  // run the batch whole: the time of the rows that are left says nothing about that size (2 x 768-wide
-  // layers, 32 x 256 with a quarter of the rows real: 0.14 ms against the whole batch's 0.25).  In bf16
-  // the bits are those of the steps that leave padding out; fp32 sums are not, so there no step of such
-  // a context leaves any out.
   float lv = 0.f;
   try {
-    if (!dry && lengths) s.set_lengths(lengths, f.cost_aware && (collect || f.dtype == mk::F32));
+    if (!dry && lengths) s.set_lengths(lengths, runs_whole(f, collect));
     s.run(tokens, labels, &lv, dry || loss != nullptr);
   } catch (const OomError& e) {
     abandon(c, dry);
@@ -1476,7 +1479,7 @@ int mimose_score(mimose_ctx* c, const int32_t* tokens, const int32_t* labels, co
   int rc = MIMOSE_OK;
   try {
     Step s(c, o, B, L, ~(uint64_t)0, false);
-    if (lengths) s.set_lengths(lengths, false);
+    if (lengths) s.set_lengths(lengths, runs_whole(c->cfg, false));
     s.run(tokens, labels, nullptr, true);
   } catch (const OomError& e) {
     abandon(c, false);

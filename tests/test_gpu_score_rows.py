@@ -12,16 +12,23 @@ pytestmark = pytest.mark.gpu
 LENGTHS = [33, 20, 7, 33, 1, 30, 2, 9]
 
 
-@pytest.mark.parametrize("name", ["fp32_preln_causal", "fp32_postln", "bf16_preln_causal", "bf16_postln"])
+SHAPES = {k: SMALL[k] for k in ("fp32_preln_causal", "fp32_postln", "bf16_preln_causal", "bf16_postln")}
+# products of several tiles: their sums depend on how many rows there are
+SHAPES["fp32_preln_causal_256"] = synthdata.ModelShape(2, 256, 4, 1024, 1000, 64, "fp32", causal=1, pre_ln=1, gelu_tanh=1, head=0)
+SHAPES["fp32_postln_256"] = synthdata.ModelShape(2, 256, 4, 1024, 1000, 64, "fp32")
+SHAPES["bf16_postln_256"] = synthdata.ModelShape(2, 256, 4, 1024, 1000, 64, "bf16")
+
+
+@pytest.mark.parametrize("name", list(SHAPES))
 @pytest.mark.parametrize("cost_aware", [0, 1])
 @pytest.mark.parametrize("collecting", [False, True])
 def test_ratios_against_a_score(name, cost_aware, collecting):
-    shape = SMALL[name]
+    shape = SHAPES[name]
     m = mi.Mimose(synthdata.shape_dict(shape), 0, arena_bytes=256 * MiB, cost_aware=cost_aware)
     m.load_params(synthdata.make_params(shape, 11, perturb=True))
     if not collecting:
         m.force_plan(0)
-    for seed, lengths in ((12, LENGTHS), (13, [max(LENGTHS)] * 3), (14, [40, 1, 1, 1, 1, 1])):
+    for seed, lengths in ((12, LENGTHS), (13, [max(LENGTHS)] * 3), (14, [40, 1, 1, 1, 1, 1]), (15, [48, 30, 9, 2, 14, 5, 20, 11] * 2)):
         tokens, labels, lens = synthdata.make_padded_batch(shape, lengths, seed)
         logp = m.score(tokens, labels, lens)
         for sign in (1.0, -1.0):
