@@ -416,10 +416,10 @@ __device__ __forceinline__ float wave_margin(const PreferenceArgs& a, const floa
   for (int k = 0; k < 2; ++k) {
     const int2 r = sequence_rows(a.ends, 2 * p + k, a.L, T);
     double s = 0.0;
-    for (int i = r.x + lane; i < r.y; i += 4 * 64) {
+    for (unsigned i = r.x + lane; i < (unsigned)r.y; i += 4 * 64) {   // (unsigned: a step behind 2^31 - 1 rows is no int)
       float v[4];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) v[u] = i + 64 * u < r.y ? logp[i + 64 * u] : 0.f;
+      for (int u = 0; u < 4; ++u) v[u] = i + 64 * u < (unsigned)r.y ? logp[i + 64 * u] : 0.f;
 #pragma unroll
       for (int u = 0; u < 4; ++u) s += (double)v[u];
     }
@@ -464,7 +464,7 @@ __global__ __launch_bounds__(kPairThreads) void pair_sums_kernel(PreferenceArgs 
   const int p = blockIdx.x, k = threadIdx.x / half, tid = threadIdx.x % half;
   const int2 r = sequence_rows(a.ends, 2 * p + k, a.L, T);
   double s = 0.0;
-  for (int i = r.x + tid; i < r.y; i += half) s += (double)logp[i];
+  for (unsigned i = r.x + tid; i < (unsigned)r.y; i += half) s += (double)logp[i];
   s = first_wave_sum<half / 64>(s, red[k], tid);
   if (tid == 0) {
     sum[k] = s;
@@ -476,7 +476,7 @@ __global__ __launch_bounds__(kPairThreads) void pair_sums_kernel(PreferenceArgs 
   if (threadIdx.x == 0) a.margin[p] = z;
   if (!slope) return;
   const float d = pair_slope(z, a);
-  for (int i = r.x + tid; i < r.y; i += half) slope[i] = k ? -d : d;
+  for (unsigned i = r.x + tid; i < (unsigned)r.y; i += half) slope[i] = k ? -d : d;
 }
 
 // mean loss of the pairs, by one block of kRowThreads
@@ -570,10 +570,10 @@ __global__ __launch_bounds__(1024) void policy_stats_kernel(const float4* __rest
   __shared__ double red[3][1024];
   const int tid = threadIdx.x;
   double s[3] = {0.0, 0.0, 0.0};
-  for (int i = tid; i < T; i += 8 * 1024) {
+  for (unsigned i = tid; i < (unsigned)T; i += 8 * 1024) {
     float4 r[8];                                        // (eight loads on their way at a time)
 #pragma unroll
-    for (int u = 0; u < 8; ++u) r[u] = i + 1024 * u < T ? rows[i + 1024 * u] : make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int u = 0; u < 8; ++u) r[u] = i + 1024 * u < (unsigned)T ? rows[i + 1024 * u] : make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
     for (int u = 0; u < 8; ++u) { s[0] += (double)r[u].y; s[1] += (double)r[u].z; s[2] += (double)r[u].w; }
   }
@@ -614,11 +614,11 @@ static void rows_t(const void* logits, int64_t ldl, const int32_t* labels, float
   const bool even = ldl % N == 0 && (((uintptr_t)logits | (uintptr_t)dlogits) & 15) == 0;
   const int64_t chunks = ((even ? 0 : N - 1) + (int64_t)V + N - 1) / N;
   const bool held = chunks <= kMostChunks;
-  for (int r = 0; r < rows; r += kRowsPerLaunch) {
-    const int n = std::min(rows - r, kRowsPerLaunch);
+  for (int64_t r = 0; r < rows; r += kRowsPerLaunch) {
+    const int n = (int)std::min<int64_t>(rows - r, kRowsPerLaunch);
     PolicyArgs a = pa;
     if (MODE == 1) {
-      a.old_logp += r; a.advantage += r; a.rows += 4 * (int64_t)r;
+      a.old_logp += r; a.advantage += r; a.rows += 4 * r;
       if (a.ref_logp) a.ref_logp += r;
       if (a.weight) a.weight += r;
     }
