@@ -165,8 +165,8 @@ int mimose_train_step_padded(mimose_ctx* ctx, const int32_t* tokens_host, const 
  * The same iteration with another loss in place of the cross-entropy, for fine-tuning after the first
  * training: plan, memory, recomputation, dropout, queueing and errors are those of mimose_train_step
  * (mimose_train_step_padded where lengths is given; NULL: every sample has L tokens).  What the loss
- * needs beside the logits comes out of the same arena, as part of the head's transient.  Labels say
- * which positions are scored (-1: none, as for the tokens of a prompt).
+ * needs beside the logits lies in memory that every step takes, so plans, peaks and dry steps hold
+ * whatever the loss.  Labels say which positions are scored (-1: none, as for the tokens of a prompt).
  *
  * mimose_train_step_preference: samples 2p and 2p+1 are the preferred and the other answer of pair p
  * (B even); the loss of mimose_op_preference_loss.

@@ -872,34 +872,35 @@ void Step::layer_backward(int l, LayerActs& A) {
   }
 }
 
-// The loss and its gradient in place of the logits; log-probabilities alone where the step scores.  Memory that only an
-// objective needs is taken here, as part of the head's transient.
+// The loss and its gradient in place of the logits; log-probabilities alone where the step scores.
+// What only an objective needs lies in gA_, which holds nothing between the end of the step before and this head's backward
+// (the copy of the margins out of it is queued ahead of that): a step takes the same memory whatever it minimises, so plans,
+// samples and dry steps hold for every loss.  It fits: 32 bytes a row at most for the policy loss (four arrays in, four numbers
+// a row out), 12 a row, 10 a sample and up to 60 for alignment for the preference loss of two samples or more; gA_ has at least
+// 64 a row (32 columns of two bytes).
 void Step::objective(void* logits, int64_t ldv, float* per_row, float* loss_dev) {
+  if (dry_) return;
   const int V = f_.vocab;
-  auto floats = [&](int64_t n) { return (float*)c_->arena.alloc((uint64_t)n * 4); };
+  char* at = (char*)gA_;
+  auto floats = [&](int64_t n) { float* p = (float*)at; at += (n * 4 + 15) / 16 * 16; return p; };
   if (obj_.kind == Objective::CROSS_ENTROPY) {
-    if (!dry_) mk::softmax_xent(dt_, logits, ldv, labels_, per_row, loss_dev, T_, V, n_valid_, st_);
+    mk::softmax_xent(dt_, logits, ldv, labels_, per_row, loss_dev, T_, V, n_valid_, st_);
   } else if (obj_.kind == Objective::SCORE) {
-    if (dry_) return;
     mk::token_logprob(dt_, logits, ldv, labels_, per_row, T_, V, st_);
     extra_from_device(per_row);
   } else if (obj_.kind == Objective::PREFERENCE) {
-    float* ref = floats(B_);
     mk::PreferenceArgs a;
+    void* workspace = floats((int64_t)(mk::token_loss_workspace_bytes(T_) / 4));
+    a.ref_logp = extra_to_device(floats(B_));
     a.seq_logp = floats(B_); a.margin = floats(B_ / 2); a.loss = loss_dev;
-    void* workspace = c_->arena.alloc(mk::token_loss_workspace_bytes(Tpad_));
-    if (dry_) return;
-    a.ends = ends_; a.pairs = B_ / 2; a.L = L_; a.ref_logp = extra_to_device(ref);
+    a.ends = ends_; a.pairs = B_ / 2; a.L = L_;
     a.beta = obj_.preference.beta; a.smoothing = obj_.preference.smoothing;
     mk::preference_loss(dt_, logits, ldv, labels_, a, logits, per_row, T_, V, workspace, st_);
     if (obj_.margin) extra_from_device(a.margin);
   } else {
-    const int arrays = 2 + (obj_.ref != nullptr) + (obj_.weight != nullptr);
-    float* in = floats(arrays * (int64_t)Tpad_);
     mk::PolicyArgs a;
-    a.rows = floats(4 * (int64_t)Tpad_); a.stats = loss_dev;
-    if (dry_) return;
-    const float* p = extra_to_device(in);
+    a.rows = floats(4 * (int64_t)T_); a.stats = loss_dev;
+    const float* p = extra_to_device(floats(extra_in()));
     a.old_logp = p; a.advantage = p += T_;
     if (obj_.ref) a.ref_logp = p += T_;
     if (obj_.weight) a.weight = p += T_;
