@@ -630,8 +630,10 @@ static void rows_t(const void* logits, int64_t ldl, const int32_t* labels, float
       held_t<T, MODE, true, true>(x, ldl, labels + r, lp, sta, sl, g, a, n, V, (int)chunks, st);
     else if (held && even)
       held_t<T, 0, false, true>(x, ldl, labels + r, lp, sta, sl, g, a, n, V, (int)chunks, st);
-    else if (held)
+    else if (held && (past || MODE == 1))
       held_t<T, MODE, true, false>(x, ldl, labels + r, lp, sta, sl, g, a, n, V, (int)chunks, st);
+    else if (held)
+      held_t<T, 0, false, false>(x, ldl, labels + r, lp, sta, sl, g, a, n, V, (int)chunks, st);
     else
       hipLaunchKernelGGL((token_rows_long_kernel<T, MODE>), dim3(n), dim3(kLongThreads), 0, st, x, ldl, labels + r, lp, sta, sl, g, a, V);
   }
