@@ -660,11 +660,17 @@ static void preference_t(const void* logits, int64_t ldl, const int32_t* labels,
     return;
   }
   // The gradient reads the rows a second time.  Where they are few, what the first pass has read is still in the last cache
-  // (256 MB), where many are it is not, and loads past the caches are faster.  Labels say what is read of them, and they are on
-  // the device: the bound is of all rows, 640 MB, of which some hundred are prompts.  6352 rows of 50257, 0.4 of them prompts
-  // (639 MB): 223 us through the caches, 249 past them; 8192 of 30522, no prompts (500 MB): 255 and 249; 16384 of 50257: 849 and
-  // 778.  Chunks a thread: 2 and 1, 788 and 749 in the last of these, 143 and 151 for 4200 rows (422 MB).
-  const bool few = rows * ldl * (int64_t)sizeof(T) <= (int64_t)640 << 20;
+  // (256 MB), where many are it is not, and loads past the caches are faster.  What counts is the rows that are scored, and labels
+  // are on the device: the bounds are of all rows, where a batch of which a quarter is prompts takes as long either way.  Rows of
+  // 50257 in bf16, us through the caches and past them, no row a prompt, a quarter of them, half of them:
+  //   gradient beside   256 MB 125 128, 106 110, 81 94   400 MB 195 193, 156 166, 127 139   640 MB 316 303, 258 259, 193 215
+  //                     850 MB 423 400, 348 342, 268 283
+  //   in place          100 MB 56 58, 46 49, 38 43   160 MB 100 85, 76 75, 55 64   256 MB 149 128, 125 109, 92 93
+  //                     640 MB 365 303 (no prompts): stores past the caches to what a cache holds are slow
+  // (30522 columns, 4000, and fp32: the same within some per cent.)  Chunks a thread: 2 and 1, 788 and 749 for 16384 rows (1.6 GB)
+  // past the caches, 143 and 151 for 4200 rows (422 MB) through them.
+  const int64_t most_cached = (int64_t)(dlogits == logits ? 160 : 640) << 20;
+  const bool few = rows * ldl * (int64_t)sizeof(T) <= most_cached;
   const int64_t before = ldl % N == 0 && ((uintptr_t)logits & 15) == 0 ? 0 : N - 1;       // of a row, in its first chunk
   const int64_t per_block = (int64_t)kRowThreads * grad_chunks(!few) * N, parts = (before + ldl + per_block - 1) / per_block;
   const int most = (int)std::max<int64_t>(1, ((int64_t)kRowsPerLaunch * 8) / parts);

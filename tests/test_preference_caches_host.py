@@ -27,3 +27,16 @@ def test_beside(runtime, dtype):  # noqa: F811
             got = preference(dtype, V, ld, T, at + offset, far)
             assert got == [(past, even, past)], (V, ld, T, got)
     """, dtype)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_in_place(runtime, dtype):  # noqa: F811
+    run(runtime, SETUP + """
+    dtype = int(sys.argv[2])
+    size, most = 2 if dtype else 4, 160 << 20
+    for V, ld, offset, even in ((50257, 50304, 0, 1), (50257, 50257, 0, 0), (1003, 1003, 0, 0), (1000, 1024, size, 0), (1000, 1000, 0, 1)):
+        rows = most // (ld * size)
+        for T, past in ((rows, 0), (rows + 1, 1), (rows * 4, 1), (rows * 5, 1)):
+            got = preference(dtype, V, ld, T, at + offset, at + offset)
+            assert got == [(past, even, past)], (V, ld, T, got)
+    """, dtype)
