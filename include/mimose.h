@@ -463,10 +463,11 @@ int mimose_op_preference_loss(int32_t dtype, const void* logits, int64_t ld, con
  *     gain = min(r A, clip(r, 1 - clip_low, 1 + clip_high) A),   kl = exp(d) - d - 1
  *     loss = sum of w (kl_weight kl - gain)
  * A token whose gain the clip holds back passes no gradient through r (one on the bound does).  A row
- * with w = 0 is left out of the loss whatever its other numbers and its logits are, its gradient is zeros.  ref_logp may be NULL when
- * kl_weight is 0.  old_logp, ref_logp, advantage, weight: fp32[T]; rows fp32 [T,4] (16-byte aligned)
- * receives logp, w (kl_weight kl - gain), w kl, and w where the clip held the gain back; stats fp32[3]
- * the sums of the last three: loss, KL, clipped share. */
+ * with w = 0 is left out of the loss whatever its other numbers and its logits are, and its gradient is
+ * zeros (rows still receives its logp).  ref_logp may be NULL when kl_weight is 0.  old_logp, ref_logp,
+ * advantage, weight: fp32[T]; rows fp32 [T,4] (16-byte aligned) receives logp, w (kl_weight kl - gain),
+ * w kl, and w where the clip held the gain back; stats fp32[3] the sums of the last three: loss, KL,
+ * clipped share. */
 int mimose_op_policy_loss(int32_t dtype, const void* logits, int64_t ld, const int32_t* labels,
                           const float* old_logp, const float* ref_logp, const float* advantage,
                           const float* weight, float scale, float clip_low, float clip_high,
@@ -479,10 +480,13 @@ int mimose_op_policy_loss(int32_t dtype, const void* logits, int64_t ld, const i
  * state_bits 8: m, v uint8[n] hold e4m3 codes (OCP: four exponent bits, three of mantissa) and m_scale,
  * v_scale fp32[ceil(n/256)] one factor for each 256 elements: the first moment is code * m_scale, the
  * square root of the second code * v_scale.  A step decodes, updates and rounds them anew with a dither
- * that is a function of element and step alone; the parameter moves by the unrounded moments.  All
- * zeros is the initial state of either.  Pointers 16-byte aligned (scales 4); a tensor may have n = 0.
+ * that is a function of element and step alone; the parameter moves by the unrounded moments.  A second
+ * moment above zero is held as the smallest code at least (2^-17.8 of its block's largest root): where an
+ * element's own root is smaller, its steps are smaller than AdamW's.  All zeros is the initial state of
+ * either.  Pointers 16-byte aligned (scales 4); a tensor may have n = 0.
  * mimose_op_adamw_table lays the list out in device memory of mimose_op_adamw_table_bytes (0: the list is
- * refused) and waits for the copy; the table holds the addresses, not the tensors.  step counts from 1.
+ * refused) and waits for the copy; the table holds the addresses, not the tensors: it is made once for
+ * tensors that stay where they are, gradients among them.  step counts from 1.
  */
 typedef struct {
   float* master; void* lowp; const float* grad;

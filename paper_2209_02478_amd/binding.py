@@ -561,7 +561,11 @@ class AdamWTable:
     tensors: dicts of tensors of one device, master (fp32), grad (fp32), m, v (fp32; uint8 or float8_e4m3fn with state_bits 8),
     lowp (bf16 or None), m_scale and v_scale (fp32, one entry for each 256 elements; state_bits 8), and decay (0 or 1).
     stream (an address; None: torch's current one) is the one that steps run on; a step on another has to have ended before
-    the table is let go."""
+    the table is let go.
+
+    Made once, where the tensors stay where they are: checking 29 tensors, laying them out and waiting for the copy takes 0.13 ms,
+    293 tensors 1.15 ms, as long as the update of the 355 M elements in them.  It holds addresses, so a gradient that comes to lie
+    elsewhere needs a new table: let gradients be written in place (zero_grad(set_to_none=False))."""
 
     BLOCK = 256   # elements that share a scale
 

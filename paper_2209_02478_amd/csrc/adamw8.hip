@@ -4,12 +4,15 @@
 //
 // Held are m and sqrt(v), not v: its square root has half the range in powers of two.  kAdamBlock neighbouring elements
 // of a tensor share an fp32 scale, which puts their largest value at 448, the largest of e4m3 (four bits of exponent,
-// three of mantissa): values down to 2^-18 of the largest keep a relative step of 1/8 or less.  Rounded to the nearest
-// code a slow moment would stand still (with b2 = 0.999 an update moves sqrt(v) by a twentieth of a per cent, codes lie
-// 6 to 12 per cent apart), so codes are rounded with a dither: a 20-bit number added below the last bit that is kept.  It
-// is the Weyl sequence (a element + b update) mod 2^32, b the golden ratio's: over the updates every element meets
-// evenly spread numbers, the rounding averages out, and nothing random has to be kept.  A second moment above zero is
-// never held as zero, which would make the next step one of m / eps.
+// three of mantissa).  Values down to 2^-14.8 of the largest (2^-6 of 448) lie within 1/8 of the next code; below that codes
+// are 2^-17.8 of the largest apart, so that a value at 2^-16 is held to a third and one below 2^-17.8 as nothing or as
+// the smallest code.  Rounded to the nearest code a slow moment would stand still (with b2 = 0.999 an update moves sqrt(v)
+// by a twentieth of a per cent, codes lie 6 to 12 per cent apart), so codes are rounded with a dither: a 20-bit number added
+// below the last bit that is kept.  It is the Weyl sequence (a element + b update) mod 2^32, b the golden ratio's: over the
+// updates every element meets evenly spread numbers, the rounding averages out, and nothing random has to be kept.
+// A second moment above zero is never held as zero, which would make the next step one of m / eps.  That is the one bias: a
+// root below 2^-17.8 of its block's largest is held as the smallest code and does not decay below it, so that such an
+// element's steps are smaller than the formula's, by the root's share of that code, as long as the block's largest stays.
 // Values that are not finite are held as NaN and do not enter their block's scale.
 //
 // Bound by memory: 18 bytes an element where a bf16 copy is written (30 with fp32 moments), 16 where not (28).  Nothing is

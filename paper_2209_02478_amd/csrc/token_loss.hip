@@ -288,10 +288,11 @@ void token_rows_held_kernel(const T* logits, int64_t ldl, const int32_t* __restr
   if (behind < ldl) zero_columns(g, behind, ldl, tid, TPR);
 }
 
-// WAVES and NCH by the chunks of a row: at least seven chunks a lane where the row has them, because fewer leave too few bytes
-// on the way to memory (policy loss, 16384 rows of 4000 in bf16: 79 us with 4 x 4, 54 with 1 x 9; of 15000: 259 with 8 x 4, 174
-// with 4 x 9), and registers of no more than 64 a lane, for two rows of 16 waves a unit.  Reading alone, 8 x 13 is ahead of 16 x
-// 7 (12288 rows of 50257: 183 us against 190); with the gradient behind it, it is not (550 against 517).
+// WAVES and NCH by the chunks of a row: as few waves as hold it with nine chunks a lane, because fewer chunks a lane leave too few
+// bytes on the way to memory (policy loss, 16384 rows of 4000 in bf16: 79 us with 4 x 4, 54 with 1 x 9; of 15000: 259 with 8 x 4,
+// 174 with 4 x 9), and registers of no more than 64 a lane, for two rows of 16 waves a unit; more chunks where 16 waves need them.
+// Reading alone, 8 x 13 is ahead of 16 x 7 (12288 rows of 50257: 183 us against 190); with the gradient behind it, it is not (550
+// against 517).
 #define HELD_ROWS(CHUNKS, M)                                 \
   if ((CHUNKS) <= 64) { M(1, 1) }                            \
   else if ((CHUNKS) <= 128) { M(1, 2) }                      \
@@ -674,9 +675,11 @@ static void preference_t(const void* logits, int64_t ldl, const int32_t* labels,
   const int64_t before = ldl % N == 0 && ((uintptr_t)logits & 15) == 0 ? 0 : N - 1;       // of a row, in its first chunk
   const int64_t per_block = (int64_t)kRowThreads * grad_chunks(!few) * N, parts = (before + ldl + per_block - 1) / per_block;
   const int most = (int)std::max<int64_t>(1, ((int64_t)kRowsPerLaunch * 8) / parts);
-  // A gradient of few blocks makes the pairs' sums itself, a launch less (2.5 us of the host's time): 4 x 33 rows of 1000 in fp32
-  // 16.2 -> 12.8 us, 240 of 50257 17.0 -> 15.3 (3100 blocks), 2400 of 1000 15.8 -> 12.5; but 3600 of 1000 13.9 -> 15.9, 500 of
-  // 50257 27.9 -> 29.7 (6500 blocks).
+  // A gradient of few blocks makes the pairs' sums itself, a launch less; but every block sums its pair's rows anew.  A quarter
+  // of the rows prompts, us with the launch of its own and without: 2 pairs of 33 rows of 1000 in fp32 13.4 and 9.6 (132
+  // blocks), 8 pairs of 50257 columns in bf16, 8 rows each 14.9 and 13.5 (1664 blocks), 14 rows 17.5 and 15.7 (2912), 31 rows
+  // 27.5 and 25.5 (6448); of 1000 columns, 150 rows each 13.0 and 11.0 (2400), 191 rows 12.9 and 13.2 (3056), 225 rows 13.5 and
+  // 14.9 (3600).  The bound is where sequences of short rows break even; long rows would bear twice as many.
   const bool sums = few && a.pairs <= kFewPairs && rows * parts <= 3072;
   float* slope = sums ? nullptr : (float*)(stat + rows);
   rows_t<T, 0>(logits, ldl, labels, logp, stat, slope, nullptr, PolicyArgs(), rows, V, !few, st);
