@@ -402,6 +402,37 @@ int mimose_op_attention_bwd(int32_t dtype, const void* qkv, const void* ctx, con
                             int32_t B, int32_t L, int32_t n_heads, int32_t head_dim,
                             int32_t causal, float p_drop, uint64_t seed, uint32_t site,
                             uint32_t step, void* stream);
+/*
+ * Attention over sequences that lie one behind the other without padding, with grouped heads.  ends: device
+ * int32 [n_seq], ascending, at most T: sequence s has the rows ends[s-1] .. ends[s]-1 (it may have none).  Query head h
+ * reads head h / (n_heads / n_kv_heads) of keys and values (n_heads a multiple of n_kv_heads); head_dim 32, 64 or 128;
+ * scale > 0.  For rows i, j of one sequence (causal: j <= i)
+ *     s_ij = scale q_i k_j,   lse_i = log sum_j exp(s_ij),   out_i = sum_j exp(s_ij - lse_i) v_j
+ * q, out [T, n_heads * head_dim], k, v [T, n_kv_heads * head_dim], storage type, each with a leading dimension of its own
+ * (below 2^21), so that a projection's output can hold all three; pointers and rows 16-byte aligned.  lse fp32
+ * [n_heads, T].  Rows from the last end on belong to no sequence: they are not read, and outputs stay there as they were.
+ * Rows of a sequence never meet those of another, whatever these hold; inside one, infinities and NaN spread.  What is
+ * written may overlap nothing else.  Sums have an order that depends on the sizes alone.  mimose_last_error(NULL) says why
+ * a call was refused.
+ */
+int mimose_op_packed_attention_fwd(int32_t dtype, const void* q, int64_t ldq, const void* k, int64_t ldk,
+                                   const void* v, int64_t ldv, void* out, int64_t ldo, float* lse,
+                                   const int32_t* ends, int32_t n_seq, int32_t T, int32_t n_heads,
+                                   int32_t n_kv_heads, int32_t head_dim, int32_t causal, float scale,
+                                   void* stream);
+/* Its gradient from what the forward pass left: with delta_i = dout_i out_i, P_ij = exp(s_ij - lse_i) and
+ * dS_ij = P_ij (dout_i v_j - delta_i)
+ *     dq_i = scale sum_j dS_ij k_j,   dk_j = scale sum dS_ij q_i,   dv_j = sum P_ij dout_i
+ * the last two over the rows and the query heads that read the head.  dout as out, dq as q, dk as k, dv as v; workspace:
+ * device scratch of mimose_op_packed_attention_bwd_workspace_bytes, 16-byte aligned. */
+uint64_t mimose_op_packed_attention_bwd_workspace_bytes(int32_t T, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim);
+int mimose_op_packed_attention_bwd(int32_t dtype, const void* q, int64_t ldq, const void* k, int64_t ldk,
+                                   const void* v, int64_t ldv, const void* out, int64_t ldo, const float* lse,
+                                   const void* dout, int64_t lddo, void* dq, int64_t lddq, void* dk,
+                                   int64_t lddk, void* dv, int64_t lddv, const int32_t* ends, int32_t n_seq,
+                                   int32_t T, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                                   int32_t causal, float scale, void* workspace, uint64_t workspace_bytes,
+                                   void* stream);
 /* dst[n] = (resid ? resid[n] : 0) + mask * src[n] / (1-p) with the mask mimose_set_dropout
  * describes for (seed, site, step).  dst, src: storage type, or fp32 when io_f32; resid: storage
  * type or NULL; dst may be src. */

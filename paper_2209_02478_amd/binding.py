@@ -131,6 +131,11 @@ SIGNATURES = {
                                           C.c_uint32, _vp]),
     "mimose_op_attention_bwd": (C.c_int, [_i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _i32, _f32,
                                           _u64, C.c_uint32, C.c_uint32, _vp]),
+    "mimose_op_packed_attention_fwd": (C.c_int, [_i32, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _i32, _i32, _i32, _i32, _i32,
+                                                 _i32, _f32, _vp]),
+    "mimose_op_packed_attention_bwd_workspace_bytes": (_u64, [_i32, _i32, _i32, _i32]),
+    "mimose_op_packed_attention_bwd": (C.c_int, [_i32, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _i64, _vp, _i64, _vp, _i64,
+                                                 _vp, _i64, _vp, _i32, _i32, _i32, _i32, _i32, _i32, _f32, _vp, _u64, _vp]),
     "mimose_op_softmax_xent": (C.c_int, [_i32, _vp, _i64, _vp, _vp, _vp, _i32, _i32, _i32, _vp]),
     "mimose_op_token_loss_workspace_bytes": (_u64, [_i32]),
     "mimose_op_token_logprob": (C.c_int, [_i32, _vp, _i64, _vp, _vp, _i32, _i32, _vp, _u64, _vp]),
@@ -473,6 +478,25 @@ def mimose_op_attention_bwd(dtype, qkv, ctx_in, dctx, lse, delta, dqkv, B, L, n_
     _check(load_library().mimose_op_attention_bwd(dtype, _ptr(qkv), _ptr(ctx_in), _ptr(dctx), _ptr(lse), _ptr(delta),
                                                   _ptr(dqkv), _ptr(lengths), B, L, n_heads, head_dim, causal, p_drop,
                                                   seed, site, step, _ptr(stream)))
+
+
+def mimose_op_packed_attention_fwd(dtype, q, ldq, k, ldk, v, ldv, out, ldo, lse, ends, n_seq, T, n_heads, n_kv_heads, head_dim, causal,
+                                   scale, stream=None):
+    _check(load_library().mimose_op_packed_attention_fwd(dtype, _ptr(q), ldq, _ptr(k), ldk, _ptr(v), ldv, _ptr(out), ldo, _ptr(lse),
+                                                         _ptr(ends), n_seq, T, n_heads, n_kv_heads, head_dim, causal, scale,
+                                                         _ptr(stream)))
+
+
+def mimose_op_packed_attention_bwd_workspace_bytes(T: int, n_heads: int, n_kv_heads: int, head_dim: int) -> int:
+    return load_library().mimose_op_packed_attention_bwd_workspace_bytes(T, n_heads, n_kv_heads, head_dim)
+
+
+def mimose_op_packed_attention_bwd(dtype, q, ldq, k, ldk, v, ldv, out, ldo, lse, dout, lddo, dq, lddq, dk, lddk, dv, lddv, ends, n_seq, T,
+                                   n_heads, n_kv_heads, head_dim, causal, scale, workspace, workspace_bytes, stream=None):
+    _check(load_library().mimose_op_packed_attention_bwd(dtype, _ptr(q), ldq, _ptr(k), ldk, _ptr(v), ldv, _ptr(out), ldo, _ptr(lse),
+                                                         _ptr(dout), lddo, _ptr(dq), lddq, _ptr(dk), lddk, _ptr(dv), lddv, _ptr(ends),
+                                                         n_seq, T, n_heads, n_kv_heads, head_dim, causal, scale, _ptr(workspace),
+                                                         workspace_bytes, _ptr(stream)))
 
 
 def mimose_op_dropout(dtype, dst, src, io_f32, resid, n, p, seed, site, step, stream=None):

@@ -146,6 +146,24 @@ void attention_fwd(int dtype, const void* qkv, void* ctx, float* lse, const Rows
 void attention_bwd(int dtype, const void* qkv, const void* ctx, const void* dctx, const float* lse,
                    float* delta, void* dqkv, const Rows& rows, int B, int L, int nh, int d, int causal,
                    const DropDesc& drop, hipStream_t st, hipEvent_t done = nullptr, int64_t rule_rows = 0);
+// Attention over packed sequences (packed_attention.hip, packed_attention_f32.hip): sequence s has the rows ends[s-1] .. ends[s] - 1
+// (device, [n_seq]) of T; n_heads / n_kv_heads query heads share a head of keys and values.
+struct PackedAttention {
+  const void *q = nullptr, *k = nullptr, *v = nullptr, *dout = nullptr;
+  void* out = nullptr;               // written by the forward pass, read by the backward
+  float* lse = nullptr;              // [n_heads, T], likewise
+  void *dq = nullptr, *dk = nullptr, *dv = nullptr;
+  float* delta = nullptr;            // [n_heads, T], scratch of the backward pass
+  int64_t ldq = 0, ldk = 0, ldv = 0, ldo = 0, lddo = 0, lddq = 0, lddk = 0, lddv = 0;
+  const int32_t* ends = nullptr;
+  int n_seq = 0, T = 0, n_heads = 0, n_kv_heads = 0;
+  float scale = 0.f;
+};
+constexpr int64_t kPackedLd = 1 << 21;                 // a leading dimension is below this: 64 rows of any type in 32 bits of bytes
+bool packed_attention_fits(int64_t T, int64_t n_seq, int64_t n_heads);   // whether a launch's blocks can be counted
+size_t packed_attention_bwd_workspace_bytes(int64_t T, int n_heads, int n_kv_heads, int d);
+void packed_attention_fwd(int dtype, const PackedAttention& p, int d, int causal, hipStream_t st);
+void packed_attention_bwd(int dtype, PackedAttention p, int d, int causal, void* workspace, hipStream_t st);
 void softmax_xent(int dtype, void* logits, int64_t ld, const int32_t* labels, float* row_loss,
                   float* loss, int T, int V, int n_valid, hipStream_t st);
 // Losses on the log-probabilities of given tokens (token_loss.hip): rows of logits, a label for each; a label

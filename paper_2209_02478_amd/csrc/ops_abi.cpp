@@ -23,6 +23,44 @@ int refuse(const char* op, const char* why) {
   mimose_set_thread_error(buf);
   return MIMOSE_ERR_INVALID_ARG;
 }
+// Rows of an operand, or (rows = 1) a plain array: where they begin, elements from one to the next, elements of each, bytes of one.
+struct RowSet { const void* at; int64_t ld, width, rows, es; bool plain = false; };
+bool overlap(const RowSet& a, const RowSet& b) {
+  if (!a.at || !b.at || a.rows < 1 || b.rows < 1) return false;
+  const int64_t la = a.ld * a.es, lb = b.ld * b.es, wa = a.width * a.es, wb = b.width * b.es;
+  const uintptr_t x = (uintptr_t)a.at, y = (uintptr_t)b.at;
+  if (x >= y + (uintptr_t)((b.rows - 1) * lb + wb) || y >= x + (uintptr_t)((a.rows - 1) * la + wa)) return false;
+  if (a.rows == 1 || b.rows == 1 || la != lb) return true;
+  const int64_t d = (((int64_t)(y - x)) % la + la) % la;   // columns of rows of one pitch: b's begin d bytes behind a's
+  return d < wa || d + wb > la;
+}
+// what is wrong with the sizes of packed attention, or null
+const char* bad_packed(int dtype, const int32_t* ends, int32_t n_seq, int32_t T, int32_t nh, int32_t nkv, int32_t d, float scale) {
+  if (bad_dtype(dtype)) return "dtype must be 0 (fp32) or 1 (bf16)";
+  if (T < 0 || n_seq < 0) return "T >= 0 and n_seq >= 0 required";
+  if (nh < 1 || nkv < 1 || nh % nkv) return "n_heads must be a multiple of n_kv_heads";
+  if (d != 32 && d != 64 && d != 128) return "head_dim must be 32, 64 or 128";
+  if (!std::isfinite(scale) || !(scale > 0.f)) return "scale must be finite and above 0";
+  if (n_seq > 0 && (!ends || (uintptr_t)ends % 4)) return "ends must be given, aligned to its elements";
+  if (!mk::packed_attention_fits(T, n_seq, nh)) return "too many rows, sequences and heads for one launch";
+  return nullptr;
+}
+// what is wrong with the operands, the first n_in of which are read and the others written, or null
+const char* bad_rows(const RowSet* s, int n_in, int n) {
+  for (int i = 0; i < n; ++i) {
+    if (!s[i].at) return "every operand must be given";
+    if (s[i].plain) {
+      if ((uintptr_t)s[i].at % 4) return "lse is not aligned to its elements";
+    } else {
+      if (s[i].ld < s[i].width || s[i].ld >= mk::kPackedLd) return "a leading dimension must cover its heads and be below 2^21";
+      if ((uintptr_t)s[i].at % 16 || s[i].ld * s[i].es % 16) return "operands and their rows must be 16-byte aligned";
+    }
+  }
+  for (int i = n_in; i < n; ++i)
+    for (int j = 0; j < i; ++j)
+      if (overlap(s[i], s[j])) return "an operand that is written overlaps another";
+  return nullptr;
+}
 // what is wrong with rows of logits and the gradient beside them, or null
 const char* bad_logits(int dtype, const void* logits, int64_t ld, const int32_t* labels, const void* dlogits, int T, int V) {
   if (bad_dtype(dtype)) return "dtype must be 0 (fp32) or 1 (bf16)";
@@ -141,6 +179,51 @@ int mimose_op_attention_bwd(int32_t dtype, const void* qkv, const void* ctx, con
     return MIMOSE_ERR_INVALID_ARG;
   mk::attention_bwd(dtype, qkv, ctx, dctx, lse, delta, dqkv, mk::Rows{lengths, nullptr, 0}, B, L, nh, d, causal,
                     make_desc(p_drop, seed, site, step), (hipStream_t)stream);
+  return done();
+}
+
+int mimose_op_packed_attention_fwd(int32_t dtype, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv,
+                                   void* out, int64_t ldo, float* lse, const int32_t* ends, int32_t n_seq, int32_t T, int32_t nh,
+                                   int32_t nkv, int32_t d, int32_t causal, float scale, void* stream) {
+  const char* const op = "mimose_op_packed_attention_fwd";
+  if (const char* why = bad_packed(dtype, ends, n_seq, T, nh, nkv, d, scale)) return refuse(op, why);
+  if (T == 0 || n_seq == 0) return MIMOSE_OK;
+  const int64_t es = mk::elt_size(dtype), w = (int64_t)nh * d, wk = (int64_t)nkv * d, n = T, stats = (int64_t)nh * T;
+  const RowSet s[] = {{q, ldq, w, n, es}, {k, ldk, wk, n, es}, {v, ldv, wk, n, es}, {ends, n_seq, n_seq, 1, 4, true}, {out, ldo, w, n, es},
+                      {lse, stats, stats, 1, 4, true}};
+  if (const char* why = bad_rows(s, 4, 6)) return refuse(op, why);
+  mk::PackedAttention p;
+  p.q = q; p.k = k; p.v = v; p.out = out; p.lse = lse; p.ldq = ldq; p.ldk = ldk; p.ldv = ldv; p.ldo = ldo;
+  p.ends = ends; p.n_seq = n_seq; p.T = T; p.n_heads = nh; p.n_kv_heads = nkv; p.scale = scale;
+  mk::packed_attention_fwd(dtype, p, d, causal, (hipStream_t)stream);
+  return done();
+}
+
+uint64_t mimose_op_packed_attention_bwd_workspace_bytes(int32_t T, int32_t nh, int32_t nkv, int32_t d) {
+  return T > 0 && nh > 0 && nkv > 0 && d > 0 ? mk::packed_attention_bwd_workspace_bytes(T, nh, nkv, d) : 0;
+}
+
+int mimose_op_packed_attention_bwd(int32_t dtype, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv,
+                                   const void* out, int64_t ldo, const float* lse, const void* dout, int64_t lddo, void* dq, int64_t lddq,
+                                   void* dk, int64_t lddk, void* dv, int64_t lddv, const int32_t* ends, int32_t n_seq, int32_t T,
+                                   int32_t nh, int32_t nkv, int32_t d, int32_t causal, float scale, void* workspace,
+                                   uint64_t workspace_bytes, void* stream) {
+  const char* const op = "mimose_op_packed_attention_bwd";
+  if (const char* why = bad_packed(dtype, ends, n_seq, T, nh, nkv, d, scale)) return refuse(op, why);
+  if (T == 0 || n_seq == 0) return MIMOSE_OK;
+  const int64_t es = mk::elt_size(dtype), w = (int64_t)nh * d, wk = (int64_t)nkv * d, n = T, stats = (int64_t)nh * T;
+  const int64_t need = (int64_t)mk::packed_attention_bwd_workspace_bytes(T, nh, nkv, d);
+  if (!workspace || (uintptr_t)workspace % 16 || workspace_bytes < (uint64_t)need)
+    return refuse(op, "workspace must be 16-byte aligned and of mimose_op_packed_attention_bwd_workspace_bytes");
+  const RowSet s[] = {{q, ldq, w, n, es}, {k, ldk, wk, n, es}, {v, ldv, wk, n, es}, {out, ldo, w, n, es}, {dout, lddo, w, n, es},
+                      {ends, n_seq, n_seq, 1, 4, true}, {lse, stats, stats, 1, 4, true}, {dq, lddq, w, n, es}, {dk, lddk, wk, n, es}, {dv, lddv, wk, n, es},
+                      {workspace, need, need, 1, 1, true}};
+  if (const char* why = bad_rows(s, 7, 11)) return refuse(op, why);
+  mk::PackedAttention p;
+  p.q = q; p.k = k; p.v = v; p.out = const_cast<void*>(out); p.lse = const_cast<float*>(lse); p.dout = dout; p.dq = dq; p.dk = dk; p.dv = dv;
+  p.ldq = ldq; p.ldk = ldk; p.ldv = ldv; p.ldo = ldo; p.lddo = lddo; p.lddq = lddq; p.lddk = lddk; p.lddv = lddv;
+  p.ends = ends; p.n_seq = n_seq; p.T = T; p.n_heads = nh; p.n_kv_heads = nkv; p.scale = scale;
+  mk::packed_attention_bwd(dtype, p, d, causal, workspace, (hipStream_t)stream);
   return done();
 }
 

@@ -1,0 +1,451 @@
+// Fused attention over packed sequences with grouped heads, bf16, head sizes 32, 64 and 128, on the MFMA units
+// (v_mfma_f32_32x32x16_bf16).
+//
+//   forward   s_ij = scale q_i k_j over the rows j of i's sequence (causal: j <= i),
+//             lse_i = log sum_j exp(s_ij),  o_i = sum_j exp(s_ij - lse_i) v_j
+//   backward  delta_i = do_i o_i,  P_ij = exp(s_ij - lse_i),  dS_ij = P_ij (do_i v_j - delta_i),
+//             dq_i = scale sum_j dS_ij k_j,  dk_j = scale sum dS_ij q_i,  dv_j = sum P_ij do_i,
+//             the last two over the rows i and the query heads that share the head of keys
+//
+// Score tiles are computed transposed, S^T = K Q^T, so that a lane's accumulator registers belong to one query (forward,
+// dQ) or one key (dK/dV): softmax statistics are reductions over a lane's own registers and one exchange with lane ^ 32,
+// and the probabilities, rounded to bf16 (they multiply bf16 rows: the same relative step as the other factor's; sums stay
+// in fp32), are the B operand of the next product as they stand.  The operand that multiplies them is read out of LDS by the
+// transposing reads, so that a tile is there once, brought by direct loads into one of two buffers while the other is
+// multiplied, one barrier to a tile.
+//
+// MFMA 32x32x16 (A: 32 x 16, B: 16 x 32, D: 32 x 32):
+//   A, B: lane holds row / column lane % 32 and reduction indices 8 * (lane / 32) .. + 7
+//   D:    lane holds column lane % 32; register r holds row 8 * (r / 4) + 4 * (lane / 32) + r % 4
+//
+// Rows of other sequences are never read: a tile's buffer ends with the sequence, and what lies behind is zeros in LDS.
+// No atomics: dQ comes from a kernel that owns query rows, dK/dV from one that owns key rows, both in a fixed order.
+#include "gemm_device.h"
+#include "packed_device.h"
+
+namespace mk {
+namespace {
+
+constexpr int TK = 64;                 // rows of a streamed tile
+constexpr int BM = 128;                // own rows of a block: 32 to a wave
+constexpr float LOG2E = 1.44269504088896340736f;
+
+__device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }   // -inf gives 0
+
+// registers 8c .. 8c+7 of an accumulator as a bf16 operand
+__device__ __forceinline__ bf16x8 regs_to_frag(const f32x16& v, int c) {
+  uint4 u;
+  u.x = pack_bf16x2(v[8 * c + 0], v[8 * c + 1]);
+  u.y = pack_bf16x2(v[8 * c + 2], v[8 * c + 3]);
+  u.z = pack_bf16x2(v[8 * c + 4], v[8 * c + 5]);
+  u.w = pack_bf16x2(v[8 * c + 6], v[8 * c + 7]);
+  return __builtin_bit_cast(bf16x8, u);
+}
+__device__ __forceinline__ void zero(f32x16& v) {
+#pragma unroll
+  for (int r = 0; r < 16; ++r) v[r] = 0.f;
+}
+// the value of lane ^ 32
+__device__ __forceinline__ float other_half(float v) {
+  const uint32_t u = __float_as_uint(v);
+  const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
+}
+
+// 16-byte chunk c of a tile's row r lies at position c ^ swizzle(r), so that a plain read (16 rows, one chunk) and a
+// transposing one (4 rows, 4 chunks in 32 lanes) both meet all 64 banks once: rows of 64, 128 and 256 bytes begin on
+// every fourth, second and the same bank, and the rest of the row number has to move the chunk.
+template <int D>
+__device__ __forceinline__ int swizzle(int r) {
+  return ((r >> 2) & 3) | (D == 64 ? (r & 2) << 1 : D == 128 ? (r & 3) << 2 : 0);
+}
+
+// A tile of TK rows in LDS: its direct loads and a wave's fragments of it.
+template <int D>
+struct Tile {
+  static constexpr int SIZE = TK * D;              // elements
+  static constexpr int LOADS = D / 32;             // 1 KB direct loads of each of four waves
+  uint32_t from[LOADS];                            // byte offset of the lane's chunk from the tile's first row
+  int plain, turned;
+  __device__ __forceinline__ void init(int wave, int lane, int ld) {
+    constexpr int NC = D / 8;
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) {
+      const int row = 16 * wave + j * (64 / NC) + lane / NC;
+      from[j] = (uint32_t)(row * ld + (((lane % NC) ^ swizzle<D>(row)) << 3)) * 2u;
+    }
+    const int h = lane >> 5, r = lane & 31, q = 4 * h + ((lane & 15) >> 2);
+    plain = r * D + ((h ^ swizzle<D>(r)) << 3);
+    turned = q * D + (((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ swizzle<D>(q)) << 3) + 4 * (lane & 1);
+  }
+  // base, bytes: the tile's rows that exist
+  __device__ __forceinline__ void load(uint64_t base, uint32_t bytes, int wave, uint32_t lds) const {
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) l_direct_load(base, bytes, from[j], lds + (uint32_t)(wave * LOADS + j) * 1024u);
+  }
+  // row 32 * block + lane % 32, columns 16 kk + 8 h .. + 7
+  __device__ __forceinline__ bf16x8 row(const bf16_t* tile, int block, int kk) const {
+    return *(const bf16x8*)(tile + block * 32 * D + (plain ^ (kk << 4)));
+  }
+  // column 32 db + lane % 32, rows base + 4 h + {0..3}, base + 8 + 4 h + {0..3} (base % 16 == 0): within 16 lanes of a
+  // transposing read, lane i gets column i of the 4 x 16 block whose row k lies at the four lanes 4k ..; 8 rows on, bit 1
+  // of swizzle() flips
+  __device__ __forceinline__ bf16x8 column(const bf16_t* tile, int db, int base) const {
+    const int at = turned ^ (db << 5);
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_l*)(tile + base * D + at));
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_l*)(tile + (base + 8) * D + (at ^ 16)));
+    typedef short s16x8 __attribute__((ext_vector_type(8)));
+    return __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  }
+};
+
+// The rows of an operand from one row on, tile after tile: scalar registers alone.
+struct Stream {
+  uint64_t base;
+  uint32_t pitch;                                  // bytes of a row
+  __device__ __forceinline__ void init(const bf16_t* first, int ld) { l_descriptor(first, (uint32_t)ld * 2u, base, pitch); }
+  __device__ __forceinline__ uint64_t at(int row) const { return base + (uint64_t)row * pitch; }
+  __device__ __forceinline__ uint32_t bytes(int rows) const { return (uint32_t)min(rows, TK) * pitch; }
+};
+
+// Every wave's direct loads so far are in LDS, and every wave is done reading what it read before.
+__device__ __forceinline__ void landed() {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+}
+
+// store a transposed accumulator (rows = head columns, lane column = token) as bf16
+template <int D>
+__device__ __forceinline__ void store_rows(bf16_t* dst, const f32x16 (&acc)[D / 32], int h, float mul) {
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      uint2 o;
+      o.x = pack_bf16x2(acc[db][4 * g] * mul, acc[db][4 * g + 1] * mul);
+      o.y = pack_bf16x2(acc[db][4 * g + 2] * mul, acc[db][4 * g + 3] * mul);
+      *(uint2*)(dst + 32 * db + 8 * g + 4 * h) = o;
+    }
+}
+
+}  // namespace
+
+// ------------------------------------------------------------------ forward
+template <int D, bool CAUSAL>
+__global__ __launch_bounds__(256, 2) void packed_fwd_kernel(PackedAttention p, int slots) {
+  constexpr int KK = D / 16, DB = D / 32;
+  __shared__ __attribute__((aligned(1024))) bf16_t tiles[2][2][Tile<D>::SIZE];   // [buffer][K, V]
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), ql = lane & 31, h = lane >> 5;
+  PackedPlace w;
+  if (!packed_place<BM>(p, slots, w)) return;
+  const int w0 = w.row + wave * 32, qi = w0 + ql, qc = min(qi, w.n - 1);
+  const float c2 = p.scale * LOG2E;                   // exp(scale * s - x) == exp2(c2 * s - LOG2E * x)
+
+  const bf16_t* qrow = (const bf16_t*)p.q + (w.first + qc) * p.ldq + w.head * D + 8 * h;
+  bf16x8 qf[KK];
+#pragma unroll
+  for (int kk = 0; kk < KK; ++kk) qf[kk] = *(const bf16x8*)(qrow + 16 * kk);
+  f32x16 o[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db) zero(o[db]);
+  float m = -INFINITY, l = 0.f;                       // running maximum of the raw (unscaled) scores, sum of exps
+  const int kend = CAUSAL ? min(w.n, w.row + BM) : w.n;
+
+  Tile<D> tk, tv;
+  tk.init(wave, lane, (int)p.ldk);
+  tv.init(wave, lane, (int)p.ldv);
+  Stream ks, vs;
+  ks.init((const bf16_t*)p.k + w.first * p.ldk + w.kv * D, (int)p.ldk);
+  vs.init((const bf16_t*)p.v + w.first * p.ldv + w.kv * D, (int)p.ldv);
+  const uint32_t lds = l_lds_address(&tiles[0][0][0]);
+  auto fetch = [&](int k0, int buf) {
+    tk.load(ks.at(k0), ks.bytes(w.n - k0), wave, lds + (uint32_t)buf * (4u * Tile<D>::SIZE));
+    tv.load(vs.at(k0), vs.bytes(w.n - k0), wave, lds + (uint32_t)buf * (4u * Tile<D>::SIZE) + 2u * Tile<D>::SIZE);
+  };
+  fetch(0, 0);
+  for (int k0 = 0, buf = 0; k0 < kend; k0 += TK, buf ^= 1) {
+    landed();
+    if (k0 + TK < kend) fetch(k0 + TK, buf ^ 1);
+    const bf16_t *Ks = tiles[buf][0], *Vs = tiles[buf][1];
+    if (w0 >= w.n || (CAUSAL && k0 > w0 + 31)) continue;   // none of this wave's queries sees the tile
+    const bool edge = k0 + TK > w.n || (CAUSAL && k0 + TK - 1 > w0);
+    f32x16 s[2];
+    float mx = -INFINITY;
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+      zero(s[kb]);
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tk.row(Ks, kb, kk), qf[kk], s[kb], 0, 0, 0);
+      if (edge) {                                     // only tiles that touch the mask pay for it
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int key = k0 + 32 * kb + 8 * (r >> 2) + 4 * h + (r & 3);
+          if (key >= w.n || (CAUSAL && key > qi)) s[kb][r] = -INFINITY;
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[kb][r]);
+    }
+    mx = fmaxf(mx, other_half(mx));
+    const float mnew = fmaxf(m, mx);                  // finite: a sequence's first row is visible to all of them
+    float alpha = 1.f;
+    if (__any(mx > m)) {                              // else alpha is 1 in every lane: nothing to scale
+      alpha = fast_exp2((m - mnew) * c2);
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[db][r] *= alpha;
+      m = mnew;
+    }
+    const float off = -mnew * c2;
+    float rs = 0.f;
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float e = fast_exp2(fmaf(s[kb][r], c2, off));
+        s[kb][r] = e;
+        rs += e;
+      }
+    rs += other_half(rs);
+    l = fmaf(l, alpha, rs);
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const bf16x8 pf = regs_to_frag(s[kb], c);
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+          o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tv.column(Vs, db, 32 * kb + 16 * c), pf, o[db], 0, 0, 0);
+      }
+  }
+  if (qi < w.n) {
+    store_rows<D>((bf16_t*)p.out + (w.first + qi) * p.ldo + w.head * D, o, h, 1.f / l);
+    if (h == 0) p.lse[(int64_t)w.head * p.T + w.first + qi] = m * p.scale + __logf(l);
+  }
+}
+
+// ------------------------------------------------------------------ dQ
+template <int D, bool CAUSAL>
+__global__ __launch_bounds__(256, 2) void packed_bwd_dq_kernel(PackedAttention p, int slots) {
+  constexpr int KK = D / 16, DB = D / 32;
+  __shared__ __attribute__((aligned(1024))) bf16_t tiles[2][2][Tile<D>::SIZE];   // [buffer][K, V]
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), ql = lane & 31, h = lane >> 5;
+  PackedPlace w;
+  if (!packed_place<BM>(p, slots, w)) return;
+  const int w0 = w.row + wave * 32, qi = w0 + ql, qc = min(qi, w.n - 1);
+  const float c2 = p.scale * LOG2E;
+
+  // delta: each half of the wave holds half of the head's columns.  Written out for the dK/dV kernel, which runs after.
+  bf16x8 qf[KK], gf[KK];
+  float delta = 0.f;
+  {
+    const int64_t r = w.first + qc;
+    const bf16_t* qrow = (const bf16_t*)p.q + r * p.ldq + w.head * D + 8 * h;
+    const bf16_t* grow = (const bf16_t*)p.dout + r * p.lddo + w.head * D + 8 * h;
+    const bf16_t* orow = (const bf16_t*)p.out + r * p.ldo + w.head * D + 8 * h;
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) {
+      qf[kk] = *(const bf16x8*)(qrow + 16 * kk);
+      gf[kk] = *(const bf16x8*)(grow + 16 * kk);
+      const bf16x8 of = *(const bf16x8*)(orow + 16 * kk);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) delta = fmaf((float)of[e], (float)gf[kk][e], delta);
+    }
+  }
+  delta += other_half(delta);
+  const int64_t stat = (int64_t)w.head * p.T + w.first;
+  if (h == 0 && qi < w.n) p.delta[stat + qi] = delta;
+  const float nlse = -LOG2E * p.lse[stat + qc];
+  f32x16 dq[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db) zero(dq[db]);
+  const int kend = CAUSAL ? min(w.n, w.row + BM) : w.n;
+
+  Tile<D> tk, tv;
+  tk.init(wave, lane, (int)p.ldk);
+  tv.init(wave, lane, (int)p.ldv);
+  Stream ks, vs;
+  ks.init((const bf16_t*)p.k + w.first * p.ldk + w.kv * D, (int)p.ldk);
+  vs.init((const bf16_t*)p.v + w.first * p.ldv + w.kv * D, (int)p.ldv);
+  const uint32_t lds = l_lds_address(&tiles[0][0][0]);
+  auto fetch = [&](int k0, int buf) {
+    tk.load(ks.at(k0), ks.bytes(w.n - k0), wave, lds + (uint32_t)buf * (4u * Tile<D>::SIZE));
+    tv.load(vs.at(k0), vs.bytes(w.n - k0), wave, lds + (uint32_t)buf * (4u * Tile<D>::SIZE) + 2u * Tile<D>::SIZE);
+  };
+  fetch(0, 0);
+  for (int k0 = 0, buf = 0; k0 < kend; k0 += TK, buf ^= 1) {
+    landed();
+    if (k0 + TK < kend) fetch(k0 + TK, buf ^ 1);
+    const bf16_t *Ks = tiles[buf][0], *Vs = tiles[buf][1];
+    if (w0 >= w.n || (CAUSAL && k0 > w0 + 31)) continue;   // none of this wave's queries sees the tile
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+      f32x16 s, dp;
+      zero(s); zero(dp);
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) {
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tk.row(Ks, kb, kk), qf[kk], s, 0, 0, 0);
+        dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tv.row(Vs, kb, kk), gf[kk], dp, 0, 0, 0);
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = fast_exp2(fmaf(s[r], c2, nlse)) * (dp[r] - delta);
+      if (k0 + TK > w.n || (CAUSAL && k0 + TK - 1 > w0)) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int key = k0 + 32 * kb + 8 * (r >> 2) + 4 * h + (r & 3);
+          if (key >= w.n || (CAUSAL && key > qi)) s[r] = 0.f;
+        }
+      }
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const bf16x8 dsf = regs_to_frag(s, c);
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+          dq[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tk.column(Ks, db, 32 * kb + 16 * c), dsf, dq[db], 0, 0, 0);
+      }
+    }
+  }
+  if (qi < w.n) store_rows<D>((bf16_t*)p.dq + (w.first + qi) * p.lddq + w.head * D, dq, h, p.scale);
+}
+
+// ------------------------------------------------------------------ dK, dV
+// A block takes its keys through the query rows of every head that shares them, one head after the other.
+template <int D, bool CAUSAL>
+__global__ __launch_bounds__(256, D == 128 ? 1 : 2) void packed_bwd_dkv_kernel(PackedAttention p, int slots) {
+  constexpr int KK = D / 16, DB = D / 32;
+  __shared__ __attribute__((aligned(1024))) bf16_t tiles[2][2][Tile<D>::SIZE];   // [buffer][Q, dO]
+  __shared__ __attribute__((aligned(16))) float lse_s[2][TK], delta_s[2][TK];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), kl = lane & 31, h = lane >> 5;
+  PackedPlace w;
+  if (!packed_place_kv<BM>(p, slots, CAUSAL, w)) return;
+  const int w0 = w.row + wave * 32, ki = w0 + kl, kc = min(ki, w.n - 1);
+  const float c2 = p.scale * LOG2E;
+
+  bf16x8 kf[KK], vf[KK];
+  {
+    const bf16_t* krow = (const bf16_t*)p.k + (w.first + kc) * p.ldk + w.kv * D + 8 * h;
+    const bf16_t* vrow = (const bf16_t*)p.v + (w.first + kc) * p.ldv + w.kv * D + 8 * h;
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) {
+      kf[kk] = *(const bf16x8*)(krow + 16 * kk);
+      vf[kk] = *(const bf16x8*)(vrow + 16 * kk);
+    }
+  }
+  f32x16 dk[DB], dv[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db) { zero(dk[db]); zero(dv[db]); }
+  const int qstart = CAUSAL ? w.row : 0;              // earlier queries never see these keys (a multiple of TK)
+  const int group = p.n_heads / p.n_kv_heads;
+
+  Tile<D> tq, tg;
+  tq.init(wave, lane, (int)p.ldq);
+  tg.init(wave, lane, (int)p.lddo);
+  Stream qs, gs;
+  qs.init((const bf16_t*)p.q + w.first * p.ldq + w.kv * group * D, (int)p.ldq);
+  gs.init((const bf16_t*)p.dout + w.first * p.lddo + w.kv * group * D, (int)p.lddo);
+  const uint32_t lds = l_lds_address(&tiles[0][0][0]);
+  const int64_t stats = (int64_t)w.kv * group * p.T + w.first;
+  float pre_lse = 0.f, pre_delta = 0.f;
+  auto fetch = [&](int head, int q0, int buf) {
+    const uint64_t at = (uint64_t)head * (D * 2u);
+    tq.load(qs.at(q0) + at, qs.bytes(w.n - q0), wave, lds + (uint32_t)buf * (4u * Tile<D>::SIZE));
+    tg.load(gs.at(q0) + at, gs.bytes(w.n - q0), wave, lds + (uint32_t)buf * (4u * Tile<D>::SIZE) + 2u * Tile<D>::SIZE);
+    if (tid < TK) {
+      const int q = min(q0 + tid, w.n - 1);
+      pre_lse = p.lse[stats + (int64_t)head * p.T + q];
+      pre_delta = p.delta[stats + (int64_t)head * p.T + q];
+    }
+  };
+  fetch(0, qstart, 0);
+  int buf = 0;
+  for (int head = 0; head < group; ++head)
+    for (int q0 = qstart; q0 < w.n; q0 += TK, buf ^= 1) {
+      // lse_s: ready for exp2, and minus infinity behind the sequence: probabilities of zero there.  This buffer was last
+      // read two tiles ago, before the last barrier.
+      if (tid < TK) { lse_s[buf][tid] = q0 + tid < w.n ? -LOG2E * pre_lse : -INFINITY; delta_s[buf][tid] = pre_delta; }
+      landed();
+      if (q0 + TK < w.n) fetch(head, q0 + TK, buf ^ 1);
+      else if (head + 1 < group) fetch(head + 1, qstart, buf ^ 1);
+      if (w0 >= w.n || (CAUSAL && q0 + TK <= w0)) continue;   // no query of the tile sees this wave's keys
+      const bf16_t *Qs = tiles[buf][0], *Gs = tiles[buf][1];
+#pragma unroll
+      for (int qb = 0; qb < 2; ++qb) {
+        f32x16 s, dp;
+        zero(s); zero(dp);
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) {
+          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tq.row(Qs, qb, kk), kf[kk], s, 0, 0, 0);
+          dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tg.row(Gs, qb, kk), vf[kk], dp, 0, 0, 0);
+        }
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const int qq = 32 * qb + 8 * g + 4 * h;
+          const float4 nl = *(const float4*)&lse_s[buf][qq], dl = *(const float4*)&delta_s[buf][qq];
+          const float nls[4] = {nl.x, nl.y, nl.z, nl.w}, dls[4] = {dl.x, dl.y, dl.z, dl.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int r = 4 * g + e;
+            const float pr = fast_exp2(fmaf(s[r], c2, nls[e]));
+            s[r] = pr;
+            dp[r] = pr * (dp[r] - dls[e]);
+          }
+        }
+        if (CAUSAL && q0 < w0 + 31) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int q = q0 + 32 * qb + 8 * (r >> 2) + 4 * h + (r & 3);
+            if (ki > q) { s[r] = 0.f; dp[r] = 0.f; }
+          }
+        }
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const bf16x8 pf = regs_to_frag(s, c), dsf = regs_to_frag(dp, c);
+#pragma unroll
+          for (int db = 0; db < DB; ++db) {
+            dv[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tg.column(Gs, db, 32 * qb + 16 * c), pf, dv[db], 0, 0, 0);
+            dk[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tq.column(Qs, db, 32 * qb + 16 * c), dsf, dk[db], 0, 0, 0);
+          }
+        }
+      }
+    }
+  if (ki < w.n) {
+    store_rows<D>((bf16_t*)p.dk + (w.first + ki) * p.lddk + w.kv * D, dk, h, p.scale);
+    store_rows<D>((bf16_t*)p.dv + (w.first + ki) * p.lddv + w.kv * D, dv, h, 1.f);
+  }
+}
+
+namespace {
+template <int D>
+void launch_fwd(const PackedAttention& p, int causal, hipStream_t st) {
+  const int slots = packed_slots(p.T, p.n_seq, BM);
+  const dim3 grid(packed_blocks(slots, p.n_kv_heads, p.n_heads / p.n_kv_heads));
+  if (causal) hipLaunchKernelGGL((packed_fwd_kernel<D, true>), grid, dim3(256), 0, st, p, slots);
+  else hipLaunchKernelGGL((packed_fwd_kernel<D, false>), grid, dim3(256), 0, st, p, slots);
+}
+template <int D>
+void launch_bwd(const PackedAttention& p, int causal, hipStream_t st) {
+  const int slots = packed_slots(p.T, p.n_seq, BM);
+  const dim3 grid(packed_blocks(slots, p.n_kv_heads, p.n_heads / p.n_kv_heads)), grid_kv(packed_blocks(slots, p.n_kv_heads, 1));
+  if (causal) {
+    hipLaunchKernelGGL((packed_bwd_dq_kernel<D, true>), grid, dim3(256), 0, st, p, slots);
+    hipLaunchKernelGGL((packed_bwd_dkv_kernel<D, true>), grid_kv, dim3(256), 0, st, p, slots);
+  } else {
+    hipLaunchKernelGGL((packed_bwd_dq_kernel<D, false>), grid, dim3(256), 0, st, p, slots);
+    hipLaunchKernelGGL((packed_bwd_dkv_kernel<D, false>), grid_kv, dim3(256), 0, st, p, slots);
+  }
+}
+}  // namespace
+
+void packed_attention_fwd_bf16(const PackedAttention& p, int d, int causal, hipStream_t st) {
+  if (d == 32) launch_fwd<32>(p, causal, st);
+  else if (d == 64) launch_fwd<64>(p, causal, st);
+  else launch_fwd<128>(p, causal, st);
+}
+void packed_attention_bwd_bf16(const PackedAttention& p, int d, int causal, hipStream_t st) {
+  if (d == 32) launch_bwd<32>(p, causal, st);
+  else if (d == 64) launch_bwd<64>(p, causal, st);
+  else launch_bwd<128>(p, causal, st);
+}
+
+}  // namespace mk

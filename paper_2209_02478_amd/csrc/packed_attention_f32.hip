@@ -1,0 +1,395 @@
+// Fused attention over packed sequences with grouped heads in fp32, head sizes 32, 64 and 128, on the fp32 matrix
+// instruction (v_mfma_f32_32x32x2_f32); formulas as in packed_attention.hip.
+//
+// Bound by the matrix instruction: 64 clocks for 4096 operations, two (forward), three (dQ) and four (dK/dV) times D / 2 of
+// them for 32 x 32 scores.  So everything else may take its time: 32 own rows belong to W waves, which take the 32-row
+// tiles of the opposite rows in turn and add their results in wave order at the end.  A wave loads a tile's rows from
+// memory straight into operands of the products along the head, the next tile's while it works, and passes them through LDS
+// of its own for the product that needs them by columns, without a barrier.
+//
+// MFMA 32x32x2: A, B: lane holds row / column lane % 32, index lane / 32 of the pair; D: lane holds column lane % 32,
+// register r holds row 8 * (r / 4) + 4 * (lane / 32) + r % 4.  Score tiles have the own rows as columns, so that register r
+// is, as it stands, the B operand of the next product for the index pair (8 * (r / 4) + r % 4, the same + 4).
+#include "gemm_device.h"
+#include "packed_device.h"
+
+namespace mk {
+namespace {
+
+constexpr int TR = 32;                 // own rows of a block, and rows of a streamed tile
+constexpr float LOG2E = 1.44269504088896340736f;
+__device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }   // 1 unit in the last place; -inf gives 0
+
+template <int D> using Rows4 = float4[D / 8];
+
+// row l32 of the tile from r0 on (rows past `last` are read as `last`): element j of group g is column 8 g + 4 h + j
+template <int D>
+__device__ __forceinline__ void fetch_rows(const float* src, int64_t ld, int r0, int last, int l32, int h, Rows4<D>& f) {
+  const float* p = src + (int64_t)min(r0 + l32, last) * ld + 4 * h;
+#pragma unroll
+  for (int g = 0; g < D / 8; ++g) f[g] = *(const float4*)(p + 8 * g);
+}
+// the same rows as they lie, [row][D + 4], to be read by columns
+template <int D>
+__device__ __forceinline__ void stash(float* tile, int l32, int h, const Rows4<D>& f) {
+#pragma unroll
+  for (int g = 0; g < D / 8; ++g) *(float4*)&tile[l32 * (D + 4) + 8 * g + 4 * h] = f[g];
+}
+__device__ __forceinline__ void clear(f32x16& v) {
+#pragma unroll
+  for (int r = 0; r < 16; ++r) v[r] = 0.f;
+}
+// s = tile rows (A) x own rows (B), which lie in LDS, over the D columns
+template <int D>
+__device__ __forceinline__ void scores(const Rows4<D>& rows, const float* own, int l32, int h, f32x16& s) {
+  clear(s);
+#pragma unroll
+  for (int g = 0; g < D / 8; ++g) {
+    const float4 a = rows[g], b = *(const float4*)&own[l32 * (D + 4) + 8 * g + 4 * h];
+    s = __builtin_amdgcn_mfma_f32_32x32x2f32(a.x, b.x, s, 0, 0, 0);
+    s = __builtin_amdgcn_mfma_f32_32x32x2f32(a.y, b.y, s, 0, 0, 0);
+    s = __builtin_amdgcn_mfma_f32_32x32x2f32(a.z, b.z, s, 0, 0, 0);
+    s = __builtin_amdgcn_mfma_f32_32x32x2f32(a.w, b.w, s, 0, 0, 0);
+  }
+}
+// acc (rows = head columns, columns = own rows) += tile^T x s
+template <int D>
+__device__ __forceinline__ void accumulate(const float* tile, int l32, int h, const f32x16& s, f32x16 (&acc)[D / 32]) {
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    const float* row = &tile[(8 * (r >> 2) + 4 * h + (r & 3)) * (D + 4) + l32];
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(row[32 * db], s[r], acc[db], 0, 0, 0);
+  }
+}
+// What the lanes of a wave have stored to LDS before, the others read after: the hardware keeps a wave's accesses in order,
+// the compiler has to be told.
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+  __builtin_amdgcn_wave_barrier();
+}
+__device__ __forceinline__ float other_half(float v) {
+  const uint32_t u = __float_as_uint(v);
+  const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
+}
+// A wave's part of a sum over the tiles goes into its own part of LDS (TR * (D + 4) floats) ...
+template <int D>
+__device__ __forceinline__ void put_part(float* part, int lane, const f32x16 (&acc)[D / 32]) {
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      *(float4*)&part[((4 * db + g) * 64 + lane) * 4] = make_float4(acc[db][4 * g], acc[db][4 * g + 1], acc[db][4 * g + 2], acc[db][4 * g + 3]);
+}
+// ... and behind a barrier wave w adds the waves' parts of head columns 8 q + 4 h .., q = w, w + W, ..., in wave order,
+// each times a factor of its own.  dst: the lane's row.
+template <int D, int W>
+__device__ __forceinline__ void store_sum(float* dst, const float* parts, int stride, int wave, int lane, const float (&factor)[W]) {
+#pragma unroll
+  for (int i = 0; i < D / 8 / W; ++i) {
+    const int q = wave + W * i;
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      const float4 v = *(const float4*)&parts[w * stride + (q * 64 + lane) * 4];
+      s.x = fmaf(v.x, factor[w], s.x); s.y = fmaf(v.y, factor[w], s.y);
+      s.z = fmaf(v.z, factor[w], s.z); s.w = fmaf(v.w, factor[w], s.w);
+    }
+    if (dst) *(float4*)(dst + 8 * q + 4 * (lane >> 5)) = s;
+  }
+}
+
+template <int D> constexpr int tile_floats() { return TR * (D + 4); }
+
+}  // namespace
+
+// ------------------------------------------------------------------ forward
+template <int D, bool CAUSAL, int W>
+__global__ __launch_bounds__(64 * W) void packed_f32_fwd_kernel(PackedAttention p, int slots) {
+  constexpr int TILE = tile_floats<D>();
+  extern __shared__ __attribute__((aligned(16))) float f_smem[];
+  float* const own = f_smem;                          // [TR][D + 4]
+  float* const stat = own + TILE;                     // [W][2][64]: maxima, sums
+  float* const mine = stat + W * 128;                 // a wave's tile, and its part of the sum afterwards
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, h = lane >> 5;
+  PackedPlace w;
+  if (!packed_place<TR>(p, slots, w)) return;
+  const int qi = w.row + l32, last = w.n - 1;
+  const float c2 = p.scale * LOG2E;
+  const float* kb = (const float*)p.k + w.first * p.ldk + w.kv * D;
+  const float* vb = (const float*)p.v + w.first * p.ldv + w.kv * D;
+  Rows4<D> kf, vf;
+  if (wave == 0) {
+    fetch_rows<D>((const float*)p.q + w.first * p.ldq + w.head * D, p.ldq, w.row, last, l32, h, kf);
+    stash<D>(own, l32, h, kf);
+  }
+  const int kend = CAUSAL ? min(w.n, w.row + TR) : w.n;
+  int k0 = wave * TR;
+  fetch_rows<D>(kb, p.ldk, k0, last, l32, h, kf);
+  fetch_rows<D>(vb, p.ldv, k0, last, l32, h, vf);
+  __syncthreads();
+  f32x16 o[D / 32];
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db) clear(o[db]);
+  float m = -INFINITY, l = 0.f;
+  float* const tile = mine + wave * TILE;
+  for (; k0 < kend; k0 += W * TR) {
+    f32x16 s;
+    scores<D>(kf, own, l32, h, s);
+    wave_sync();
+    stash<D>(tile, l32, h, vf);
+    wave_sync();
+    if (k0 + W * TR < kend) {
+      fetch_rows<D>(kb, p.ldk, k0 + W * TR, last, l32, h, kf);
+      fetch_rows<D>(vb, p.ldv, k0 + W * TR, last, l32, h, vf);
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int key = k0 + 8 * (r >> 2) + 4 * h + (r & 3);
+      if (key >= w.n || (CAUSAL && key > qi)) s[r] = -INFINITY;
+      mx = fmaxf(mx, s[r]);
+    }
+    mx = fmaxf(mx, other_half(mx));
+    const float mnew = fmaxf(m, mx), base = mnew == -INFINITY ? 0.f : mnew;   // a wave's tile may lie behind all that a row sees
+    const float alpha = fast_exp2((m - base) * c2);
+    m = mnew;
+    float rs = 0.f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      s[r] = fast_exp2((s[r] - base) * c2);
+      rs += s[r];
+    }
+    rs += other_half(rs);
+    l = fmaf(l, alpha, rs);
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[db][r] *= alpha;
+    accumulate<D>(tile, l32, h, s, o);
+  }
+  wave_sync();
+  put_part<D>(tile, lane, o);
+  stat[wave * 128 + lane] = m;
+  stat[wave * 128 + 64 + lane] = l;
+  __syncthreads();
+  float top = -INFINITY, total = 0.f, factor[W];
+#pragma unroll
+  for (int i = 0; i < W; ++i) top = fmaxf(top, stat[i * 128 + lane]);
+#pragma unroll
+  for (int i = 0; i < W; ++i) {
+    factor[i] = fast_exp2((stat[i * 128 + lane] - top) * c2);
+    total = fmaf(stat[i * 128 + 64 + lane], factor[i], total);
+  }
+#pragma unroll
+  for (int i = 0; i < W; ++i) factor[i] /= total;
+  const bool real = qi < w.n;
+  store_sum<D, W>(real ? (float*)p.out + (w.first + qi) * p.ldo + w.head * D : nullptr, mine, TILE, wave, lane, factor);
+  if (real && wave == 0 && h == 0) p.lse[(int64_t)w.head * p.T + w.first + qi] = fmaf(top, p.scale, logf(total));
+}
+
+// ------------------------------------------------------------------ dQ
+template <int D, bool CAUSAL, int W>
+__global__ __launch_bounds__(64 * W) void packed_f32_bwd_dq_kernel(PackedAttention p, int slots) {
+  constexpr int TILE = tile_floats<D>();
+  extern __shared__ __attribute__((aligned(16))) float f_smem[];
+  float *const own_q = f_smem, *const own_g = own_q + TILE, *const mine = own_g + TILE;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, h = lane >> 5;
+  PackedPlace w;
+  if (!packed_place<TR>(p, slots, w)) return;
+  const int qi = w.row + l32, last = w.n - 1;
+  const int64_t stats = (int64_t)w.head * p.T + w.first;
+  const float* kb = (const float*)p.k + w.first * p.ldk + w.kv * D;
+  const float* vb = (const float*)p.v + w.first * p.ldv + w.kv * D;
+  Rows4<D> kf, vf;
+  fetch_rows<D>((const float*)p.dout + w.first * p.lddo + w.head * D, p.lddo, w.row, last, l32, h, kf);
+  fetch_rows<D>((const float*)p.out + w.first * p.ldo + w.head * D, p.ldo, w.row, last, l32, h, vf);
+  float delta = 0.f;
+#pragma unroll
+  for (int g = 0; g < D / 8; ++g) {
+    delta = fmaf(kf[g].x, vf[g].x, delta); delta = fmaf(kf[g].y, vf[g].y, delta);
+    delta = fmaf(kf[g].z, vf[g].z, delta); delta = fmaf(kf[g].w, vf[g].w, delta);
+  }
+  delta += other_half(delta);
+  if (wave == 0) {
+    stash<D>(own_g, l32, h, kf);
+    fetch_rows<D>((const float*)p.q + w.first * p.ldq + w.head * D, p.ldq, w.row, last, l32, h, kf);
+    stash<D>(own_q, l32, h, kf);
+    if (h == 0 && qi < w.n) p.delta[stats + qi] = delta;
+  }
+  const float lse = p.lse[stats + min(qi, last)];
+  const int kend = CAUSAL ? min(w.n, w.row + TR) : w.n;
+  int k0 = wave * TR;
+  fetch_rows<D>(kb, p.ldk, k0, last, l32, h, kf);
+  fetch_rows<D>(vb, p.ldv, k0, last, l32, h, vf);
+  __syncthreads();
+  f32x16 dq[D / 32];
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db) clear(dq[db]);
+  float* const tile = mine + wave * TILE;
+  for (; k0 < kend; k0 += W * TR) {
+    f32x16 s, dp;
+    scores<D>(kf, own_q, l32, h, s);
+    wave_sync();
+    stash<D>(tile, l32, h, kf);
+    wave_sync();
+    scores<D>(vf, own_g, l32, h, dp);
+    if (k0 + W * TR < kend) {
+      fetch_rows<D>(kb, p.ldk, k0 + W * TR, last, l32, h, kf);
+      fetch_rows<D>(vb, p.ldv, k0 + W * TR, last, l32, h, vf);
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int key = k0 + 8 * (r >> 2) + 4 * h + (r & 3);
+      const float pr = fast_exp2(fmaf(s[r], p.scale, -lse) * LOG2E);
+      s[r] = key >= w.n || (CAUSAL && key > qi) ? 0.f : pr * (dp[r] - delta);
+    }
+    accumulate<D>(tile, l32, h, s, dq);
+  }
+  wave_sync();
+  put_part<D>(tile, lane, dq);
+  __syncthreads();
+  float factor[W];
+#pragma unroll
+  for (int i = 0; i < W; ++i) factor[i] = p.scale;
+  store_sum<D, W>(qi < w.n ? (float*)p.dq + (w.first + qi) * p.lddq + w.head * D : nullptr, mine, TILE, wave, lane, factor);
+}
+
+// ------------------------------------------------------------------ dK, dV
+template <int D, bool CAUSAL, int W>
+__global__ __launch_bounds__(64 * W) void packed_f32_bwd_dkv_kernel(PackedAttention p, int slots) {
+  constexpr int TILE = tile_floats<D>();
+  extern __shared__ __attribute__((aligned(16))) float f_smem[];
+  float *const own_k = f_smem, *const own_v = own_k + TILE, *const rowstat = own_v + TILE;   // rowstat [W][2][TR]: lse, delta of a tile
+  float *const mine_q = rowstat + W * 2 * TR, *const mine_g = mine_q + W * TILE;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, h = lane >> 5;
+  PackedPlace w;
+  if (!packed_place_kv<TR>(p, slots, CAUSAL, w)) return;
+  const int ki = w.row + l32, last = w.n - 1, group = p.n_heads / p.n_kv_heads;
+  const float* qb = (const float*)p.q + w.first * p.ldq + w.kv * group * D;
+  const float* gb = (const float*)p.dout + w.first * p.lddo + w.kv * group * D;
+  const int64_t stats = (int64_t)w.kv * group * p.T + w.first;
+  Rows4<D> qf, gf;
+  if (wave == 0) {
+    fetch_rows<D>((const float*)p.k + w.first * p.ldk + w.kv * D, p.ldk, w.row, last, l32, h, qf);
+    fetch_rows<D>((const float*)p.v + w.first * p.ldv + w.kv * D, p.ldv, w.row, last, l32, h, gf);
+    stash<D>(own_k, l32, h, qf);
+    stash<D>(own_v, l32, h, gf);
+  }
+  // the tiles of all heads that share these keys, one head after the other; a wave takes every W-th
+  const int qstart = CAUSAL ? w.row : 0, per_head = (w.n - qstart + TR - 1) / TR, tiles = per_head * group;
+  float pre = 0.f;                                    // lse (lanes 0 ..) and delta (lanes 32 ..) of the tile's rows
+  auto fetch = [&](int t) {
+    const int head = t / per_head, q0 = qstart + (t - head * per_head) * TR;
+    fetch_rows<D>(qb + head * D, p.ldq, q0, last, l32, h, qf);
+    fetch_rows<D>(gb + head * D, p.lddo, q0, last, l32, h, gf);
+    pre = (h ? p.delta : p.lse)[stats + (int64_t)head * p.T + min(q0 + l32, last)];
+  };
+  int t = wave;
+  if (t < tiles) fetch(t);
+  __syncthreads();
+  f32x16 dk[D / 32], dv[D / 32];
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db) { clear(dk[db]); clear(dv[db]); }
+  float *const tile_q = mine_q + wave * TILE, *const tile_g = mine_g + wave * TILE, *const st = rowstat + wave * 2 * TR;
+  for (; t < tiles; t += W) {
+    const int q0 = qstart + t % per_head * TR;
+    f32x16 s, dp;
+    scores<D>(qf, own_k, l32, h, s);
+    scores<D>(gf, own_v, l32, h, dp);
+    wave_sync();
+    stash<D>(tile_q, l32, h, qf);
+    stash<D>(tile_g, l32, h, gf);
+    st[lane] = pre;
+    wave_sync();
+    if (t + W < tiles) fetch(t + W);
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const float4 nl = *(const float4*)&st[8 * g + 4 * h], dl = *(const float4*)&st[TR + 8 * g + 4 * h];
+      const float ls[4] = {nl.x, nl.y, nl.z, nl.w}, ds[4] = {dl.x, dl.y, dl.z, dl.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int r = 4 * g + e, q = q0 + 8 * g + 4 * h + e;
+        const float pr = q >= w.n || (CAUSAL && ki > q) ? 0.f : fast_exp2(fmaf(s[r], p.scale, -ls[e]) * LOG2E);
+        s[r] = pr;
+        dp[r] = pr * (dp[r] - ds[e]);
+      }
+    }
+    accumulate<D>(tile_g, l32, h, s, dv);
+    accumulate<D>(tile_q, l32, h, dp, dk);
+  }
+  wave_sync();
+  put_part<D>(tile_q, lane, dk);
+  put_part<D>(tile_g, lane, dv);
+  __syncthreads();
+  float factor[W], one[W];
+#pragma unroll
+  for (int i = 0; i < W; ++i) { factor[i] = p.scale; one[i] = 1.f; }
+  const bool real = ki < w.n;
+  store_sum<D, W>(real ? (float*)p.dk + (w.first + ki) * p.lddk + w.kv * D : nullptr, mine_q, TILE, wave, lane, factor);
+  store_sum<D, W>(real ? (float*)p.dv + (w.first + ki) * p.lddv + w.kv * D : nullptr, mine_g, TILE, wave, lane, one);
+}
+
+namespace {
+template <auto K, int W, int FLOATS>
+void launch(unsigned blocks, const PackedAttention& p, int slots, hipStream_t st) {
+  static const bool configured = [] {
+    (void)hipFuncSetAttribute((const void*)K, hipFuncAttributeMaxDynamicSharedMemorySize, FLOATS * 4);
+    return true;
+  }();
+  (void)configured;
+  hipLaunchKernelGGL(K, dim3(blocks), dim3(64 * W), FLOATS * 4, st, p, slots);
+}
+template <int D, bool CAUSAL>
+void fwd(const PackedAttention& p, hipStream_t st) {
+  constexpr int W = 2, T = tile_floats<D>();
+  const int slots = packed_slots(p.T, p.n_seq, TR);
+  launch<packed_f32_fwd_kernel<D, CAUSAL, W>, W, T + W * 128 + W * T>(packed_blocks(slots, p.n_kv_heads, p.n_heads / p.n_kv_heads), p, slots, st);
+}
+template <int D, bool CAUSAL>
+void bwd(const PackedAttention& p, hipStream_t st) {
+  constexpr int W = 2, T = tile_floats<D>();
+  const int slots = packed_slots(p.T, p.n_seq, TR);
+  launch<packed_f32_bwd_dq_kernel<D, CAUSAL, W>, W, 2 * T + W * T>(packed_blocks(slots, p.n_kv_heads, p.n_heads / p.n_kv_heads), p, slots, st);
+  launch<packed_f32_bwd_dkv_kernel<D, CAUSAL, W>, W, 2 * T + W * 2 * TR + 2 * W * T>(packed_blocks(slots, p.n_kv_heads, 1), p, slots, st);
+}
+}  // namespace
+
+void packed_attention_fwd_bf16(const PackedAttention& p, int d, int causal, hipStream_t st);
+void packed_attention_bwd_bf16(const PackedAttention& p, int d, int causal, hipStream_t st);
+
+bool packed_attention_fits(int64_t T, int64_t n_seq, int64_t n_heads) {
+  return (packed_slots64(T, n_seq, TR) + 8) * n_heads < (int64_t)1 << 23;   // a grid's threads are counted in 32 bits
+}
+
+size_t packed_attention_bwd_workspace_bytes(int64_t T, int n_heads, int n_kv_heads, int d) {
+  (void)n_kv_heads; (void)d;
+  return ((size_t)T * n_heads * sizeof(float) + 255) / 256 * 256;
+}
+
+#define BY_HEAD_(CALL, D, CAUSAL)                                                                       \
+  do {                                                                                                  \
+    if (D == 32) { if (CAUSAL) CALL(32, true); else CALL(32, false); }                                  \
+    else if (D == 64) { if (CAUSAL) CALL(64, true); else CALL(64, false); }                             \
+    else { if (CAUSAL) CALL(128, true); else CALL(128, false); }                                        \
+  } while (0)
+
+void packed_attention_fwd(int dtype, const PackedAttention& p, int d, int causal, hipStream_t st) {
+  if (p.T == 0 || p.n_seq == 0) return;
+  if (dtype == BF16) { packed_attention_fwd_bf16(p, d, causal, st); return; }
+#define FWD_(D_, C_) fwd<D_, C_>(p, st)
+  BY_HEAD_(FWD_, d, causal);
+#undef FWD_
+}
+
+void packed_attention_bwd(int dtype, PackedAttention p, int d, int causal, void* workspace, hipStream_t st) {
+  if (p.T == 0 || p.n_seq == 0) return;
+  p.delta = (float*)workspace;
+  if (dtype == BF16) { packed_attention_bwd_bf16(p, d, causal, st); return; }
+#define BWD_(D_, C_) bwd<D_, C_>(p, st)
+  BY_HEAD_(BWD_, d, causal);
+#undef BWD_
+}
+
+}  // namespace mk
