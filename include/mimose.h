@@ -535,6 +535,42 @@ int mimose_op_adamw_table(const mimose_adamw_tensor* tensors, int32_t count, int
                           void* device, uint64_t bytes, mimose_adamw_table* out, void* stream);
 int mimose_op_adamw_step(const mimose_adamw_table* table, const mimose_adamw_cfg* cfg, int64_t step,
                          void* stream);
+/*
+ * Update of many matrices with orthogonalised steps (Muon) for a caller's own tensors.  Per matrix [rows, cols], row-major: fp32
+ * master values, fp32 gradient, fp32 momentum, optionally a bf16 copy that receives the master rounded to nearest-even.
+ *     momentum <- cfg.momentum * momentum + grad,   u = grad + cfg.momentum * momentum (nesterov) or momentum
+ *     X = u / (|u| + eps), |u| the root of the sum of squares;   cfg.iterations times X <- a X + b A X + c A A X with A = X X^T
+ *         (A = X^T X from the right where rows > cols; a, b, c = 3.4445, -4.7750, 2.0315)
+ *     master <- master - lr (rms sqrt(max(rows, cols)) X + weight_decay master)
+ * so that a step's elements are about lr rms large.  X, A and b A + c A A are held in fp16 (times 2^10) between products, sums in fp32:
+ * X is 0.1 to 0.7 % off the exact one (2-norm), most where its singular values reach over orders of magnitude.  All zeros is the
+ * initial momentum.  Pointers 16-byte aligned; sides up to 2^20; a matrix may be empty; no matrix may share memory that is written
+ * with another.
+ * mimose_op_muon_table lays a list out in device memory of mimose_op_muon_table_bytes (0: the list is refused) and waits for the
+ * copy; the table holds the addresses, not the tensors.  A step works on the matrices in parts, in the list's order, one after the
+ * other in one scratch: the fewer, the fuller the device, the more, the smaller the scratch (parts: at most so many, 1 to 64; about
+ * 8 bytes for each element of the largest part).  mimose_op_muon_step needs 16-byte aligned scratch of table->workspace_bytes,
+ * whose content it neither needs nor keeps.
+ */
+typedef struct {
+  float* master; void* lowp; const float* grad; float* momentum;
+  int32_t rows, cols;
+} mimose_muon_matrix;
+typedef struct {
+  float lr, momentum, weight_decay, rms, eps;
+  int32_t nesterov, iterations;
+} mimose_muon_cfg;
+typedef struct {                                      /* plain data, filled by mimose_op_muon_table */
+  void* device;
+  uint64_t workspace_bytes;
+  int32_t matrices, parts;
+  int32_t chunks[64], tri[64], full[64];              /* units of work up to each part's end */
+} mimose_muon_table;
+uint64_t mimose_op_muon_table_bytes(const mimose_muon_matrix* matrices, int32_t count, int32_t parts);
+int mimose_op_muon_table(const mimose_muon_matrix* matrices, int32_t count, int32_t parts, void* device,
+                         uint64_t bytes, mimose_muon_table* out, void* stream);
+int mimose_op_muon_step(const mimose_muon_table* table, const mimose_muon_cfg* cfg, void* workspace,
+                        uint64_t workspace_bytes, void* stream);
 /* sum_out (may be NULL when has_ln = 0) = tok_emb[id] + pos_emb[pos]; y = LN(sum) or sum. */
 int mimose_op_embed_fwd(int32_t dtype, const int32_t* ids, const void* tok_emb, const void* pos_emb,
                         const void* gamma, const void* beta, void* sum_out, void* y, int32_t B,

@@ -66,6 +66,20 @@ class mimose_adamw_table(C.Structure):
     _fields_ = [("device", C.c_void_p)] + [(n, C.c_int32) for n in ("tensors", "chunks", "state_bits", "reserved_")]
 
 
+class mimose_muon_matrix(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("master", "lowp", "grad", "momentum")] + [(n, C.c_int32) for n in ("rows", "cols")]
+
+
+class mimose_muon_cfg(C.Structure):
+    _fields_ = [(n, C.c_float) for n in ("lr", "momentum", "weight_decay", "rms", "eps")] + \
+               [(n, C.c_int32) for n in ("nesterov", "iterations")]
+
+
+class mimose_muon_table(C.Structure):
+    _fields_ = [("device", C.c_void_p), ("workspace_bytes", C.c_uint64)] + [(n, C.c_int32) for n in ("matrices", "parts")] + \
+               [(n, C.c_int32 * 64) for n in ("chunks", "tri", "full")]
+
+
 class MimoseError(RuntimeError):
     def __init__(self, code: int, msg: str):
         super().__init__(f"libmimose: {ERR_NAMES.get(code, code)}: {msg}")
@@ -146,6 +160,9 @@ SIGNATURES = {
     "mimose_op_adamw_table_bytes": (_u64, [_vp, _i32, _i32]),
     "mimose_op_adamw_table": (C.c_int, [_vp, _i32, _i32, _vp, _u64, C.POINTER(mimose_adamw_table), _vp]),
     "mimose_op_adamw_step": (C.c_int, [C.POINTER(mimose_adamw_table), C.POINTER(mimose_adamw_cfg), _i64, _vp]),
+    "mimose_op_muon_table_bytes": (_u64, [_vp, _i32, _i32]),
+    "mimose_op_muon_table": (C.c_int, [_vp, _i32, _i32, _vp, _u64, C.POINTER(mimose_muon_table), _vp]),
+    "mimose_op_muon_step": (C.c_int, [C.POINTER(mimose_muon_table), C.POINTER(mimose_muon_cfg), _vp, _u64, _vp]),
     "mimose_op_embed_fwd": (C.c_int, [_i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _f32, _i32, _vp]),
     "mimose_op_embed_bwd": (C.c_int, [_i32, _vp, _vp, _vp, _vp, _i32, _vp, _vp, _i32, _i32, _i32, _i32, _vp]),
 }
@@ -568,6 +585,30 @@ def mimose_op_adamw_step(table, step, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8,
     _check(load_library().mimose_op_adamw_step(C.byref(getattr(table, "table", table)), C.byref(cfg), step, _ptr(stream)))
 
 
+def mimose_op_muon_table_bytes(matrices, parts: int) -> int:
+    """matrices: a ctypes array of mimose_muon_matrix; raises where the library refuses the list."""
+    n = load_library().mimose_op_muon_table_bytes(matrices, len(matrices), parts)
+    if not n:
+        _check(MIMOSE_ERR_INVALID_ARG)
+    return n
+
+
+def mimose_op_muon_table(matrices, parts: int, device, nbytes: int, stream=None) -> mimose_muon_table:
+    out = mimose_muon_table()
+    _check(load_library().mimose_op_muon_table(matrices, len(matrices), parts, _ptr(device), nbytes, C.byref(out), _ptr(stream)))
+    return out
+
+
+def mimose_op_muon_step(table, lr=1e-3, momentum=0.95, weight_decay=0.01, rms=0.2, eps=1e-7, nesterov=1, iterations=5, workspace=None,
+                        workspace_bytes=0, stream=None):
+    """table: a mimose_muon_table, or the MuonTable that owns one and, where none is given, a workspace."""
+    if workspace is None and isinstance(table, MuonTable):
+        workspace, workspace_bytes = table.workspace, table.workspace.numel()
+    cfg = mimose_muon_cfg(lr, momentum, weight_decay, rms, eps, nesterov, iterations)
+    _check(load_library().mimose_op_muon_step(C.byref(getattr(table, "table", table)), C.byref(cfg), _ptr(workspace), workspace_bytes,
+                                              _ptr(stream)))
+
+
 def mimose_op_embed_fwd(dtype, ids, tok, pos, gamma, beta, sum_out, y, B, L, H, eps, has_ln, stream=None):
     _check(load_library().mimose_op_embed_fwd(dtype, _ptr(ids), _ptr(tok), _ptr(pos), _ptr(gamma), _ptr(beta),
                                               _ptr(sum_out), _ptr(y), B, L, H, eps, has_ln, _ptr(stream)))
@@ -620,6 +661,43 @@ class AdamWTable:
         with torch.cuda.stream(owner):
             self.memory = torch.empty(nbytes, dtype=torch.uint8, device=device)
             self.table = mimose_op_adamw_table(entries, state_bits, self.memory, nbytes, stream)
+
+
+class MuonTable:
+    """The device table and the scratch of a list of matrices, for mimose_op_muon_step; keeps the tensors alive.
+
+    matrices: dicts of contiguous tensors [rows, cols] of one device, master, grad, momentum (fp32) and lowp (bf16 or None).
+    parts: a step works on the list in at most so many parts, in a scratch that is that much smaller (about 8 bytes for each element
+    of the largest part).  stream (an address; None: torch's current one) is the one that steps run on; a step on another has to have
+    ended before the table is let go, and two steps that run at once need a workspace each.  Like AdamWTable it holds addresses:
+    gradients have to be written in place."""
+
+    def __init__(self, matrices, parts: int = 1, stream=None):
+        import torch
+        self.matrices = [dict(t) for t in matrices]
+        entries = (mimose_muon_matrix * len(self.matrices))()
+        device = self.matrices[0]["master"].device if self.matrices else None
+        for e, t in zip(entries, self.matrices):
+            shape = t["master"].shape
+            if len(shape) != 2:
+                raise ValueError("master: a matrix [rows, cols] is required")
+            for name, dtype in (("master", torch.float32), ("grad", torch.float32), ("momentum", torch.float32), ("lowp", torch.bfloat16)):
+                x = t.get(name)
+                if x is None and name == "lowp":
+                    continue
+                if x is None or x.shape != shape or x.dtype != dtype or not x.is_contiguous() or not x.is_cuda or x.device != device:
+                    raise ValueError(f"{name}: a contiguous tensor of shape {tuple(shape)} of {dtype} on the list's one device is required")
+                setattr(e, name, x.data_ptr() or None)
+            e.rows, e.cols = shape
+        nbytes = mimose_op_muon_table_bytes(entries, parts)
+        if stream is None:
+            stream = torch.cuda.current_stream(device).cuda_stream
+        # memory of that stream's own: other streams' may still be in use by what was queued there
+        owner = torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)
+        with torch.cuda.stream(owner):
+            self.memory = torch.empty(nbytes, dtype=torch.uint8, device=device)
+            self.table = mimose_op_muon_table(entries, parts, self.memory, nbytes, stream)
+            self.workspace = torch.empty(self.table.workspace_bytes, dtype=torch.uint8, device=device)
 
 
 class Mimose:
@@ -725,4 +803,4 @@ class Mimose:
 
 
 __all__ = [n for n in dir() if n.startswith("mimose_") or n.startswith("MIMOSE_") or n.startswith("Q_")] + \
-          ["Mimose", "AdamWTable", "MimoseError", "make_cfg", "load_library", "LIB_PATH", "SIGNATURES", "ERR_NAMES", "KERNEL_CLASSES", "PLAN_MODES", "COLLECTORS"]
+          ["Mimose", "AdamWTable", "MuonTable", "MimoseError", "make_cfg", "load_library", "LIB_PATH", "SIGNATURES", "ERR_NAMES", "KERNEL_CLASSES", "PLAN_MODES", "COLLECTORS"]

@@ -1,13 +1,16 @@
 // C ABI of the kernel-level entry points: argument checks, then the launcher.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdio>
+#include <cstring>
 #include <new>
 #include <vector>
 
 #include "../../include/mimose.h"
 #include "kernels.h"
+#include "muon.h"
 
 // sets what mimose_last_error(NULL) returns on this thread (mimose.cpp)
 void mimose_set_thread_error(const char* msg);
@@ -394,6 +397,185 @@ int mimose_op_adamw_step(const mimose_adamw_table* table, const mimose_adamw_cfg
   const mk::AdamChunk* chunks = (const mk::AdamChunk*)((const char*)table->device + adamw_entries_bytes(table->tensors, table->state_bits));
   if (table->state_bits == 8) mk::adamw8_update((const mk::Adam8Tensor*)table->device, chunks, table->chunks, h, step, (hipStream_t)stream);
   else mk::adamw_update(mk::BF16, (const mk::AdamTensor*)table->device, chunks, table->chunks, h, (hipStream_t)stream);
+  return done();
+}
+
+// A list of matrices laid out: entries, units of work and scratch.  why: null, or what is wrong with the list.
+struct MuonPlan {
+  std::vector<mk::MuonMatrix> mats;
+  std::vector<mk::MuonChunk> chunks;
+  std::vector<mk::MuonTile> tri, full;
+  mimose_muon_table table = {};
+  const char* why = nullptr;
+  uint64_t bytes() const {
+    return std::max<size_t>(16, mats.size() * sizeof(mk::MuonMatrix) + chunks.size() * sizeof(mk::MuonChunk) + (tri.size() + full.size()) * sizeof(mk::MuonTile));
+  }
+};
+static int64_t muon_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
+static int64_t muon_chunk(int64_t n) { return std::max<int64_t>(16384, muon_up((n + 1023) / 1024, 4096)); }   // at most 1024 sums of a matrix
+static int64_t muon_scratch(int64_t rows, int64_t cols) {
+  if (rows < 1 || cols < 1) return 0;
+  const int64_t mp = muon_up(std::min(rows, cols), mk::kMuonTile), np = muon_up(std::max(rows, cols), mk::kMuonTile), n = rows * cols;
+  return 4 * mp * np + 4 * mp * mp + muon_up((n + muon_chunk(n) - 1) / muon_chunk(n) * 8, 256);
+}
+static const char* bad_muon_list(const mimose_muon_matrix* t, int32_t count, int32_t parts) {
+  if (!t || count < 1) return "at least one matrix required";
+  if (parts < 1 || parts > 64) return "1 to 64 parts required";
+  struct Range { uintptr_t from, to; bool written; };
+  std::vector<Range> all;
+  int64_t chunks = 0, tiles = 0;
+  for (int32_t i = 0; i < count; ++i) {
+    if (t[i].rows < 0 || t[i].cols < 0 || t[i].rows > mk::kMuonSide || t[i].cols > mk::kMuonSide) return "a matrix has a side below 0 or above 2^20";
+    const int64_t n = (int64_t)t[i].rows * t[i].cols;
+    if (n == 0) continue;
+    if (!t[i].master || !t[i].grad || !t[i].momentum) return "master, grad and momentum of a matrix must be given";
+    if (((uintptr_t)t[i].master | (uintptr_t)t[i].grad | (uintptr_t)t[i].momentum | (uintptr_t)t[i].lowp) & 15)
+      return "master, lowp, grad and momentum of a matrix must be 16-byte aligned";
+    const uintptr_t f = (uintptr_t)n * 4;
+    all.push_back({(uintptr_t)t[i].master, (uintptr_t)t[i].master + f, true});
+    all.push_back({(uintptr_t)t[i].momentum, (uintptr_t)t[i].momentum + f, true});
+    all.push_back({(uintptr_t)t[i].grad, (uintptr_t)t[i].grad + f, false});
+    if (t[i].lowp) all.push_back({(uintptr_t)t[i].lowp, (uintptr_t)t[i].lowp + f / 2, true});
+    chunks += (n + muon_chunk(n) - 1) / muon_chunk(n);
+    tiles += muon_up(t[i].rows, mk::kMuonTile) / mk::kMuonTile * (muon_up(t[i].cols, mk::kMuonTile) / mk::kMuonTile);
+    if (chunks >= (1 << 22) || tiles >= (1 << 22)) return "too many elements: 2^36 at most";   // a grid's threads are counted in 32 bits
+  }
+  std::sort(all.begin(), all.end(), [](const Range& a, const Range& b) { return a.from < b.from; });
+  uintptr_t end = 0, end_written = 0;
+  for (const Range& r : all) {
+    if (r.from < (r.written ? end : end_written)) return "memory that is written belongs to two matrices, or to two of a matrix' tensors";
+    end = std::max(end, r.to);
+    if (r.written) end_written = std::max(end_written, r.to);
+  }
+  return nullptr;
+}
+static MuonPlan muon_plan(const mimose_muon_matrix* t, int32_t count, int32_t parts) {
+  MuonPlan p;
+  if ((p.why = bad_muon_list(t, count, parts))) return p;
+  // the smallest scratch that takes the list in so many parts, in its order
+  auto parts_of = [&](int64_t room) {
+    int k = 1;
+    int64_t used = 0;
+    for (int32_t i = 0; i < count; ++i) {
+      const int64_t s = muon_scratch(t[i].rows, t[i].cols);
+      if (used + s > room) { ++k; used = 0; }
+      used += s;
+    }
+    return k;
+  };
+  int64_t low = 0, high = 0;
+  for (int32_t i = 0; i < count; ++i) {
+    const int64_t s = muon_scratch(t[i].rows, t[i].cols);
+    low = std::max(low, s);
+    high += s;
+  }
+  while (low < high) {
+    const int64_t mid = low + (high - low) / 2;
+    if (parts_of(mid) <= parts) high = mid; else low = mid + 1;
+  }
+  mimose_muon_table& out = p.table;
+  out.workspace_bytes = std::max<uint64_t>(16, (uint64_t)high);
+  out.matrices = count;
+  int part = 0;
+  int64_t used = 0;
+  auto close = [&]() {
+    out.chunks[part] = (int32_t)p.chunks.size();
+    out.tri[part] = (int32_t)p.tri.size();
+    out.full[part] = (int32_t)p.full.size();
+  };
+  for (int32_t i = 0; i < count; ++i) {
+    const int64_t rows = t[i].rows, cols = t[i].cols, n = rows * cols, s = muon_scratch(rows, cols);
+    if (used + s > high) { close(); ++part; used = 0; }
+    mk::MuonMatrix m = {t[i].master, (uint16_t*)t[i].lowp, t[i].grad, t[i].momentum};
+    m.rows = (int32_t)rows;
+    m.cols = (int32_t)cols;
+    m.chunk = muon_chunk(n);
+    if (n > 0) {
+      m.mp = (int32_t)muon_up(std::min(rows, cols), mk::kMuonTile);
+      m.np = (int32_t)muon_up(std::max(rows, cols), mk::kMuonTile);
+      const int64_t x = 2 * (int64_t)m.mp * m.np, a = 2 * (int64_t)m.mp * m.mp;
+      m.x[0] = (uint64_t)used; m.x[1] = m.x[0] + x; m.a = m.x[1] + x; m.b = m.a + a; m.partial = m.b + a;
+      for (int64_t c = 0; c < n; c += m.chunk) p.chunks.push_back({i, 0, c});
+      const int mt = m.mp / mk::kMuonTile, nt = m.np / mk::kMuonTile;
+      for (int a0 = 0; a0 < mt; ++a0) {
+        for (int b0 = a0; b0 < mt; ++b0) p.tri.push_back({i, (uint16_t)a0, (uint16_t)b0});
+        for (int b0 = 0; b0 < nt; ++b0) p.full.push_back({i, (uint16_t)a0, (uint16_t)b0});
+      }
+    }
+    used += s;
+    p.mats.push_back(m);
+  }
+  close();
+  out.parts = part + 1;
+  return p;
+}
+
+uint64_t mimose_op_muon_table_bytes(const mimose_muon_matrix* matrices, int32_t count, int32_t parts) {
+  const char* const op = "mimose_op_muon_table_bytes";
+  try {
+    const MuonPlan p = muon_plan(matrices, count, parts);
+    if (p.why) { refuse(op, p.why); return 0; }
+    return p.bytes();
+  } catch (const std::bad_alloc&) {
+    refuse(op, "no host memory for the table");
+    return 0;
+  }
+}
+
+int mimose_op_muon_table(const mimose_muon_matrix* matrices, int32_t count, int32_t parts, void* device, uint64_t bytes,
+                         mimose_muon_table* out, void* stream) {
+  const char* const op = "mimose_op_muon_table";
+  try {
+    MuonPlan p = muon_plan(matrices, count, parts);
+    if (p.why) return refuse(op, p.why);
+    if (!out || !device || ((uintptr_t)device & 15) || bytes < p.bytes())
+      return refuse(op, "out and 16-byte aligned device memory of mimose_op_muon_table_bytes must be given");
+    std::vector<char> host(p.bytes(), 0);
+    char* to = host.data();
+    auto put = [&](const void* from, size_t n) { if (n) memcpy(to, from, n); to += n; };
+    put(p.mats.data(), p.mats.size() * sizeof(mk::MuonMatrix));
+    put(p.chunks.data(), p.chunks.size() * sizeof(mk::MuonChunk));
+    put(p.tri.data(), p.tri.size() * sizeof(mk::MuonTile));
+    put(p.full.data(), p.full.size() * sizeof(mk::MuonTile));
+    if (hipMemcpyAsync(device, host.data(), host.size(), hipMemcpyHostToDevice, (hipStream_t)stream) != hipSuccess ||
+        hipStreamSynchronize((hipStream_t)stream) != hipSuccess) {
+      (void)hipGetLastError();
+      mimose_set_thread_error("mimose_op_muon_table: copy to the device failed");
+      return MIMOSE_ERR_HIP;
+    }
+    *out = p.table;
+    out->device = device;
+  } catch (const std::bad_alloc&) {
+    return refuse(op, "no host memory for the table");
+  }
+  return MIMOSE_OK;
+}
+
+int mimose_op_muon_step(const mimose_muon_table* table, const mimose_muon_cfg* cfg, void* workspace, uint64_t workspace_bytes, void* stream) {
+  const char* const op = "mimose_op_muon_step";
+  if (!table || !table->device || table->matrices < 1 || table->parts < 1 || table->parts > 64 || !cfg)
+    return refuse(op, "a table of mimose_op_muon_table and cfg must be given");
+  int last[3] = {0, 0, 0};
+  for (int i = 0; i < table->parts; ++i) {
+    const int now[3] = {table->chunks[i], table->tri[i], table->full[i]};
+    for (int k = 0; k < 3; ++k) {
+      if (now[k] < last[k] || now[k] >= (1 << 23)) return refuse(op, "a table of mimose_op_muon_table and cfg must be given");
+      last[k] = now[k];
+    }
+  }
+  if (const char* why = mk::bad_muon(cfg->lr, cfg->momentum, cfg->weight_decay, cfg->rms, cfg->eps, cfg->iterations)) return refuse(op, why);
+  if (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < table->workspace_bytes)
+    return refuse(op, "workspace must be 16-byte aligned and of table->workspace_bytes");
+  const mk::MuonMatrix* mats = (const mk::MuonMatrix*)table->device;
+  const mk::MuonChunk* chunks = (const mk::MuonChunk*)(mats + table->matrices);
+  const mk::MuonTile *tri = (const mk::MuonTile*)(chunks + last[0]), *full = tri + last[1];
+  const mk::MuonHyper h = {cfg->lr, cfg->momentum, cfg->weight_decay, cfg->rms, cfg->eps, cfg->nesterov != 0, cfg->iterations};
+  int c0 = 0, t0 = 0, f0 = 0;
+  for (int i = 0; i < table->parts; ++i) {
+    mk::muon_update(mats, chunks + c0, table->chunks[i] - c0, tri + t0, table->tri[i] - t0, full + f0, table->full[i] - f0, workspace, h,
+                    (hipStream_t)stream);
+    c0 = table->chunks[i]; t0 = table->tri[i]; f0 = table->full[i];
+  }
   return done();
 }
 
