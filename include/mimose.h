@@ -563,8 +563,8 @@ typedef struct {
 typedef struct {                                      /* plain data, filled by mimose_op_muon_table */
   void* device;
   uint64_t workspace_bytes;
-  int32_t matrices, parts;
-  int32_t chunks[64], tri[64], full[64];              /* units of work up to each part's end */
+  int32_t matrices, parts, small, reserved_;
+  int32_t units[7][64];                               /* units of work up to each part's end */
 } mimose_muon_table;
 uint64_t mimose_op_muon_table_bytes(const mimose_muon_matrix* matrices, int32_t count, int32_t parts);
 int mimose_op_muon_table(const mimose_muon_matrix* matrices, int32_t count, int32_t parts, void* device,

@@ -35,7 +35,7 @@ def orthogonalise(u, eps, iterations):
     for k in reversed(range(iterations)):
         s, p, X = values[k], values[k + 1], xs[k]
         A = X @ X.T
-        B = b * A + c * A @ A
+        B = a * np.eye(m) + b * A + c * A @ A                            # what is held of the factor
         i, j = s[:, None], s[None, :]
         for noise, part in ((F16_NOISE * (B ** 2).sum(), j + 0 * i), (F16_NOISE * (A ** 2).sum(), (b + c * (i * i + j * j)) * j)):
             sym, anti = (part + part.T) / 2, (part - part.T) / 2         # of symmetric noise times X

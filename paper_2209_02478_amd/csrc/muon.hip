@@ -8,109 +8,176 @@
 // is above 1.21, 1.47 and 11.  The products' operands are therefore held in fp16 times 2^10: as many bits as any 16-bit type has
 // (values from 6e-8 of the largest on keep all eleven; bf16 keeps eight, and the step is then 1 to 5 % off instead of 0.1 to
 // 0.6), at the same rate of the matrix units.  Sums are fp32, the norm's fp64 (squares of gradients of 1e-20 are numbers there).
-// A and A A are symmetric: only tiles on and above the diagonal are multiplied, and stored twice.
-#include "gemm_large.h"
-#include "muon.h"
+// A and A A are symmetric: only tiles on and above the diagonal are multiplied, and stored twice.  What is held of an iteration's
+// factor is B = a I + b A + c A A, so that X' = B X: a X beside the product would be read again, and the error is the same
+// (0.13 and 0.64 % either way for gradients of 768 x 768 from a normal distribution and with few large directions).
+#include "muon_device.h"
 
 namespace mk {
+
+using namespace muon;
+
 namespace {
 
-typedef _Float16 f16;
-typedef f16 f16x4 __attribute__((ext_vector_type(4)));
-typedef f16 f16x8 __attribute__((ext_vector_type(8)));
-using large::f32x4;
-
-constexpr float kHeld = 1024.f, kBack = 1.f / 1024.f;        // operands are held times 2^10
-constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
-constexpr int BK = 64;
-
-__device__ __forceinline__ f16* in_scratch(char* ws, uint64_t at) { return (f16*)(ws + at); }
-
-// sum over the block's 256 threads, in every one of them; the order is fixed
+// sum over the block's waves, in every thread; the order is fixed
+template <int WAVES>
 __device__ __forceinline__ double block_sum(double v, double* lds) {
-  const int tid = threadIdx.x;
-  lds[tid] = v;
+#pragma unroll
+  for (int s = 32; s > 0; s >>= 1) v += __shfl_xor(v, s);
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
   __syncthreads();
-  for (int s = 128; s > 0; s >>= 1) {
-    if (tid < s) lds[tid] += lds[tid + s];
-    __syncthreads();
-  }
-  return lds[0];
+  v = 0.0;
+#pragma unroll
+  for (int i = 0; i < WAVES; ++i) v += lds[i];
+  return v;
 }
+
+// four elements of a row, which may begin at any of them
+typedef float f32x4_at4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t u32x2_at2 __attribute__((ext_vector_type(2), aligned(2)));
+__device__ __forceinline__ f32x4 load_row4(const float* row, int c, int cols) {
+  if (c + 4 <= cols) return *(const f32x4_at4*)(row + c);
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int e = 0; e < 3; ++e)
+    if (c + e < cols) v[e] = row[c + e];
+  return v;
+}
+// the same where rows are asked for together: no branch between the loads.  whole: the four elements exist in every lane
+__device__ __forceinline__ f32x4 load_edge4(const float* row, int c, int cols, bool whole) {
+  if (whole) return *(const f32x4_at4*)(row + c);
+  f32x4 v;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float x = row[min(c + e, cols - 1)];
+    v[e] = c + e < cols ? x : 0.f;
+  }
+  return v;
+}
+__device__ __forceinline__ void store_row4(float* row, uint16_t* low, int c, int cols, const f32x4& v) {
+  if (c + 4 <= cols) {
+    *(f32x4_at4*)(row + c) = v;
+    if (low) *(u32x2_at2*)(low + c) = u32x2_at2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 3; ++e)
+    if (c + e < cols) {
+      row[c + e] = v[e];
+      if (low) low[c + e] = f32_to_bf16(v[e]);
+    }
+}
+// the weights' step, of four elements
+__device__ __forceinline__ f32x4 stepped(const MuonHyper& h, const f32x4& w, const f32x4& x, float step) {
+  f32x4 n;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) n[e] = w[e] - h.lr * fmaf(h.weight_decay, w[e], step * x[e]);
+  return n;
+}
+__device__ __forceinline__ f32x4 direction(const MuonHyper& h, const f32x4& g, const f32x4& m) {
+  f32x4 u;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) u[e] = h.nesterov ? fmaf(h.momentum, m[e], g[e]) : m[e];
+  return u;
+}
+__device__ __forceinline__ float step_size(const MuonMatrix& t, const MuonHyper& h) { return h.rms * sqrtf((float)max(t.rows, t.cols)) * kBack; }
+
+// A tile that is turned passes through LDS in pieces of four elements: piece p of row i lies at p ^ (i / 4), so that 32 lanes that
+// write one piece of rows four apart, or read one row's pieces, meet all banks once.
+__device__ __forceinline__ int turn_at(int row, int piece) { return row * kMuonTile + ((piece ^ ((row >> 2) & 31)) << 2); }
 
 }  // namespace
 
 // Momentum, and each chunk's sum of u^2.
 __global__ __launch_bounds__(256) void muon_momentum_kernel(const MuonMatrix* mats, const MuonChunk* chunks, char* ws, MuonHyper h) {
-  __shared__ double lds[256];
+  __shared__ double lds[4];
   const MuonChunk c = chunks[blockIdx.x];
   const MuonMatrix& t = mats[c.matrix];
-  const int64_t n = (int64_t)t.rows * t.cols, end = min(n, c.start + t.chunk);
-  const float* g = t.grad;
-  float* m = t.momentum;
+  const int64_t chunk = t.chunk, n = min((int64_t)t.rows * t.cols - c.start, chunk);
+  const float* g = t.grad + c.start;                         // chunks begin on multiples of 4, tensors on 16 bytes
+  float* m = t.momentum + c.start;
   double sum = 0.0;
-  auto one = [&](float gi, float mi, float& out) {
-    out = fmaf(h.momentum, mi, gi);
-    const float u = h.nesterov ? fmaf(h.momentum, out, gi) : out;
-    sum += (double)u * u;
+  auto four = [&](int64_t i, const f32x4& gv, f32x4 mv) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) mv[e] = fmaf(h.momentum, mv[e], gv[e]);
+    *(f32x4*)(m + i) = mv;
+    const f32x4 u = direction(h, gv, mv);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum += (double)u[e] * u[e];
   };
-  int64_t i = c.start + 4 * threadIdx.x;                     // chunks begin on multiples of 4, tensors on 16 bytes
-  for (; i + 4 <= end; i += 1024) {
-    const float4 gv = *(const float4*)(g + i), mv = *(const float4*)(m + i);
-    float4 o;
-    one(gv.x, mv.x, o.x); one(gv.y, mv.y, o.y); one(gv.z, mv.z, o.z); one(gv.w, mv.w, o.w);
-    *(float4*)(m + i) = o;
+  int64_t i = 4 * threadIdx.x;
+  for (; i + 3 * 1024 + 4 <= n; i += 4 * 1024) {
+    f32x4 gv[4], mv[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      gv[q] = *(const f32x4*)(g + i + q * 1024);
+      mv[q] = *(const f32x4*)(m + i + q * 1024);
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) four(i + q * 1024, gv[q], mv[q]);
   }
-  for (int64_t j = i; j < end && j < i + 4; ++j) {
-    float o;
-    one(g[j], m[j], o);
+  for (; i + 4 <= n; i += 1024) four(i, *(const f32x4*)(g + i), *(const f32x4*)(m + i));
+  for (int64_t j = i; j < n && j < i + 4; ++j) {
+    const float o = fmaf(h.momentum, m[j], g[j]), u = h.nesterov ? fmaf(h.momentum, o, g[j]) : o;
     m[j] = o;
+    sum += (double)u * u;
   }
-  sum = block_sum(sum, lds);
-  if (threadIdx.x == 0) ((double*)(ws + t.partial))[c.start / t.chunk] = sum;
+  sum = block_sum<4>(sum, lds);
+  if (threadIdx.x == 0) ((double*)(ws + t.partial))[c.start / chunk] = sum;
 }
 
-// X = u / (|u| + eps), 128 x 128 of it a block, zeros behind the matrix' last row and column.
+// X = u / (|u| + eps), 128 x 128 of it a block, zeros behind the matrix' last row and column.  A thread takes 4 x 4 elements at a
+// time, eight loads in flight, and turns them in registers where X is the matrix turned.
 __global__ __launch_bounds__(256) void muon_start_kernel(const MuonMatrix* mats, const MuonTile* tiles, char* ws, MuonHyper h) {
-  __shared__ double lds[256];
-  __shared__ f16 turn[32][kMuonTile + 2];
+  __shared__ double lds[4];
+  __shared__ __attribute__((aligned(16))) f16 turn[kMuonTile * kMuonTile];
   const MuonTile tile = tiles[blockIdx.x];
   const MuonMatrix& t = mats[tile.matrix];
-  const int64_t n = (int64_t)t.rows * t.cols;
-  const int parts = (int)((n + t.chunk - 1) / t.chunk), tid = threadIdx.x;
+  const int rows = t.rows, cols = t.cols, np = t.np, tid = threadIdx.x;
+  const int64_t n = (int64_t)rows * cols;
+  const int parts = (int)((n + t.chunk - 1) / t.chunk);
   double sum = 0.0;
   for (int i = tid; i < parts; i += 256) sum += ((const double*)(ws + t.partial))[i];
-  const double norm = sqrt(block_sum(sum, lds)) + (double)h.eps;
-  const float inv = (float)((double)kHeld / norm);           // (eps above 0: finite)
-  const bool tall = t.rows > t.cols;
-  f16* x = in_scratch(ws, t.x[0]) + (int64_t)tile.i * kMuonTile * t.np + (int64_t)tile.j * kMuonTile;
-  auto u = [&](int64_t at) {
-    const float g = t.grad[at], m = t.momentum[at];
-    return (h.nesterov ? fmaf(h.momentum, m, g) : m) * inv;
-  };
-  const int col = tid & 127, row0 = tid >> 7;
-  if (!tall) {
-    const int c = tile.j * kMuonTile + col;
-    for (int r = row0; r < kMuonTile; r += 2) {
-      const int row = tile.i * kMuonTile + r;
-      x[(int64_t)r * t.np + col] = row < t.rows && c < t.cols ? (f16)u((int64_t)row * t.cols + c) : (f16)0.f;
+  const double norm = sqrt(block_sum<4>(sum, lds)) + (double)h.eps;
+  const float inv = (float)((double)kHeld / norm);           // (eps is 1e-30 or more: finite)
+  const bool tall = rows > cols;
+  f16* x = in_scratch(ws, t.x[0]) + (int64_t)tile.i * kMuonTile * np + (int64_t)tile.j * kMuonTile;
+  const int r0 = (tall ? tile.j : tile.i) * kMuonTile, c = (tid & 31) * 4, at = (tall ? tile.i : tile.j) * kMuonTile + c;   // of u
+  const float *const grad = t.grad, *const mom = t.momentum;
+  const bool whole = at - c + kMuonTile <= cols;
+  for (int k = 0; k < 4; ++k) {
+    const int r = k * 32 + (tid >> 5) * 4;
+    f32x4 g[4], m[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int64_t row = (int64_t)min(r0 + r + q, rows - 1) * cols;
+      g[q] = load_edge4(grad + row, at, cols, whole);
+      m[q] = load_edge4(mom + row, at, cols, whole);
     }
-    return;
+    f16 o[4][4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const f32x4 u = direction(h, g[q], m[q]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[q][e] = r0 + r + q < rows ? (f16)(u[e] * inv) : (f16)0.f;
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      if (tall) *(f16x4*)&turn[turn_at(c + q, r >> 2)] = f16x4{o[0][q], o[1][q], o[2][q], o[3][q]};
+      else *(f16x4*)(x + (int64_t)(r + q) * np + c) = f16x4{o[q][0], o[q][1], o[q][2], o[q][3]};
+    }
   }
-  // X[i][j] = u[j][i]: 32 rows of u at a time through LDS
-  for (int j0 = 0; j0 < kMuonTile; j0 += 32) {
-    const int c = tile.i * kMuonTile + col;
-    for (int r = row0; r < 32; r += 2) {
-      const int row = tile.j * kMuonTile + j0 + r;
-      turn[r][col] = row < t.rows && c < t.cols ? (f16)u((int64_t)row * t.cols + c) : (f16)0.f;
-    }
-    __syncthreads();
-    for (int i = tid >> 5; i < kMuonTile; i += 8) x[(int64_t)i * t.np + j0 + (tid & 31)] = turn[tid & 31][i];
-    __syncthreads();
+  if (!tall) return;
+  __syncthreads();
+#pragma unroll 4
+  for (int k = 0; k < 16; ++k) {
+    const int i = k * 8 + (tid >> 5);
+    *(f16x4*)(x + (int64_t)i * np + c) = *(const f16x4*)&turn[turn_at(i, tid & 31)];
   }
 }
 
-// STAGE 1: A = X X^T.  2: B = b A + c A A.  3: X' = a X + B X.  A block makes 128 x 128.
+// STAGE 1: A = X X^T.  2: B = a I + b A + c A A.  3: X' = B X.  A block makes 128 x 128; for matrices of which larger tiles would be
+// mostly padding, or too few (muon_large).
 template <int STAGE>
 __global__ __launch_bounds__(256, 2) void muon_product_kernel(const MuonMatrix* mats, const MuonTile* tiles, char* ws, int from) {
   using namespace large;
@@ -125,7 +192,9 @@ __global__ __launch_bounds__(256, 2) void muon_product_kernel(const MuonMatrix* 
   const int mp = __builtin_amdgcn_readfirstlane(t.mp), np = __builtin_amdgcn_readfirstlane(t.np);
   const int ti = __builtin_amdgcn_readfirstlane(tile.i), tj = __builtin_amdgcn_readfirstlane(tile.j);
   const f16 *x = in_scratch(ws, t.x[from]), *a = in_scratch(ws, t.a), *b = in_scratch(ws, t.b);
-  const int lda = STAGE == 1 ? np : mp, ldb = STAGE == 2 ? mp : np, K = STAGE == 1 ? np : mp;
+  // (zeros behind the last index need no product)
+  const int lda = STAGE == 1 ? np : mp, ldb = STAGE == 2 ? mp : np;
+  const int K = __builtin_amdgcn_readfirstlane(STAGE == 1 ? max(t.rows, t.cols) : min(t.rows, t.cols));
   const f16* pa = (STAGE == 1 ? x : STAGE == 2 ? a : b) + (int64_t)ti * R * lda;
   const f16* pb = STAGE == 3 ? x + tj * R : (STAGE == 1 ? x : a) + (int64_t)tj * R * ldb;
   uint64_t base_a, base_b;
@@ -156,7 +225,7 @@ __global__ __launch_bounds__(256, 2) void muon_product_kernel(const MuonMatrix* 
   for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const int steps = K / BK;
+  const int steps = (K + BK - 1) / BK;
   fetch(0);
   for (int k = 0, buf = 0; k < steps; ++k, buf ^= 1) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -186,10 +255,10 @@ __global__ __launch_bounds__(256, 2) void muon_product_kernel(const MuonMatrix* 
     for (int j = 0; j < 4; ++j) {
       const int row = wm * 64 + i * 16 + lr, piece = wn * 16 + j * 4 + lq;
       f32x4 v = acc[i][j];
-      if (STAGE != 1) {                                      // the operand itself, at the same place
-        const f16x4 s = *(const f16x4*)((STAGE == 2 ? a + ((int64_t)ti * R + row) * mp : x + ((int64_t)ti * R + row) * np) + tj * R + piece * 4);
+      if (STAGE == 2) {
+        const f16x4 s = *(const f16x4*)(a + ((int64_t)ti * R + row) * mp + tj * R + piece * 4);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = STAGE == 2 ? fmaf(kB, (float)s[e], kC * kBack * v[e]) : fmaf(kA, (float)s[e], kBack * v[e]);
+        for (int e = 0; e < 4; ++e) v[e] = fmaf(kB, (float)s[e], kC * kBack * v[e]) + (ti == tj && row == piece * 4 + e ? kA * kHeld : 0.f);
       } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] *= kBack;
@@ -202,11 +271,13 @@ __global__ __launch_bounds__(256, 2) void muon_product_kernel(const MuonMatrix* 
   __syncthreads();
   f16* const c = in_scratch(ws, STAGE == 1 ? t.a : STAGE == 2 ? t.b : t.x[from ^ 1]);
   const int ldc = STAGE == 3 ? np : mp;
+#pragma unroll 4
   for (int s = 0; s < R * R / 4 / 256; ++s) {
     const int row = s * 8 + (tid >> 5), piece = tid & 31;
     *(f16x4*)(c + ((int64_t)ti * R + row) * ldc + tj * R + piece * 4) = *(const f16x4*)(out + at(row, piece));
   }
   if (STAGE != 3 && ti != tj) {
+#pragma unroll 4
     for (int s = 0; s < R * R / 4 / 256; ++s) {              // the same below the diagonal
       const int col = s * 8 + (tid >> 5), row = (tid & 31) * 4;
       f16x4 o;
@@ -217,53 +288,207 @@ __global__ __launch_bounds__(256, 2) void muon_product_kernel(const MuonMatrix* 
   }
 }
 
-// The weights' step from the finished X.
+// The weights' step from the finished X, in the same blocks of 4 x 4 elements as the start.
 __global__ __launch_bounds__(256) void muon_apply_kernel(const MuonMatrix* mats, const MuonTile* tiles, const char* ws, MuonHyper h, int from) {
-  __shared__ f16 turn[32][kMuonTile + 2];
+  __shared__ __attribute__((aligned(16))) f16 turn[kMuonTile * kMuonTile];
   const MuonTile tile = tiles[blockIdx.x];
   const MuonMatrix& t = mats[tile.matrix];
-  const bool tall = t.rows > t.cols;
-  const f16* x = (const f16*)(ws + t.x[from]) + (int64_t)tile.i * kMuonTile * t.np + (int64_t)tile.j * kMuonTile;
-  const float step = h.rms * sqrtf((float)max(t.rows, t.cols)) * kBack;
-  auto apply = [&](int64_t at, f16 v) {
-    const float w = t.master[at], n = w - h.lr * fmaf(h.weight_decay, w, step * (float)v);
-    t.master[at] = n;
-    if (t.lowp) t.lowp[at] = f32_to_bf16(n);
-  };
-  const int tid = threadIdx.x, col = tid & 127, row0 = tid >> 7;
-  if (!tall) {
-    const int c = tile.j * kMuonTile + col;
-    for (int r = row0; r < kMuonTile; r += 2) {
-      const int row = tile.i * kMuonTile + r;
-      if (row < t.rows && c < t.cols) apply((int64_t)row * t.cols + c, x[(int64_t)r * t.np + col]);
+  const int rows = t.rows, cols = t.cols, np = t.np, tid = threadIdx.x, c = (tid & 31) * 4;
+  const bool tall = rows > cols;
+  const f16* x = (const f16*)(ws + t.x[from]) + (int64_t)tile.i * kMuonTile * np + (int64_t)tile.j * kMuonTile;
+  const float step = step_size(t, h);
+  const int r0 = (tall ? tile.j : tile.i) * kMuonTile, at = (tall ? tile.i : tile.j) * kMuonTile + c;   // of the weights
+  float* const master = t.master;
+  uint16_t* const lowp = t.lowp;
+  const bool whole = at - c + kMuonTile <= cols;
+  if (tall) {
+#pragma unroll 4
+    for (int k = 0; k < 16; ++k) {
+      const int i = k * 8 + (tid >> 5);
+      *(f16x4*)&turn[turn_at(i, tid & 31)] = *(const f16x4*)(x + (int64_t)i * np + c);
     }
-    return;
+    __syncthreads();
   }
-  for (int j0 = 0; j0 < kMuonTile; j0 += 32) {
-    for (int i = tid >> 5; i < kMuonTile; i += 8) turn[tid & 31][i] = x[(int64_t)i * t.np + j0 + (tid & 31)];
-    __syncthreads();
-    const int c = tile.i * kMuonTile + col;
-    for (int r = row0; r < 32; r += 2) {
-      const int row = tile.j * kMuonTile + j0 + r;
-      if (row < t.rows && c < t.cols) apply((int64_t)row * t.cols + c, turn[r][col]);
+  for (int k = 0; k < 4; ++k) {
+    const int r = k * 32 + (tid >> 5) * 4;
+    f32x4 w[4];
+    f16x4 s[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      w[q] = load_edge4(master + (int64_t)min(r0 + r + q, rows - 1) * cols, at, cols, whole);
+      s[q] = tall ? *(const f16x4*)&turn[turn_at(c + q, r >> 2)] : *(const f16x4*)(x + (int64_t)(r + q) * np + c);
     }
-    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      f32x4 v;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = tall ? (float)s[e][q] : (float)s[q][e];
+      if (r0 + r + q >= rows) continue;
+      const int64_t row = (int64_t)(r0 + r + q) * cols;
+      store_row4(master + row, lowp ? lowp + row : nullptr, at, cols, stepped(h, w[q], v, step));
+    }
   }
 }
 
-void muon_update(const MuonMatrix* mats, const MuonChunk* chunks, int n_chunks, const MuonTile* tri, int n_tri, const MuonTile* full, int n_full,
-                 void* workspace, const MuonHyper& h, hipStream_t st) {
-  if (n_chunks < 1) return;
+// A matrix of at most 128 x 256 (or turned) in one block: X, A and B stay in LDS, and the whole update is one launch.  Rows of X, A
+// and B are 16 bytes longer than their elements, so that neither the fragments' rows nor their columns meet in a bank.  The gradient
+// and the momentum are read twice, before and behind the norm, the second time out of the caches: held in registers they make the
+// code so long that fetching it takes longer.
+__global__ __launch_bounds__(512) void muon_small_kernel(const MuonMatrix* mats, MuonHyper h) {
+  extern __shared__ __attribute__((aligned(16))) f16 s_smem[];
+  __shared__ double lds[8];
+  constexpr int PX = kMuonSmallLong + 8, PA = kMuonSmallShort + 8;
+  f16 *const X = s_smem, *const A = X + kMuonSmallShort * PX, *const B = A + kMuonSmallShort * PA;
+  const MuonMatrix& t = mats[blockIdx.x];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lr = lane & 15, lq = lane >> 4;
+  const int rows = t.rows, cols = t.cols;
+  const bool tall = rows > cols;
+  const int m64 = (min(rows, cols) + 63) / 64 * 64, n64 = (max(rows, cols) + 63) / 64 * 64;   // what there is of X, with zeros behind
+  // a lane takes four elements of a row, as many lanes as the row needs (a power of two), rows `apart` apart four at a time
+  const int lanes = cols <= 16 ? 2 : cols <= 32 ? 3 : cols <= 64 ? 4 : cols <= 128 ? 5 : 6, apart = 512 >> lanes;
+  const int c = 4 * (tid & ((1 << lanes) - 1)), mine = tid >> lanes, many = min(max(cols - c, 0), 4);
+  const float *const grad = t.grad;
+  float *const mom = t.momentum, *const master = t.master;
+  double sum = 0.0;
+  auto two = [&](int r, f32x4& g, f32x4& m) {
+    r = min(r, rows - 1) * cols;
+    g = load_row4(grad + r, c, cols);
+    m = load_row4(mom + r, c, cols);
+  };
+  for (int r0 = mine; r0 < rows; r0 += 4 * apart) {
+    f32x4 g[4], m[4];
+    if (many)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) two(r0 + apart * q, g[q], m[q]);
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (many && r0 + apart * q < rows) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) m[q][e] = fmaf(h.momentum, m[q][e], g[q][e]);
+        store_row4(mom + (r0 + apart * q) * cols, nullptr, c, cols, m[q]);
+        const f32x4 u = direction(h, g[q], m[q]);            // (zeros behind the row)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum += (double)u[e] * u[e];
+      }
+  }
+  for (int i = tid; i < m64 * PX / 8; i += 512) ((f16x8*)X)[i] = f16x8{};
+  const float inv = (float)((double)kHeld / (sqrt(block_sum<8>(sum, lds)) + (double)h.eps));
+  for (int r0 = mine; r0 < rows; r0 += 4 * apart) {
+    f32x4 g[4], m[4];
+    if (many)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) two(r0 + apart * q, g[q], m[q]);
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (many && r0 + apart * q < rows) {
+        const f32x4 u = direction(h, g[q], m[q]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (e < many) X[tall ? (c + e) * PX + r0 + apart * q : (r0 + apart * q) * PX + c + e] = (f16)(u[e] * inv);
+      }
+  }
+  __syncthreads();
+  const int mt = m64 / 16, nt = n64 / 16;
+  auto row_frag = [&](const f16* s, int pitch, int block, int k) { return *(const f16x8*)(s + (block * 16 + lr) * pitch + k + 8 * lq); };
+  // a symmetric product of S's rows with themselves (A: of X's, K = n64; B: of A's, K = m64), tiles on and above the diagonal
+  auto symmetric = [&](const f16* S, int pitch, int K, f16* to, bool second) {
+    for (int q = wave; q < mt * (mt + 1) / 2; q += 8) {
+      int i = 0, left = q;
+      while (left >= mt - i) { left -= mt - i; ++i; }
+      const int j = i + left;
+      f32x4 acc = {0.f, 0.f, 0.f, 0.f}, odd = acc;             // (two sums: the one's product need not wait for the other's)
+      for (int k = 0; k < K; k += 64) {
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(row_frag(S, pitch, j, k), row_frag(S, pitch, i, k), acc, 0, 0, 0);
+        odd = __builtin_amdgcn_mfma_f32_16x16x32_f16(row_frag(S, pitch, j, k + 32), row_frag(S, pitch, i, k + 32), odd, 0, 0, 0);
+      }
+      acc += odd;
+      // row 16 i + lr, columns 16 j + 4 lq .. + 3
+      f16x4 o;
+      f16x4 s = {};
+      if (second) s = *(const f16x4*)(A + (16 * i + lr) * PA + 16 * j + 4 * lq);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float v = second ? fmaf(kB, (float)s[e], kC * kBack * acc[e]) + (i == j && lr == 4 * lq + e ? kA * kHeld : 0.f) : kBack * acc[e];
+        o[e] = (f16)v;
+        if (i != j) to[(16 * j + 4 * lq + e) * PA + 16 * i + lr] = o[e];
+      }
+      *(f16x4*)(to + (16 * i + lr) * PA + 16 * j + 4 * lq) = o;
+    }
+  };
+  for (int it = 0; it < h.iterations; ++it) {
+    symmetric(X, PX, n64, A, false);
+    __syncthreads();
+    symmetric(A, PA, m64, B, true);
+    __syncthreads();
+    // X' = B X: 16 columns of X' come from the same 16 of X, which only their wave reads and writes
+    for (int j = wave; j < nt; j += 8) {
+      f32x4 acc[kMuonSmallShort / 16];
+#pragma unroll
+      for (int i = 0; i < kMuonSmallShort / 16; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int k = 0; k < m64; k += 32) {
+        const f16* p = X + (k + 8 * lq + (lr >> 2)) * PX + 16 * j + 4 * (lr & 3);
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_l*)p), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_l*)(p + 4 * PX));
+        typedef short s16x8 __attribute__((ext_vector_type(8)));
+        const f16x8 xf = __builtin_bit_cast(f16x8, (s16x8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+        for (int i = 0; i < kMuonSmallShort / 16; ++i)
+          if (i < mt) acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(xf, row_frag(B, PA, i, k), acc[i], 0, 0, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < kMuonSmallShort / 16; ++i)
+        if (i < mt) {
+          f16x4 o;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[e] = (f16)(kBack * acc[i][e]);
+          *(f16x4*)(X + (16 * i + lr) * PX + 16 * j + 4 * lq) = o;
+        }
+    }
+    __syncthreads();
+  }
+  const float step = step_size(t, h);
+  for (int r0 = mine; r0 < rows; r0 += 4 * apart) {
+    f32x4 w[4];
+    if (many)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) w[q] = load_row4(master + min(r0 + apart * q, rows - 1) * cols, c, cols);
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (many && r0 + apart * q < rows) {
+        const int r = r0 + apart * q;
+        f32x4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = (float)X[tall ? min(c + e, cols - 1) * PX + r : r * PX + c + e];
+        store_row4(master + r * cols, t.lowp ? t.lowp + r * cols : nullptr, c, cols, stepped(h, w[q], v, step));
+      }
+  }
+}
+
+void muon_update_small(const MuonMatrix* mats, int count, const MuonHyper& h, hipStream_t st) {
+  if (count < 1) return;
+  constexpr int LDS = (kMuonSmallShort * (kMuonSmallLong + 8) + 2 * kMuonSmallShort * (kMuonSmallShort + 8)) * 2;
+  static const bool configured = [] {
+    (void)hipFuncSetAttribute((const void*)muon_small_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+    return true;
+  }();
+  (void)configured;
+  hipLaunchKernelGGL(muon_small_kernel, dim3(count), dim3(512), LDS, st, mats, h);
+}
+
+void muon_update(const MuonMatrix* mats, const MuonUnits& u, void* workspace, const MuonHyper& h, hipStream_t st) {
+  if (u.n_chunks < 1) return;
   char* const ws = (char*)workspace;
-  hipLaunchKernelGGL(muon_momentum_kernel, dim3(n_chunks), dim3(256), 0, st, mats, chunks, ws, h);
-  hipLaunchKernelGGL(muon_start_kernel, dim3(n_full), dim3(256), 0, st, mats, full, ws, h);
+  hipLaunchKernelGGL(muon_momentum_kernel, dim3(u.n_chunks), dim3(256), 0, st, mats, u.chunks, ws, h);
+  hipLaunchKernelGGL(muon_start_kernel, dim3(u.n_cells), dim3(256), 0, st, mats, u.cells, ws, h);
   int from = 0;
   for (int i = 0; i < h.iterations; ++i, from ^= 1) {
-    hipLaunchKernelGGL((muon_product_kernel<1>), dim3(n_tri), dim3(256), 0, st, mats, tri, ws, from);
-    hipLaunchKernelGGL((muon_product_kernel<2>), dim3(n_tri), dim3(256), 0, st, mats, tri, ws, from);
-    hipLaunchKernelGGL((muon_product_kernel<3>), dim3(n_full), dim3(256), 0, st, mats, full, ws, from);
+    if (u.large[0]) muon_large_product(1, mats, u.large_tiles[0], u.large[0], ws, from, st);
+    if (u.n_tri) hipLaunchKernelGGL((muon_product_kernel<1>), dim3(u.n_tri), dim3(256), 0, st, mats, u.tri, ws, from);
+    if (u.large[1]) muon_large_product(2, mats, u.large_tiles[1], u.large[1], ws, from, st);
+    if (u.n_tri) hipLaunchKernelGGL((muon_product_kernel<2>), dim3(u.n_tri), dim3(256), 0, st, mats, u.tri, ws, from);
+    if (u.large[2]) muon_large_product(3, mats, u.large_tiles[2], u.large[2], ws, from, st);
+    if (u.n_full) hipLaunchKernelGGL((muon_product_kernel<3>), dim3(u.n_full), dim3(256), 0, st, mats, u.full, ws, from);
   }
-  hipLaunchKernelGGL(muon_apply_kernel, dim3(n_full), dim3(256), 0, st, mats, full, ws, h, from);
+  hipLaunchKernelGGL(muon_apply_kernel, dim3(u.n_cells), dim3(256), 0, st, mats, u.cells, ws, h, from);
 }
 
 }  // namespace mk

@@ -49,7 +49,7 @@ def check(matrices, table, **kw):
             assert torch.equal(t["lowp"], t["master"].bfloat16())
 
 
-SHAPES = [(1, 1), (1, 9), (9, 1), (3, 4), (64, 64), (65, 130), (130, 65), (128, 128), (127, 129), (129, 257), (300, 77), (77, 300), (256, 256)]
+SHAPES = [(1, 1), (1, 9), (9, 1), (3, 4), (64, 64), (65, 130), (130, 65), (128, 128), (127, 129), (129, 257), (300, 77), (77, 300), (256, 256), (128, 256), (256, 128), (128, 257), (129, 256), (33, 200)]
 
 
 @pytest.mark.parametrize("shape", SHAPES, ids=str)
@@ -57,6 +57,16 @@ def test_one_matrix(shape):
     ms = [matrix(shape, sum(shape))]
     table = mi.MuonTable(ms)
     for _ in range(2):                                            # the second step starts from the first one's momentum
+        check(ms, table)
+
+
+@pytest.mark.parametrize("parts", [1, 3])
+def test_large_tiles(parts):
+    """Sides from the smallest that takes tiles of 256 on, whole tiles and not, beside smaller ones."""
+    ms = [matrix(s, i) for i, s in enumerate([(513, 513), (700, 1300), (64, 70), (1300, 700), (640, 520), (300, 400), (768, 768), (520, 2100)])]
+    table = mi.MuonTable(ms, parts=parts)
+    table.workspace.fill_(0xFF)
+    for _ in range(2):
         check(ms, table)
 
 
@@ -136,7 +146,7 @@ def test_the_same_whatever_the_list():
 
 def test_captured_on_two_workspaces():
     """Two captured steps with a workspace each, replayed side by side, beside an eager one."""
-    sets = [[matrix((90, 150), s), matrix((150, 90), s + 1)] for s in (20, 30, 40)]
+    sets = [[matrix((90, 150), s), matrix((310, 150), s + 1)] for s in (20, 30, 40)]
     eager = [[{k: x.clone() for k, x in t.items()} for t in ms] for ms in sets]
     tables = [mi.MuonTable(ms) for ms in sets]
     for table in tables:

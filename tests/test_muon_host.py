@@ -61,7 +61,7 @@ def test_table():
 def table(**kw):
     t = mi.mimose_muon_table()
     t.device, t.workspace_bytes, t.matrices, t.parts = AT[0], 1 << 16, 1, 1
-    t.chunks[0] = t.tri[0] = t.full[0] = 1
+    t.units[0][0] = t.units[1][0] = 1
     for k, v in kw.items():
         setattr(t, k, v)
     return t
@@ -77,8 +77,8 @@ def test_steps(wrong, why):
 
 
 def test_tables_that_are_none():
-    for kw in (dict(device=None), dict(matrices=0), dict(parts=0), dict(parts=65)):
+    for kw in (dict(device=None), dict(matrices=-1), dict(parts=0), dict(parts=65)):
         assert "table" in refused(mi.mimose_op_muon_step, table(**kw), workspace=AT[1], workspace_bytes=1 << 16)
     t = table(parts=2)
-    t.chunks[1] = 0
+    t.units[0][1] = 0
     assert "table" in refused(mi.mimose_op_muon_step, t, workspace=AT[1], workspace_bytes=1 << 16)

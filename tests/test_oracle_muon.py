@@ -32,8 +32,8 @@ def test_distance_of_rounded_operands(shape, decay):
     a, b, c = muon.COEFFICIENTS
     for _ in range(5):
         A = held(x @ x.T)
-        B = held(b * A + c * A @ A)
-        x = held(a * x + B @ x)
+        B = held(a * np.eye(len(A)) + b * A + c * A @ A)
+        x = held(B @ x)
     want, off = muon.orthogonalise(u, 0.0, 5)
     got = np.linalg.norm((x.T if shape[0] > shape[1] else x) - want)
     assert off / 3 <= got <= 2 * off
