@@ -23,6 +23,8 @@
 #include "gemm_device.h"
 #include "packed_device.h"
 
+#include <type_traits>
+
 namespace mk {
 namespace {
 
@@ -60,18 +62,18 @@ __device__ __forceinline__ int swizzle(int r) {
   return ((r >> 2) & 3) | (D == 64 ? (r & 2) << 1 : D == 128 ? (r & 3) << 2 : 0);
 }
 
-// A tile of TK rows in LDS: its direct loads and a wave's fragments of it.
-template <int D>
+// A tile of TK rows in LDS: its direct loads by WAVES waves, and a wave's fragments of it.
+template <int D, int WAVES = 4>
 struct Tile {
   static constexpr int SIZE = TK * D;              // elements
-  static constexpr int LOADS = D / 32;             // 1 KB direct loads of each of four waves
+  static constexpr int LOADS = D / 8 / WAVES;      // 1 KB direct loads of each wave
   uint32_t from[LOADS];                            // byte offset of the lane's chunk from the tile's first row
   int plain, turned;
   __device__ __forceinline__ void init(int wave, int lane, int ld) {
     constexpr int NC = D / 8;
 #pragma unroll
     for (int j = 0; j < LOADS; ++j) {
-      const int row = 16 * wave + j * (64 / NC) + lane / NC;
+      const int row = TK / WAVES * wave + j * (64 / NC) + lane / NC;
       from[j] = (uint32_t)(row * ld + (((lane % NC) ^ swizzle<D>(row)) << 3)) * 2u;
     }
     const int h = lane >> 5, r = lane & 31, q = 4 * h + ((lane & 15) >> 2);
@@ -108,10 +110,23 @@ struct Stream {
   __device__ __forceinline__ uint32_t bytes(int rows) const { return (uint32_t)min(rows, TK) * pitch; }
 };
 
+// Every wave's LDS accesses so far are done.
+__device__ __forceinline__ void meet() {
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
 // Every wave's direct loads so far are in LDS, and every wave is done reading what it read before.
 __device__ __forceinline__ void landed() {
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
+}
+
+// A number that a branch's code goes by, as it is: keeps the compiler from turning that code into selects that every tile would pay for
+// (for a mask, 48 instructions for 32 x 32 scores beside the 72 that they need; two copies of the loop's body instead spill).
+__device__ __forceinline__ int branch_stays(int v) {
+  asm volatile("" : "+v"(v));
+  return v;
 }
 
 // store a transposed accumulator (rows = head columns, lane column = token) as bf16
@@ -137,7 +152,7 @@ __global__ __launch_bounds__(256, 2) void packed_fwd_kernel(PackedAttention p, i
   __shared__ __attribute__((aligned(1024))) bf16_t tiles[2][2][Tile<D>::SIZE];   // [buffer][K, V]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), ql = lane & 31, h = lane >> 5;
   PackedPlace w;
-  if (!packed_place<BM>(p, slots, w)) return;
+  if (!packed_place<BM, CAUSAL>(p, slots, w)) return;
   const int w0 = w.row + wave * 32, qi = w0 + ql, qc = min(qi, w.n - 1);
   const float c2 = p.scale * LOG2E;                   // exp(scale * s - x) == exp2(c2 * s - LOG2E * x)
 
@@ -162,13 +177,9 @@ __global__ __launch_bounds__(256, 2) void packed_fwd_kernel(PackedAttention p, i
     tk.load(ks.at(k0), ks.bytes(w.n - k0), wave, lds + (uint32_t)buf * (4u * Tile<D>::SIZE));
     tv.load(vs.at(k0), vs.bytes(w.n - k0), wave, lds + (uint32_t)buf * (4u * Tile<D>::SIZE) + 2u * Tile<D>::SIZE);
   };
-  fetch(0, 0);
-  for (int k0 = 0, buf = 0; k0 < kend; k0 += TK, buf ^= 1) {
-    landed();
-    if (k0 + TK < kend) fetch(k0 + TK, buf ^ 1);
-    const bf16_t *Ks = tiles[buf][0], *Vs = tiles[buf][1];
-    if (w0 >= w.n || (CAUSAL && k0 > w0 + 31)) continue;   // none of this wave's queries sees the tile
+  auto step = [&](int k0, int buf) __attribute__((always_inline)) {
     const bool edge = k0 + TK > w.n || (CAUSAL && k0 + TK - 1 > w0);
+    const bf16_t *Ks = tiles[buf][0], *Vs = tiles[buf][1];
     f32x16 s[2];
     float mx = -INFINITY;
 #pragma unroll
@@ -176,16 +187,19 @@ __global__ __launch_bounds__(256, 2) void packed_fwd_kernel(PackedAttention p, i
       zero(s[kb]);
 #pragma unroll
       for (int kk = 0; kk < KK; ++kk) s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tk.row(Ks, kb, kk), qf[kk], s[kb], 0, 0, 0);
-      if (edge) {                                     // only tiles that touch the mask pay for it
+    }
+    if (edge) {                                       // the tile touches the mask
+      const int end = branch_stays((CAUSAL ? min(w.n, qi + 1) : w.n) - k0 - 4 * h);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int key = k0 + 32 * kb + 8 * (r >> 2) + 4 * h + (r & 3);
-          if (key >= w.n || (CAUSAL && key > qi)) s[kb][r] = -INFINITY;
-        }
-      }
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (32 * kb + 8 * (r >> 2) + (r & 3) >= end) s[kb][r] = -INFINITY;
+    }
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
       for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[kb][r]);
-    }
     mx = fmaxf(mx, other_half(mx));
     const float mnew = fmaxf(m, mx);                  // finite: a sequence's first row is visible to all of them
     float alpha = 1.f;
@@ -218,6 +232,12 @@ __global__ __launch_bounds__(256, 2) void packed_fwd_kernel(PackedAttention p, i
         for (int db = 0; db < DB; ++db)
           o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tv.column(Vs, db, 32 * kb + 16 * c), pf, o[db], 0, 0, 0);
       }
+  };
+  fetch(0, 0);
+  for (int k0 = 0, buf = 0; k0 < kend; k0 += TK, buf ^= 1) {
+    landed();
+    if (k0 + TK < kend) fetch(k0 + TK, buf ^ 1);
+    if (w0 < w.n && !(CAUSAL && k0 > w0 + 31)) step(k0, buf);   // else none of this wave's queries sees the tile
   }
   if (qi < w.n) {
     store_rows<D>((bf16_t*)p.out + (w.first + qi) * p.ldo + w.head * D, o, h, 1.f / l);
@@ -232,7 +252,7 @@ __global__ __launch_bounds__(256, 2) void packed_bwd_dq_kernel(PackedAttention p
   __shared__ __attribute__((aligned(1024))) bf16_t tiles[2][2][Tile<D>::SIZE];   // [buffer][K, V]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), ql = lane & 31, h = lane >> 5;
   PackedPlace w;
-  if (!packed_place<BM>(p, slots, w)) return;
+  if (!packed_place<BM, CAUSAL>(p, slots, w)) return;
   const int w0 = w.row + wave * 32, qi = w0 + ql, qc = min(qi, w.n - 1);
   const float c2 = p.scale * LOG2E;
 
@@ -273,12 +293,9 @@ __global__ __launch_bounds__(256, 2) void packed_bwd_dq_kernel(PackedAttention p
     tk.load(ks.at(k0), ks.bytes(w.n - k0), wave, lds + (uint32_t)buf * (4u * Tile<D>::SIZE));
     tv.load(vs.at(k0), vs.bytes(w.n - k0), wave, lds + (uint32_t)buf * (4u * Tile<D>::SIZE) + 2u * Tile<D>::SIZE);
   };
-  fetch(0, 0);
-  for (int k0 = 0, buf = 0; k0 < kend; k0 += TK, buf ^= 1) {
-    landed();
-    if (k0 + TK < kend) fetch(k0 + TK, buf ^ 1);
+  auto step = [&](int k0, int buf) __attribute__((always_inline)) {
+    const bool edge = k0 + TK > w.n || (CAUSAL && k0 + TK - 1 > w0);
     const bf16_t *Ks = tiles[buf][0], *Vs = tiles[buf][1];
-    if (w0 >= w.n || (CAUSAL && k0 > w0 + 31)) continue;   // none of this wave's queries sees the tile
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
       f32x16 s, dp;
@@ -290,12 +307,11 @@ __global__ __launch_bounds__(256, 2) void packed_bwd_dq_kernel(PackedAttention p
       }
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[r] = fast_exp2(fmaf(s[r], c2, nlse)) * (dp[r] - delta);
-      if (k0 + TK > w.n || (CAUSAL && k0 + TK - 1 > w0)) {
+      if (edge) {
+        const int end = branch_stays((CAUSAL ? min(w.n, qi + 1) : w.n) - k0 - 32 * kb - 4 * h);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int key = k0 + 32 * kb + 8 * (r >> 2) + 4 * h + (r & 3);
-          if (key >= w.n || (CAUSAL && key > qi)) s[r] = 0.f;
-        }
+        for (int r = 0; r < 16; ++r)
+          if (8 * (r >> 2) + (r & 3) >= end) s[r] = 0.f;
       }
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
@@ -305,20 +321,29 @@ __global__ __launch_bounds__(256, 2) void packed_bwd_dq_kernel(PackedAttention p
           dq[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tk.column(Ks, db, 32 * kb + 16 * c), dsf, dq[db], 0, 0, 0);
       }
     }
+  };
+  fetch(0, 0);
+  for (int k0 = 0, buf = 0; k0 < kend; k0 += TK, buf ^= 1) {
+    landed();
+    if (k0 + TK < kend) fetch(k0 + TK, buf ^ 1);
+    if (w0 < w.n && !(CAUSAL && k0 > w0 + 31)) step(k0, buf);   // else none of this wave's queries sees the tile
   }
   if (qi < w.n) store_rows<D>((bf16_t*)p.dq + (w.first + qi) * p.lddq + w.head * D, dq, h, p.scale);
 }
 
 // ------------------------------------------------------------------ dK, dV
-// A block takes its keys through the query rows of every head that shares them, one head after the other.
-template <int D, bool CAUSAL>
-__global__ __launch_bounds__(256, D == 128 ? 1 : 2) void packed_bwd_dkv_kernel(PackedAttention p, int slots) {
-  constexpr int KK = D / 16, DB = D / 32;
-  __shared__ __attribute__((aligned(1024))) bf16_t tiles[2][2][Tile<D>::SIZE];   // [buffer][Q, dO]
-  __shared__ __attribute__((aligned(16))) float lse_s[2][TK], delta_s[2][TK];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), kl = lane & 31, h = lane >> 5;
+// A block takes its keys through the query rows of every head that shares them.  G groups of KW waves, 32 keys to a wave: each
+// group has the same keys and every G-th tile of those rows, in tiles of its own, and their sums are added at the end in the groups' order.
+template <int D, bool CAUSAL, int KW, int G>
+__global__ __launch_bounds__(64 * KW * G, KW * G == 4 ? 2 : 1) void packed_bwd_dkv_kernel(PackedAttention p, int slots) {
+  constexpr int KK = D / 16, DB = D / 32, BN = 32 * KW;
+  typedef Tile<D, KW> T;
+  __shared__ __attribute__((aligned(1024))) bf16_t tiles[G][2][2][T::SIZE];      // [group][buffer][Q, dO]
+  __shared__ __attribute__((aligned(16))) float lse_s[G][2][TK], delta_s[G][2][TK];
+  const int tid = threadIdx.x, lane = tid & 63, all = __builtin_amdgcn_readfirstlane(tid >> 6), kl = lane & 31, h = lane >> 5;
+  const int g = all / KW, wave = all - g * KW;
   PackedPlace w;
-  if (!packed_place_kv<BM>(p, slots, CAUSAL, w)) return;
+  if (!packed_place_kv<BN, CAUSAL>(p, slots, w)) return;
   const int w0 = w.row + wave * 32, ki = w0 + kl, kc = min(ki, w.n - 1);
   const float c2 = p.scale * LOG2E;
 
@@ -335,10 +360,158 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void packed_bwd_dkv_kernel(P
   f32x16 dk[DB], dv[DB];
 #pragma unroll
   for (int db = 0; db < DB; ++db) { zero(dk[db]); zero(dv[db]); }
+  const int qstart = CAUSAL ? w.row / TK * TK : 0;    // earlier queries never see these keys
+  const int group = p.n_heads / p.n_kv_heads, per_head = (w.n - qstart + TK - 1) / TK, steps = (per_head * group + G - 1) / G;
+
+  T tq, tg;
+  tq.init(wave, lane, (int)p.ldq);
+  tg.init(wave, lane, (int)p.lddo);
+  Stream qs, gs;
+  qs.init((const bf16_t*)p.q + w.first * p.ldq + w.kv * group * D, (int)p.ldq);
+  gs.init((const bf16_t*)p.dout + w.first * p.lddo + w.kv * group * D, (int)p.lddo);
+  const uint32_t lds = l_lds_address(&tiles[0][0][0][0]) + (uint32_t)g * (8u * T::SIZE);
+  const int64_t stats = (int64_t)w.kv * group * p.T + w.first;
+  const int mine = tid - g * (64 * KW);               // thread of the group
+  float pre_lse = 0.f, pre_delta = 0.f;
+  int head = 0, q0 = qstart + g * TK;                 // the tile to fetch
+  auto settle = [&]() {
+    while (q0 >= w.n && head < group) { q0 -= per_head * TK; ++head; }
+  };
+  auto fetch = [&](int buf) {                         // behind the last head: nothing
+    if (head < group) {
+      const uint64_t at = (uint64_t)head * (D * 2u);
+      tq.load(qs.at(q0) + at, qs.bytes(w.n - q0), wave, lds + (uint32_t)buf * (4u * T::SIZE));
+      tg.load(gs.at(q0) + at, gs.bytes(w.n - q0), wave, lds + (uint32_t)buf * (4u * T::SIZE) + 2u * T::SIZE);
+      if (mine < TK) {
+        const int q = min(q0 + mine, w.n - 1);
+        pre_lse = p.lse[stats + (int64_t)head * p.T + q];
+        pre_delta = p.delta[stats + (int64_t)head * p.T + q];
+      }
+    }
+  };
+  auto step = [&](int at, int buf) __attribute__((always_inline)) {   // at: the tile's first row
+    const bf16_t *Qs = tiles[g][buf][0], *Gs = tiles[g][buf][1];
+#pragma unroll
+    for (int qb = 0; qb < 2; ++qb) {
+      f32x16 s, dp;
+      zero(s); zero(dp);
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) {
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tq.row(Qs, qb, kk), kf[kk], s, 0, 0, 0);
+        dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tg.row(Gs, qb, kk), vf[kk], dp, 0, 0, 0);
+      }
+#pragma unroll
+      for (int q4 = 0; q4 < 4; ++q4) {
+        const int qq = 32 * qb + 8 * q4 + 4 * h;
+        const float4 nl = *(const float4*)&lse_s[g][buf][qq], dl = *(const float4*)&delta_s[g][buf][qq];
+        const float nls[4] = {nl.x, nl.y, nl.z, nl.w}, dls[4] = {dl.x, dl.y, dl.z, dl.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int r = 4 * q4 + e;
+          const float pr = fast_exp2(fmaf(s[r], c2, nls[e]));
+          s[r] = pr;
+          dp[r] = pr * (dp[r] - dls[e]);
+        }
+      }
+      if (CAUSAL && at < w0 + 31) {                   // the tile touches the mask
+        const int first = branch_stays(ki - at - 32 * qb - 4 * h);
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (8 * (r >> 2) + (r & 3) < first) { s[r] = 0.f; dp[r] = 0.f; }
+      }
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const bf16x8 pf = regs_to_frag(s, c), dsf = regs_to_frag(dp, c);
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+          dv[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tg.column(Gs, db, 32 * qb + 16 * c), pf, dv[db], 0, 0, 0);
+          dk[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tq.column(Qs, db, 32 * qb + 16 * c), dsf, dk[db], 0, 0, 0);
+        }
+      }
+    }
+  };
+  settle();
+  fetch(0);
+  for (int turn = 0, buf = 0; turn < steps; ++turn, buf ^= 1) {
+    const bool some = head < group && w0 < w.n;
+    const int at = q0;
+    // lse_s: ready for exp2, and minus infinity behind the sequence: probabilities of zero there.  This buffer was last
+    // read two tiles ago, before the last barrier.
+    if (mine < TK) { lse_s[g][buf][mine] = at + mine < w.n ? -LOG2E * pre_lse : -INFINITY; delta_s[g][buf][mine] = pre_delta; }
+    landed();
+    q0 += G * TK;
+    settle();
+    fetch(buf ^ 1);
+    if (some && !(CAUSAL && at + TK <= w0)) step(at, buf);   // else no query of the tile sees this wave's keys
+  }
+  bf16_t* const dk_row = (bf16_t*)p.dk + (w.first + ki) * p.lddk + w.kv * D;
+  bf16_t* const dv_row = (bf16_t*)p.dv + (w.first + ki) * p.lddv + w.kv * D;
+  if (G == 1) {
+    if (ki < w.n) {
+      store_rows<D>(dk_row, dk, h, p.scale);
+      store_rows<D>(dv_row, dv, h, 1.f);
+    }
+    return;
+  }
+  // Four registers at a time are a part: rows 8 (part % 4) + 4 h .. of 32 head columns.  Group g adds all groups' parts
+  // of its share of them.
+  constexpr int PARTS = 8 * DB, SHARE = PARTS / G;
+  float4* const parts = (float4*)&tiles[0][0][0][0];  // [group][wave][part][lane], as large as the tiles
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < PARTS; ++i) {
+    const f32x16& v = i < PARTS / 2 ? dk[i / 4] : dv[i / 4 - DB];
+    parts[((g * KW + wave) * PARTS + i) * 64 + lane] = make_float4(v[4 * (i & 3)], v[4 * (i & 3) + 1], v[4 * (i & 3) + 2], v[4 * (i & 3) + 3]);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < SHARE; ++i) {
+    const int part = g * SHARE + i;
+    float4 s = parts[(wave * PARTS + part) * 64 + lane];
+#pragma unroll
+    for (int o = 1; o < G; ++o) {
+      const float4 v = parts[((o * KW + wave) * PARTS + part) * 64 + lane];
+      s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+    }
+    const bool keys = part < PARTS / 2;
+    const float mul = keys ? p.scale : 1.f;
+    const int column = (part % (PARTS / 2)) / 4 * 32 + 8 * (part & 3) + 4 * h;
+    if (ki < w.n) *(uint2*)((keys ? dk_row : dv_row) + column) = make_uint2(pack_bf16x2(s.x * mul, s.y * mul), pack_bf16x2(s.z * mul, s.w * mul));
+  }
+}
+
+// Heads of 128: a wave with both gradients of 32 keys would need more registers than let two waves run on a SIMD.  So a pair of waves
+// has the same 32 keys: the first makes S and P and holds dV, the second makes dP and dS and holds dK; P passes from the one to the other
+// through LDS in fp32, behind a second barrier, which leaves the exponentials of the one beside the products of the other.
+template <bool CAUSAL>
+__global__ __launch_bounds__(512) void packed_bwd_dkv_pair_kernel(PackedAttention p, int slots) {
+  constexpr int D = 128, KK = D / 16, DB = D / 32, BN = 128;
+  typedef Tile<D, 8> T;
+  __shared__ __attribute__((aligned(1024))) bf16_t tiles[2][2][T::SIZE];         // [buffer][Q, dO]
+  __shared__ __attribute__((aligned(16))) float4 passed[4][2][4][64];            // P: [keys' wave][half of the rows][registers / 4][lane]
+  __shared__ __attribute__((aligned(16))) float lse_s[2][TK], delta_s[2][TK];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), kl = lane & 31, h = lane >> 5;
+  const int kw = wave & 3;
+  const bool values = wave < 4;                       // holds dV
+  PackedPlace w;
+  if (!packed_place_kv<BN, CAUSAL>(p, slots, w)) return;
+  const int w0 = w.row + kw * 32, ki = w0 + kl, kc = min(ki, w.n - 1);
+  const float c2 = p.scale * LOG2E;
+
+  bf16x8 own[KK];                                     // the keys' rows of K, or of V
+  {
+    const bf16_t* row = values ? (const bf16_t*)p.k + (w.first + kc) * p.ldk : (const bf16_t*)p.v + (w.first + kc) * p.ldv;
+    row += w.kv * D + 8 * h;
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) own[kk] = *(const bf16x8*)(row + 16 * kk);
+  }
+  f32x16 acc[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db) zero(acc[db]);
   const int qstart = CAUSAL ? w.row : 0;              // earlier queries never see these keys (a multiple of TK)
   const int group = p.n_heads / p.n_kv_heads;
 
-  Tile<D> tq, tg;
+  T tq, tg;
   tq.init(wave, lane, (int)p.ldq);
   tg.init(wave, lane, (int)p.lddo);
   Stream qs, gs;
@@ -349,69 +522,99 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void packed_bwd_dkv_kernel(P
   float pre_lse = 0.f, pre_delta = 0.f;
   auto fetch = [&](int head, int q0, int buf) {
     const uint64_t at = (uint64_t)head * (D * 2u);
-    tq.load(qs.at(q0) + at, qs.bytes(w.n - q0), wave, lds + (uint32_t)buf * (4u * Tile<D>::SIZE));
-    tg.load(gs.at(q0) + at, gs.bytes(w.n - q0), wave, lds + (uint32_t)buf * (4u * Tile<D>::SIZE) + 2u * Tile<D>::SIZE);
+    tq.load(qs.at(q0) + at, qs.bytes(w.n - q0), wave, lds + (uint32_t)buf * (4u * T::SIZE));
+    tg.load(gs.at(q0) + at, gs.bytes(w.n - q0), wave, lds + (uint32_t)buf * (4u * T::SIZE) + 2u * T::SIZE);
     if (tid < TK) {
       const int q = min(q0 + tid, w.n - 1);
       pre_lse = p.lse[stats + (int64_t)head * p.T + q];
       pre_delta = p.delta[stats + (int64_t)head * p.T + q];
     }
   };
-  fetch(0, qstart, 0);
-  int buf = 0;
-  for (int head = 0; head < group; ++head)
-    for (int q0 = qstart; q0 < w.n; q0 += TK, buf ^= 1) {
-      // lse_s: ready for exp2, and minus infinity behind the sequence: probabilities of zero there.  This buffer was last
-      // read two tiles ago, before the last barrier.
-      if (tid < TK) { lse_s[buf][tid] = q0 + tid < w.n ? -LOG2E * pre_lse : -INFINITY; delta_s[buf][tid] = pre_delta; }
-      landed();
-      if (q0 + TK < w.n) fetch(head, q0 + TK, buf ^ 1);
-      else if (head + 1 < group) fetch(head + 1, qstart, buf ^ 1);
-      if (w0 >= w.n || (CAUSAL && q0 + TK <= w0)) continue;   // no query of the tile sees this wave's keys
-      const bf16_t *Qs = tiles[buf][0], *Gs = tiles[buf][1];
+  // a tile's first half: S and P, or dP
+  f32x16 s[2];
+  auto first = [&](int q0, int buf, auto values_) __attribute__((always_inline)) {
+    constexpr bool VALUES = decltype(values_)::value;
 #pragma unroll
-      for (int qb = 0; qb < 2; ++qb) {
-        f32x16 s, dp;
-        zero(s); zero(dp);
+    for (int qb = 0; qb < 2; ++qb) {
+      zero(s[qb]);
 #pragma unroll
-        for (int kk = 0; kk < KK; ++kk) {
-          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tq.row(Qs, qb, kk), kf[kk], s, 0, 0, 0);
-          dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tg.row(Gs, qb, kk), vf[kk], dp, 0, 0, 0);
-        }
+      for (int kk = 0; kk < KK; ++kk)
+        s[qb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(VALUES ? tq.row(tiles[buf][0], qb, kk) : tg.row(tiles[buf][1], qb, kk), own[kk], s[qb], 0, 0, 0);
+    }
+    if (!VALUES) return;
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const int qq = 32 * qb + 8 * g + 4 * h;
-          const float4 nl = *(const float4*)&lse_s[buf][qq], dl = *(const float4*)&delta_s[buf][qq];
-          const float nls[4] = {nl.x, nl.y, nl.z, nl.w}, dls[4] = {dl.x, dl.y, dl.z, dl.w};
+    for (int qb = 0; qb < 2; ++qb)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int r = 4 * g + e;
-            const float pr = fast_exp2(fmaf(s[r], c2, nls[e]));
-            s[r] = pr;
-            dp[r] = pr * (dp[r] - dls[e]);
-          }
-        }
-        if (CAUSAL && q0 < w0 + 31) {
+      for (int q4 = 0; q4 < 4; ++q4) {
+        const int qq = 32 * qb + 8 * q4 + 4 * h;
+        const float4 nl = *(const float4*)&lse_s[buf][qq];
+        const float nls[4] = {nl.x, nl.y, nl.z, nl.w};
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int q = q0 + 32 * qb + 8 * (r >> 2) + 4 * h + (r & 3);
-            if (ki > q) { s[r] = 0.f; dp[r] = 0.f; }
-          }
-        }
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const bf16x8 pf = regs_to_frag(s, c), dsf = regs_to_frag(dp, c);
-#pragma unroll
-          for (int db = 0; db < DB; ++db) {
-            dv[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tg.column(Gs, db, 32 * qb + 16 * c), pf, dv[db], 0, 0, 0);
-            dk[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tq.column(Qs, db, 32 * qb + 16 * c), dsf, dk[db], 0, 0, 0);
-          }
+        for (int e = 0; e < 4; ++e) {
+          const int r = 4 * q4 + e;
+          s[qb][r] = fast_exp2(fmaf(s[qb][r], c2, nls[e]));
         }
       }
+    if (CAUSAL && q0 < w0 + 31) {                     // the tile touches the mask
+      const int from = branch_stays(ki - q0 - 4 * h);
+#pragma unroll
+      for (int qb = 0; qb < 2; ++qb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (32 * qb + 8 * (r >> 2) + (r & 3) < from) s[qb][r] = 0.f;
     }
+#pragma unroll
+    for (int qb = 0; qb < 2; ++qb)
+#pragma unroll
+      for (int q4 = 0; q4 < 4; ++q4)
+        passed[kw][qb][q4][lane] = make_float4(s[qb][4 * q4], s[qb][4 * q4 + 1], s[qb][4 * q4 + 2], s[qb][4 * q4 + 3]);
+  };
+  // its second half: dV, or dS and dK
+  auto second = [&](int buf, auto values_) __attribute__((always_inline)) {
+    constexpr bool VALUES = decltype(values_)::value;
+#pragma unroll
+    for (int qb = 0; qb < 2; ++qb) {
+      if (!VALUES) {
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) {
+          const float4 pr = passed[kw][qb][q4][lane], dl = *(const float4*)&delta_s[buf][32 * qb + 8 * q4 + 4 * h];
+          s[qb][4 * q4] = pr.x * (s[qb][4 * q4] - dl.x);
+          s[qb][4 * q4 + 1] = pr.y * (s[qb][4 * q4 + 1] - dl.y);
+          s[qb][4 * q4 + 2] = pr.z * (s[qb][4 * q4 + 2] - dl.z);
+          s[qb][4 * q4 + 3] = pr.w * (s[qb][4 * q4 + 3] - dl.w);
+        }
+      }
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const bf16x8 f = regs_to_frag(s[qb], c);
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+          acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(VALUES ? tg.column(tiles[buf][1], db, 32 * qb + 16 * c) : tq.column(tiles[buf][0], db, 32 * qb + 16 * c),
+                                                            f, acc[db], 0, 0, 0);
+      }
+    }
+  };
+  // the same barriers in both roles' loops
+  auto run = [&](auto values_) __attribute__((always_inline)) {
+    int buf = 0;
+    for (int head = 0; head < group; ++head)
+      for (int q0 = qstart; q0 < w.n; q0 += TK, buf ^= 1) {
+        if (tid < TK) { lse_s[buf][tid] = q0 + tid < w.n ? -LOG2E * pre_lse : -INFINITY; delta_s[buf][tid] = pre_delta; }
+        landed();
+        if (q0 + TK < w.n) fetch(head, q0 + TK, buf ^ 1);
+        else if (head + 1 < group) fetch(head + 1, qstart, buf ^ 1);
+        const bool some = w0 < w.n && !(CAUSAL && q0 + TK <= w0);   // a query of the tile sees this wave's keys
+        if (some) first(q0, buf, values_);
+        meet();                                       // P is there
+        if (some) second(buf, values_);
+      }
+  };
+  fetch(0, qstart, 0);
+  if (values) run(std::true_type());
+  else run(std::false_type());
   if (ki < w.n) {
-    store_rows<D>((bf16_t*)p.dk + (w.first + ki) * p.lddk + w.kv * D, dk, h, p.scale);
-    store_rows<D>((bf16_t*)p.dv + (w.first + ki) * p.lddv + w.kv * D, dv, h, 1.f);
+    if (values) store_rows<D>((bf16_t*)p.dv + (w.first + ki) * p.lddv + w.kv * D, acc, h, 1.f);
+    else store_rows<D>((bf16_t*)p.dk + (w.first + ki) * p.lddk + w.kv * D, acc, h, p.scale);
   }
 }
 
@@ -423,16 +626,17 @@ void launch_fwd(const PackedAttention& p, int causal, hipStream_t st) {
   if (causal) hipLaunchKernelGGL((packed_fwd_kernel<D, true>), grid, dim3(256), 0, st, p, slots);
   else hipLaunchKernelGGL((packed_fwd_kernel<D, false>), grid, dim3(256), 0, st, p, slots);
 }
-template <int D>
-void launch_bwd(const PackedAttention& p, int causal, hipStream_t st) {
-  const int slots = packed_slots(p.T, p.n_seq, BM);
-  const dim3 grid(packed_blocks(slots, p.n_kv_heads, p.n_heads / p.n_kv_heads)), grid_kv(packed_blocks(slots, p.n_kv_heads, 1));
-  if (causal) {
-    hipLaunchKernelGGL((packed_bwd_dq_kernel<D, true>), grid, dim3(256), 0, st, p, slots);
-    hipLaunchKernelGGL((packed_bwd_dkv_kernel<D, true>), grid_kv, dim3(256), 0, st, p, slots);
+template <int D, bool CAUSAL>
+void launch_bwd(const PackedAttention& p, hipStream_t st) {
+  const int slots = packed_slots(p.T, p.n_seq, BM), kv = p.n_kv_heads;
+  hipLaunchKernelGGL((packed_bwd_dq_kernel<D, CAUSAL>), dim3(packed_blocks(slots, kv, p.n_heads / kv)), dim3(256), 0, st, p, slots);
+  if constexpr (D == 128) {
+    hipLaunchKernelGGL((packed_bwd_dkv_pair_kernel<CAUSAL>), dim3(packed_blocks(slots, kv, 1)), dim3(512), 0, st, p, slots);
+  } else if ((int64_t)slots * kv >= 1024) {           // two blocks and more for every place that there is
+    hipLaunchKernelGGL((packed_bwd_dkv_kernel<D, CAUSAL, 4, 1>), dim3(packed_blocks(slots, kv, 1)), dim3(256), 0, st, p, slots);
   } else {
-    hipLaunchKernelGGL((packed_bwd_dq_kernel<D, false>), grid, dim3(256), 0, st, p, slots);
-    hipLaunchKernelGGL((packed_bwd_dkv_kernel<D, false>), grid_kv, dim3(256), 0, st, p, slots);
+    const int small = packed_slots(p.T, p.n_seq, 64);
+    hipLaunchKernelGGL((packed_bwd_dkv_kernel<D, CAUSAL, 2, 4>), dim3(packed_blocks(small, kv, 1)), dim3(512), 0, st, p, small);
   }
 }
 }  // namespace
@@ -443,9 +647,9 @@ void packed_attention_fwd_bf16(const PackedAttention& p, int d, int causal, hipS
   else launch_fwd<128>(p, causal, st);
 }
 void packed_attention_bwd_bf16(const PackedAttention& p, int d, int causal, hipStream_t st) {
-  if (d == 32) launch_bwd<32>(p, causal, st);
-  else if (d == 64) launch_bwd<64>(p, causal, st);
-  else launch_bwd<128>(p, causal, st);
+  if (d == 32) causal ? launch_bwd<32, true>(p, st) : launch_bwd<32, false>(p, st);
+  else if (d == 64) causal ? launch_bwd<64, true>(p, st) : launch_bwd<64, false>(p, st);
+  else causal ? launch_bwd<128, true>(p, st) : launch_bwd<128, false>(p, st);
 }
 
 }  // namespace mk

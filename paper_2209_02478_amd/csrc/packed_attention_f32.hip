@@ -114,7 +114,7 @@ __global__ __launch_bounds__(64 * W) void packed_f32_fwd_kernel(PackedAttention 
   float* const mine = stat + W * 128;                 // a wave's tile, and its part of the sum afterwards
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, h = lane >> 5;
   PackedPlace w;
-  if (!packed_place<TR>(p, slots, w)) return;
+  if (!packed_place<TR, CAUSAL>(p, slots, w)) return;
   const int qi = w.row + l32, last = w.n - 1;
   const float c2 = p.scale * LOG2E;
   const float* kb = (const float*)p.k + w.first * p.ldk + w.kv * D;
@@ -197,7 +197,7 @@ __global__ __launch_bounds__(64 * W) void packed_f32_bwd_dq_kernel(PackedAttenti
   float *const own_q = f_smem, *const own_g = own_q + TILE, *const mine = own_g + TILE;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, h = lane >> 5;
   PackedPlace w;
-  if (!packed_place<TR>(p, slots, w)) return;
+  if (!packed_place<TR, CAUSAL>(p, slots, w)) return;
   const int qi = w.row + l32, last = w.n - 1;
   const int64_t stats = (int64_t)w.head * p.T + w.first;
   const float* kb = (const float*)p.k + w.first * p.ldk + w.kv * D;
@@ -265,7 +265,7 @@ __global__ __launch_bounds__(64 * W) void packed_f32_bwd_dkv_kernel(PackedAttent
   float *const mine_q = rowstat + W * 2 * TR, *const mine_g = mine_q + W * TILE;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, h = lane >> 5;
   PackedPlace w;
-  if (!packed_place_kv<TR>(p, slots, CAUSAL, w)) return;
+  if (!packed_place_kv<TR, CAUSAL>(p, slots, w)) return;
   const int ki = w.row + l32, last = w.n - 1, group = p.n_heads / p.n_kv_heads;
   const float* qb = (const float*)p.q + w.first * p.ldq + w.kv * group * D;
   const float* gb = (const float*)p.dout + w.first * p.lddo + w.kv * group * D;

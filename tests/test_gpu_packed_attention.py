@@ -128,6 +128,15 @@ def test_many_sequences(dtype, count):
     Call(dtype, 2, 1, 32, lengths, behind=5, seed=count).check(1)
 
 
+@pytest.mark.parametrize("dtype,d,causal", [(1, 32, 0), (1, 64, 0), (1, 64, 1), (1, 128, 1), (0, 64, 1)])
+@pytest.mark.parametrize("count", [60, 70])
+def test_blocks_for_the_whole_device(dtype, d, causal, count):
+    """Heads of keys and rows enough to fill the device with blocks that share nothing, sequences in order of work and not."""
+    rng = np.random.default_rng(d)
+    lengths = rng.integers(1, 260, count).tolist()
+    Call(dtype, 16, 16, d, lengths, behind=1, seed=d).check(causal)
+
+
 @pytest.mark.parametrize("dtype", [1, 0])
 @pytest.mark.parametrize("spread", [1e-20, 8.0])
 def test_scores_of_any_size(dtype, spread):
