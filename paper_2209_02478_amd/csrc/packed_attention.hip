@@ -23,6 +23,7 @@
 #include "gemm_device.h"
 #include "packed_device.h"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace mk {
@@ -122,13 +123,6 @@ __device__ __forceinline__ void landed() {
   __syncthreads();
 }
 
-// A number that a branch's code goes by, as it is: keeps the compiler from turning that code into selects that every tile would pay for
-// (for a mask, 48 instructions for 32 x 32 scores beside the 72 that they need; two copies of the loop's body instead spill).
-__device__ __forceinline__ int branch_stays(int v) {
-  asm volatile("" : "+v"(v));
-  return v;
-}
-
 // store a transposed accumulator (rows = head columns, lane column = token) as bf16
 template <int D>
 __device__ __forceinline__ void store_rows(bf16_t* dst, const f32x16 (&acc)[D / 32], int h, float mul) {
@@ -152,7 +146,7 @@ __global__ __launch_bounds__(256, 2) void packed_fwd_kernel(PackedAttention p, i
   __shared__ __attribute__((aligned(1024))) bf16_t tiles[2][2][Tile<D>::SIZE];   // [buffer][K, V]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), ql = lane & 31, h = lane >> 5;
   PackedPlace w;
-  if (!packed_place<BM, CAUSAL>(p, slots, w)) return;
+  if (!packed_place<BM, CAUSAL>(p, slots, blockIdx.x, w)) return;
   const int w0 = w.row + wave * 32, qi = w0 + ql, qc = min(qi, w.n - 1);
   const float c2 = p.scale * LOG2E;                   // exp(scale * s - x) == exp2(c2 * s - LOG2E * x)
 
@@ -173,29 +167,30 @@ __global__ __launch_bounds__(256, 2) void packed_fwd_kernel(PackedAttention p, i
   ks.init((const bf16_t*)p.k + w.first * p.ldk + w.kv * D, (int)p.ldk);
   vs.init((const bf16_t*)p.v + w.first * p.ldv + w.kv * D, (int)p.ldv);
   const uint32_t lds = l_lds_address(&tiles[0][0][0]);
-  auto fetch = [&](int k0, int buf) {
-    tk.load(ks.at(k0), ks.bytes(w.n - k0), wave, lds + (uint32_t)buf * (4u * Tile<D>::SIZE));
-    tv.load(vs.at(k0), vs.bytes(w.n - k0), wave, lds + (uint32_t)buf * (4u * Tile<D>::SIZE) + 2u * Tile<D>::SIZE);
-  };
-  auto step = [&](int k0, int buf) __attribute__((always_inline)) {
-    const bool edge = k0 + TK > w.n || (CAUSAL && k0 + TK - 1 > w0);
-    const bf16_t *Ks = tiles[buf][0], *Vs = tiles[buf][1];
-    f32x16 s[2];
-    float mx = -INFINITY;
+  auto fetch_k = [&](int k0, int buf) { tk.load(ks.at(k0), ks.bytes(w.n - k0), wave, lds + (uint32_t)buf * (4u * Tile<D>::SIZE)); };
+  auto fetch_v = [&](int k0, int buf) { tv.load(vs.at(k0), vs.bytes(w.n - k0), wave, lds + (uint32_t)buf * (4u * Tile<D>::SIZE) + 2u * Tile<D>::SIZE); };
+  f32x16 s[2];                                        // the tile's scores
+  auto scores = [&](int buf, f32x16 (&to)[2]) __attribute__((always_inline)) {
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
-      zero(s[kb]);
+      zero(to[kb]);
 #pragma unroll
-      for (int kk = 0; kk < KK; ++kk) s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tk.row(Ks, kb, kk), qf[kk], s[kb], 0, 0, 0);
+      for (int kk = 0; kk < KK; ++kk) to[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tk.row(tiles[buf][0], kb, kk), qf[kk], to[kb], 0, 0, 0);
     }
+  };
+  // A tile's scores are made while the exponentials of the one before are: a wave's products and its vector instructions then run side
+  // by side, and not only those of the other wave on its SIMD.
+  auto step = [&](int k0, int buf) __attribute__((always_inline)) {
+    const bool edge = k0 + TK > w.n || (CAUSAL && k0 + TK - 1 > w0);
     if (edge) {                                       // the tile touches the mask
-      const int end = branch_stays((CAUSAL ? min(w.n, qi + 1) : w.n) - k0 - 4 * h);
+      const int end = (CAUSAL ? min(w.n, qi + 1) : w.n) - k0 - 4 * h;
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
         for (int r = 0; r < 16; ++r)
           if (32 * kb + 8 * (r >> 2) + (r & 3) >= end) s[kb][r] = -INFINITY;
     }
+    float mx = -INFINITY;
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -211,6 +206,8 @@ __global__ __launch_bounds__(256, 2) void packed_fwd_kernel(PackedAttention p, i
         for (int r = 0; r < 16; ++r) o[db][r] *= alpha;
       m = mnew;
     }
+    f32x16 next[2];
+    scores(buf ^ 1, next);                            // (behind the last tile: of whatever is there, unused)
     const float off = -mnew * c2;
     float rs = 0.f;
 #pragma unroll
@@ -230,15 +227,30 @@ __global__ __launch_bounds__(256, 2) void packed_fwd_kernel(PackedAttention p, i
         const bf16x8 pf = regs_to_frag(s[kb], c);
 #pragma unroll
         for (int db = 0; db < DB; ++db)
-          o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tv.column(Vs, db, 32 * kb + 16 * c), pf, o[db], 0, 0, 0);
+          o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tv.column(tiles[buf][1], db, 32 * kb + 16 * c), pf, o[db], 0, 0, 0);
       }
+    s[0] = next[0];
+    s[1] = next[1];
   };
-  fetch(0, 0);
-  for (int k0 = 0, buf = 0; k0 < kend; k0 += TK, buf ^= 1) {
-    landed();
-    if (k0 + TK < kend) fetch(k0 + TK, buf ^ 1);
-    if (w0 < w.n && !(CAUSAL && k0 > w0 + 31)) step(k0, buf);   // else none of this wave's queries sees the tile
+  fetch_k(0, 0);
+  fetch_v(0, 0);
+  if (TK < kend) fetch_k(TK, 1);
+  landed();
+  if (w0 < w.n) scores(0, s);
+  meet();                                             // the first tile of K is used up
+  // the tiles that this wave's queries see, then those that only other waves' do
+  const int seen = w0 >= w.n ? 0 : CAUSAL ? min(kend, w0 + 32) : kend;
+  int k0 = 0, buf = 0;
+  auto turn = [&]() __attribute__((always_inline)) {
+    if (k0 > 0) landed();
+    if (k0 + 2 * TK < kend) fetch_k(k0 + 2 * TK, buf);
+    if (k0 + TK < kend) fetch_v(k0 + TK, buf ^ 1);
+  };
+  for (; k0 < seen; k0 += TK, buf ^= 1) {
+    turn();
+    step(k0, buf);
   }
+  for (; k0 < kend; k0 += TK, buf ^= 1) turn();
   if (qi < w.n) {
     store_rows<D>((bf16_t*)p.out + (w.first + qi) * p.ldo + w.head * D, o, h, 1.f / l);
     if (h == 0) p.lse[(int64_t)w.head * p.T + w.first + qi] = m * p.scale + __logf(l);
@@ -246,17 +258,17 @@ __global__ __launch_bounds__(256, 2) void packed_fwd_kernel(PackedAttention p, i
 }
 
 // ------------------------------------------------------------------ dQ
-template <int D, bool CAUSAL>
-__global__ __launch_bounds__(256, 2) void packed_bwd_dq_kernel(PackedAttention p, int slots) {
-  constexpr int KK = D / 16, DB = D / 32;
-  __shared__ __attribute__((aligned(1024))) bf16_t tiles[2][2][Tile<D>::SIZE];   // [buffer][K, V]
+// smem: [buffer][K, V].  TELL: delta is written out for the keys' gradients, which are made after.
+template <int D, bool CAUSAL, bool TELL>
+__device__ __forceinline__ void bwd_dq(const PackedAttention& p, int slots, int block, bf16_t* smem) {
+  constexpr int KK = D / 16, DB = D / 32, SIZE = Tile<D>::SIZE;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), ql = lane & 31, h = lane >> 5;
   PackedPlace w;
-  if (!packed_place<BM, CAUSAL>(p, slots, w)) return;
+  if (!packed_place<BM, CAUSAL>(p, slots, block, w)) return;
   const int w0 = w.row + wave * 32, qi = w0 + ql, qc = min(qi, w.n - 1);
   const float c2 = p.scale * LOG2E;
 
-  // delta: each half of the wave holds half of the head's columns.  Written out for the dK/dV kernel, which runs after.
+  // delta: each half of the wave holds half of the head's columns
   bf16x8 qf[KK], gf[KK];
   float delta = 0.f;
   {
@@ -275,7 +287,7 @@ __global__ __launch_bounds__(256, 2) void packed_bwd_dq_kernel(PackedAttention p
   }
   delta += other_half(delta);
   const int64_t stat = (int64_t)w.head * p.T + w.first;
-  if (h == 0 && qi < w.n) p.delta[stat + qi] = delta;
+  if (TELL && h == 0 && qi < w.n) p.delta[stat + qi] = delta;
   const float nlse = -LOG2E * p.lse[stat + qc];
   f32x16 dq[DB];
 #pragma unroll
@@ -288,14 +300,14 @@ __global__ __launch_bounds__(256, 2) void packed_bwd_dq_kernel(PackedAttention p
   Stream ks, vs;
   ks.init((const bf16_t*)p.k + w.first * p.ldk + w.kv * D, (int)p.ldk);
   vs.init((const bf16_t*)p.v + w.first * p.ldv + w.kv * D, (int)p.ldv);
-  const uint32_t lds = l_lds_address(&tiles[0][0][0]);
+  const uint32_t lds = l_lds_address(smem);
   auto fetch = [&](int k0, int buf) {
-    tk.load(ks.at(k0), ks.bytes(w.n - k0), wave, lds + (uint32_t)buf * (4u * Tile<D>::SIZE));
-    tv.load(vs.at(k0), vs.bytes(w.n - k0), wave, lds + (uint32_t)buf * (4u * Tile<D>::SIZE) + 2u * Tile<D>::SIZE);
+    tk.load(ks.at(k0), ks.bytes(w.n - k0), wave, lds + (uint32_t)buf * (4u * SIZE));
+    tv.load(vs.at(k0), vs.bytes(w.n - k0), wave, lds + (uint32_t)buf * (4u * SIZE) + 2u * SIZE);
   };
   auto step = [&](int k0, int buf) __attribute__((always_inline)) {
     const bool edge = k0 + TK > w.n || (CAUSAL && k0 + TK - 1 > w0);
-    const bf16_t *Ks = tiles[buf][0], *Vs = tiles[buf][1];
+    const bf16_t *Ks = smem + buf * 2 * SIZE, *Vs = Ks + SIZE;
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
       f32x16 s, dp;
@@ -308,7 +320,7 @@ __global__ __launch_bounds__(256, 2) void packed_bwd_dq_kernel(PackedAttention p
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[r] = fast_exp2(fmaf(s[r], c2, nlse)) * (dp[r] - delta);
       if (edge) {
-        const int end = branch_stays((CAUSAL ? min(w.n, qi + 1) : w.n) - k0 - 32 * kb - 4 * h);
+        const int end = (CAUSAL ? min(w.n, qi + 1) : w.n) - k0 - 32 * kb - 4 * h;
 #pragma unroll
         for (int r = 0; r < 16; ++r)
           if (8 * (r >> 2) + (r & 3) >= end) s[r] = 0.f;
@@ -330,20 +342,27 @@ __global__ __launch_bounds__(256, 2) void packed_bwd_dq_kernel(PackedAttention p
   }
   if (qi < w.n) store_rows<D>((bf16_t*)p.dq + (w.first + qi) * p.lddq + w.head * D, dq, h, p.scale);
 }
+template <int D, bool CAUSAL>
+__global__ __launch_bounds__(256, 2) void packed_bwd_dq_kernel(PackedAttention p, int slots) {
+  __shared__ __attribute__((aligned(1024))) bf16_t tiles[4 * Tile<D>::SIZE];
+  bwd_dq<D, CAUSAL, true>(p, slots, blockIdx.x, tiles);
+}
 
 // ------------------------------------------------------------------ dK, dV
 // A block takes its keys through the query rows of every head that shares them.  G groups of KW waves, 32 keys to a wave: each
 // group has the same keys and every G-th tile of those rows, in tiles of its own, and their sums are added at the end in the groups' order.
-template <int D, bool CAUSAL, int KW, int G>
-__global__ __launch_bounds__(64 * KW * G, KW * G == 4 ? 2 : 1) void packed_bwd_dkv_kernel(PackedAttention p, int slots) {
+// smem: [group][buffer][Q, dO], and behind it lse and delta of the tiles' rows.  TOLD: delta is there; else the block makes it of dO and O.
+template <int D, int G> constexpr int dkv_elements() { return G * 4 * TK * D + G * 2 * 2 * TK * 2; }
+template <int D, bool CAUSAL, int KW, int G, bool TOLD>
+__device__ __forceinline__ void bwd_dkv(const PackedAttention& p, int slots, int block, bf16_t* smem) {
   constexpr int KK = D / 16, DB = D / 32, BN = 32 * KW;
   typedef Tile<D, KW> T;
-  __shared__ __attribute__((aligned(1024))) bf16_t tiles[G][2][2][T::SIZE];      // [group][buffer][Q, dO]
-  __shared__ __attribute__((aligned(16))) float lse_s[G][2][TK], delta_s[G][2][TK];
   const int tid = threadIdx.x, lane = tid & 63, all = __builtin_amdgcn_readfirstlane(tid >> 6), kl = lane & 31, h = lane >> 5;
   const int g = all / KW, wave = all - g * KW;
   PackedPlace w;
-  if (!packed_place_kv<BN, CAUSAL>(p, slots, w)) return;
+  if (!packed_place_kv<BN, CAUSAL>(p, slots, block, w)) return;
+  bf16_t* const tiles = smem + g * (4 * T::SIZE);
+  float *const lse_s = (float*)(smem + G * 4 * T::SIZE) + g * (4 * TK), *const delta_s = lse_s + 2 * TK;   // [buffer][row]
   const int w0 = w.row + wave * 32, ki = w0 + kl, kc = min(ki, w.n - 1);
   const float c2 = p.scale * LOG2E;
 
@@ -369,7 +388,7 @@ __global__ __launch_bounds__(64 * KW * G, KW * G == 4 ? 2 : 1) void packed_bwd_d
   Stream qs, gs;
   qs.init((const bf16_t*)p.q + w.first * p.ldq + w.kv * group * D, (int)p.ldq);
   gs.init((const bf16_t*)p.dout + w.first * p.lddo + w.kv * group * D, (int)p.lddo);
-  const uint32_t lds = l_lds_address(&tiles[0][0][0][0]) + (uint32_t)g * (8u * T::SIZE);
+  const uint32_t lds = l_lds_address(tiles);
   const int64_t stats = (int64_t)w.kv * group * p.T + w.first;
   const int mine = tid - g * (64 * KW);               // thread of the group
   float pre_lse = 0.f, pre_delta = 0.f;
@@ -382,15 +401,32 @@ __global__ __launch_bounds__(64 * KW * G, KW * G == 4 ? 2 : 1) void packed_bwd_d
       const uint64_t at = (uint64_t)head * (D * 2u);
       tq.load(qs.at(q0) + at, qs.bytes(w.n - q0), wave, lds + (uint32_t)buf * (4u * T::SIZE));
       tg.load(gs.at(q0) + at, gs.bytes(w.n - q0), wave, lds + (uint32_t)buf * (4u * T::SIZE) + 2u * T::SIZE);
-      if (mine < TK) {
-        const int q = min(q0 + mine, w.n - 1);
+      if (TOLD) {
+        if (mine < TK) {
+          const int64_t q = stats + (int64_t)head * p.T + min(q0 + mine, w.n - 1);
+          pre_lse = p.lse[q];
+          pre_delta = p.delta[q];
+        }
+      } else {                                        // KW threads to a row
+        const int64_t q = min(q0 + mine / KW, w.n - 1);
+        const int column = (w.kv * group + head) * D + mine % KW * (D / KW);
+        const bf16_t* grow = (const bf16_t*)p.dout + (w.first + q) * p.lddo + column;
+        const bf16_t* orow = (const bf16_t*)p.out + (w.first + q) * p.ldo + column;
         pre_lse = p.lse[stats + (int64_t)head * p.T + q];
-        pre_delta = p.delta[stats + (int64_t)head * p.T + q];
+        pre_delta = 0.f;
+#pragma unroll
+        for (int i = 0; i < D / KW / 8; ++i) {
+          const bf16x8 gv = *(const bf16x8*)(grow + 8 * i), ov = *(const bf16x8*)(orow + 8 * i);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) pre_delta = fmaf((float)ov[e], (float)gv[e], pre_delta);
+        }
+#pragma unroll
+        for (int s = 1; s < KW; s <<= 1) pre_delta += __shfl_xor(pre_delta, s);
       }
     }
   };
   auto step = [&](int at, int buf) __attribute__((always_inline)) {   // at: the tile's first row
-    const bf16_t *Qs = tiles[g][buf][0], *Gs = tiles[g][buf][1];
+    const bf16_t *Qs = tiles + buf * 2 * T::SIZE, *Gs = Qs + T::SIZE;
 #pragma unroll
     for (int qb = 0; qb < 2; ++qb) {
       f32x16 s, dp;
@@ -403,7 +439,7 @@ __global__ __launch_bounds__(64 * KW * G, KW * G == 4 ? 2 : 1) void packed_bwd_d
 #pragma unroll
       for (int q4 = 0; q4 < 4; ++q4) {
         const int qq = 32 * qb + 8 * q4 + 4 * h;
-        const float4 nl = *(const float4*)&lse_s[g][buf][qq], dl = *(const float4*)&delta_s[g][buf][qq];
+        const float4 nl = *(const float4*)&lse_s[buf * TK + qq], dl = *(const float4*)&delta_s[buf * TK + qq];
         const float nls[4] = {nl.x, nl.y, nl.z, nl.w}, dls[4] = {dl.x, dl.y, dl.z, dl.w};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -414,7 +450,7 @@ __global__ __launch_bounds__(64 * KW * G, KW * G == 4 ? 2 : 1) void packed_bwd_d
         }
       }
       if (CAUSAL && at < w0 + 31) {                   // the tile touches the mask
-        const int first = branch_stays(ki - at - 32 * qb - 4 * h);
+        const int first = ki - at - 32 * qb - 4 * h;
 #pragma unroll
         for (int r = 0; r < 16; ++r)
           if (8 * (r >> 2) + (r & 3) < first) { s[r] = 0.f; dp[r] = 0.f; }
@@ -437,7 +473,8 @@ __global__ __launch_bounds__(64 * KW * G, KW * G == 4 ? 2 : 1) void packed_bwd_d
     const int at = q0;
     // lse_s: ready for exp2, and minus infinity behind the sequence: probabilities of zero there.  This buffer was last
     // read two tiles ago, before the last barrier.
-    if (mine < TK) { lse_s[g][buf][mine] = at + mine < w.n ? -LOG2E * pre_lse : -INFINITY; delta_s[g][buf][mine] = pre_delta; }
+    const int r = TOLD ? mine : mine / KW;
+    if (r < TK && (TOLD || mine % KW == 0)) { lse_s[buf * TK + r] = at + r < w.n ? -LOG2E * pre_lse : -INFINITY; delta_s[buf * TK + r] = pre_delta; }
     landed();
     q0 += G * TK;
     settle();
@@ -456,7 +493,7 @@ __global__ __launch_bounds__(64 * KW * G, KW * G == 4 ? 2 : 1) void packed_bwd_d
   // Four registers at a time are a part: rows 8 (part % 4) + 4 h .. of 32 head columns.  Group g adds all groups' parts
   // of its share of them.
   constexpr int PARTS = 8 * DB, SHARE = PARTS / G;
-  float4* const parts = (float4*)&tiles[0][0][0][0];  // [group][wave][part][lane], as large as the tiles
+  float4* const parts = (float4*)smem;  // [group][wave][part][lane], as large as the tiles
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < PARTS; ++i) {
@@ -479,6 +516,19 @@ __global__ __launch_bounds__(64 * KW * G, KW * G == 4 ? 2 : 1) void packed_bwd_d
     if (ki < w.n) *(uint2*)((keys ? dk_row : dv_row) + column) = make_uint2(pack_bf16x2(s.x * mul, s.y * mul), pack_bf16x2(s.z * mul, s.w * mul));
   }
 }
+template <int D, bool CAUSAL, int KW, int G>
+__global__ __launch_bounds__(64 * KW * G, KW * G == 4 ? 2 : 1) void packed_bwd_dkv_kernel(PackedAttention p, int slots) {
+  __shared__ __attribute__((aligned(1024))) bf16_t smem[dkv_elements<D, G>()];
+  bwd_dkv<D, CAUSAL, KW, G, true>(p, slots, blockIdx.x, smem);
+}
+
+// Both in one launch, for few rows: the first `queries` blocks make dQ, the others dK and dV with a delta of their own.
+template <int D, bool CAUSAL>
+__global__ __launch_bounds__(256) void packed_bwd_small_kernel(PackedAttention p, int slots, int slots_kv, int queries) {
+  extern __shared__ __attribute__((aligned(1024))) bf16_t small_smem[];
+  if ((int)blockIdx.x < queries) bwd_dq<D, CAUSAL, false>(p, slots, blockIdx.x, small_smem);
+  else bwd_dkv<D, CAUSAL, 2, 2, false>(p, slots_kv, blockIdx.x - queries, small_smem);
+}
 
 // Heads of 128: a wave with both gradients of 32 keys would need more registers than let two waves run on a SIMD.  So a pair of waves
 // has the same 32 keys: the first makes S and P and holds dV, the second makes dP and dS and holds dK; P passes from the one to the other
@@ -494,7 +544,7 @@ __global__ __launch_bounds__(512) void packed_bwd_dkv_pair_kernel(PackedAttentio
   const int kw = wave & 3;
   const bool values = wave < 4;                       // holds dV
   PackedPlace w;
-  if (!packed_place_kv<BN, CAUSAL>(p, slots, w)) return;
+  if (!packed_place_kv<BN, CAUSAL>(p, slots, blockIdx.x, w)) return;
   const int w0 = w.row + kw * 32, ki = w0 + kl, kc = min(ki, w.n - 1);
   const float c2 = p.scale * LOG2E;
 
@@ -556,7 +606,7 @@ __global__ __launch_bounds__(512) void packed_bwd_dkv_pair_kernel(PackedAttentio
         }
       }
     if (CAUSAL && q0 < w0 + 31) {                     // the tile touches the mask
-      const int from = branch_stays(ki - q0 - 4 * h);
+      const int from = ki - q0 - 4 * h;
 #pragma unroll
       for (int qb = 0; qb < 2; ++qb)
 #pragma unroll
@@ -628,15 +678,25 @@ void launch_fwd(const PackedAttention& p, int causal, hipStream_t st) {
 }
 template <int D, bool CAUSAL>
 void launch_bwd(const PackedAttention& p, hipStream_t st) {
-  const int slots = packed_slots(p.T, p.n_seq, BM), kv = p.n_kv_heads;
-  hipLaunchKernelGGL((packed_bwd_dq_kernel<D, CAUSAL>), dim3(packed_blocks(slots, kv, p.n_heads / kv)), dim3(256), 0, st, p, slots);
+  const int slots = packed_slots(p.T, p.n_seq, BM), kv = p.n_kv_heads, small = packed_slots(p.T, p.n_seq, 64);
+  const unsigned queries = packed_blocks(slots, kv, p.n_heads / kv), keys = packed_blocks(small, kv, 1);
+  if (packed_bwd_small(p.T, queries + keys)) {
+    constexpr int LDS = std::max(4 * Tile<D>::SIZE, dkv_elements<D, 2>()) * 2;
+    static const bool configured = [] {
+      (void)hipFuncSetAttribute((const void*)packed_bwd_small_kernel<D, CAUSAL>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+      return true;
+    }();
+    (void)configured;
+    hipLaunchKernelGGL((packed_bwd_small_kernel<D, CAUSAL>), dim3(queries + keys), dim3(256), LDS, st, p, slots, small, (int)queries);
+    return;
+  }
+  hipLaunchKernelGGL((packed_bwd_dq_kernel<D, CAUSAL>), dim3(queries), dim3(256), 0, st, p, slots);
   if constexpr (D == 128) {
     hipLaunchKernelGGL((packed_bwd_dkv_pair_kernel<CAUSAL>), dim3(packed_blocks(slots, kv, 1)), dim3(512), 0, st, p, slots);
   } else if ((int64_t)slots * kv >= 1024) {           // two blocks and more for every place that there is
     hipLaunchKernelGGL((packed_bwd_dkv_kernel<D, CAUSAL, 4, 1>), dim3(packed_blocks(slots, kv, 1)), dim3(256), 0, st, p, slots);
   } else {
-    const int small = packed_slots(p.T, p.n_seq, 64);
-    hipLaunchKernelGGL((packed_bwd_dkv_kernel<D, CAUSAL, 2, 4>), dim3(packed_blocks(small, kv, 1)), dim3(512), 0, st, p, small);
+    hipLaunchKernelGGL((packed_bwd_dkv_kernel<D, CAUSAL, 2, 4>), dim3(keys), dim3(512), 0, st, p, small);
   }
 }
 }  // namespace

@@ -114,7 +114,7 @@ __global__ __launch_bounds__(64 * W) void packed_f32_fwd_kernel(PackedAttention 
   float* const mine = stat + W * 128;                 // a wave's tile, and its part of the sum afterwards
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, h = lane >> 5;
   PackedPlace w;
-  if (!packed_place<TR, CAUSAL>(p, slots, w)) return;
+  if (!packed_place<TR, CAUSAL>(p, slots, blockIdx.x, w)) return;
   const int qi = w.row + l32, last = w.n - 1;
   const float c2 = p.scale * LOG2E;
   const float* kb = (const float*)p.k + w.first * p.ldk + w.kv * D;
@@ -190,14 +190,14 @@ __global__ __launch_bounds__(64 * W) void packed_f32_fwd_kernel(PackedAttention 
 }
 
 // ------------------------------------------------------------------ dQ
-template <int D, bool CAUSAL, int W>
-__global__ __launch_bounds__(64 * W) void packed_f32_bwd_dq_kernel(PackedAttention p, int slots) {
+// TELL: delta is written out for the keys' gradients, which are made after.
+template <int D, bool CAUSAL, int W, bool TELL>
+__device__ __forceinline__ void f32_bwd_dq(const PackedAttention& p, int slots, int block, float* f_smem) {
   constexpr int TILE = tile_floats<D>();
-  extern __shared__ __attribute__((aligned(16))) float f_smem[];
   float *const own_q = f_smem, *const own_g = own_q + TILE, *const mine = own_g + TILE;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, h = lane >> 5;
   PackedPlace w;
-  if (!packed_place<TR, CAUSAL>(p, slots, w)) return;
+  if (!packed_place<TR, CAUSAL>(p, slots, block, w)) return;
   const int qi = w.row + l32, last = w.n - 1;
   const int64_t stats = (int64_t)w.head * p.T + w.first;
   const float* kb = (const float*)p.k + w.first * p.ldk + w.kv * D;
@@ -216,7 +216,7 @@ __global__ __launch_bounds__(64 * W) void packed_f32_bwd_dq_kernel(PackedAttenti
     stash<D>(own_g, l32, h, kf);
     fetch_rows<D>((const float*)p.q + w.first * p.ldq + w.head * D, p.ldq, w.row, last, l32, h, kf);
     stash<D>(own_q, l32, h, kf);
-    if (h == 0 && qi < w.n) p.delta[stats + qi] = delta;
+    if (TELL && h == 0 && qi < w.n) p.delta[stats + qi] = delta;
   }
   const float lse = p.lse[stats + min(qi, last)];
   const int kend = CAUSAL ? min(w.n, w.row + TR) : w.n;
@@ -256,16 +256,22 @@ __global__ __launch_bounds__(64 * W) void packed_f32_bwd_dq_kernel(PackedAttenti
   store_sum<D, W>(qi < w.n ? (float*)p.dq + (w.first + qi) * p.lddq + w.head * D : nullptr, mine, TILE, wave, lane, factor);
 }
 
-// ------------------------------------------------------------------ dK, dV
 template <int D, bool CAUSAL, int W>
-__global__ __launch_bounds__(64 * W) void packed_f32_bwd_dkv_kernel(PackedAttention p, int slots) {
-  constexpr int TILE = tile_floats<D>();
+__global__ __launch_bounds__(64 * W) void packed_f32_bwd_dq_kernel(PackedAttention p, int slots) {
   extern __shared__ __attribute__((aligned(16))) float f_smem[];
+  f32_bwd_dq<D, CAUSAL, W, true>(p, slots, blockIdx.x, f_smem);
+}
+
+// ------------------------------------------------------------------ dK, dV
+// TOLD: delta is there; else it is made of dO and O.
+template <int D, bool CAUSAL, int W, bool TOLD>
+__device__ __forceinline__ void f32_bwd_dkv(const PackedAttention& p, int slots, int block, float* f_smem) {
+  constexpr int TILE = tile_floats<D>();
   float *const own_k = f_smem, *const own_v = own_k + TILE, *const rowstat = own_v + TILE;   // rowstat [W][2][TR]: lse, delta of a tile
   float *const mine_q = rowstat + W * 2 * TR, *const mine_g = mine_q + W * TILE;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, h = lane >> 5;
   PackedPlace w;
-  if (!packed_place_kv<TR, CAUSAL>(p, slots, w)) return;
+  if (!packed_place_kv<TR, CAUSAL>(p, slots, block, w)) return;
   const int ki = w.row + l32, last = w.n - 1, group = p.n_heads / p.n_kv_heads;
   const float* qb = (const float*)p.q + w.first * p.ldq + w.kv * group * D;
   const float* gb = (const float*)p.dout + w.first * p.lddo + w.kv * group * D;
@@ -284,7 +290,21 @@ __global__ __launch_bounds__(64 * W) void packed_f32_bwd_dkv_kernel(PackedAttent
     const int head = t / per_head, q0 = qstart + (t - head * per_head) * TR;
     fetch_rows<D>(qb + head * D, p.ldq, q0, last, l32, h, qf);
     fetch_rows<D>(gb + head * D, p.lddo, q0, last, l32, h, gf);
-    pre = (h ? p.delta : p.lse)[stats + (int64_t)head * p.T + min(q0 + l32, last)];
+    const int64_t at = stats + (int64_t)head * p.T + min(q0 + l32, last);
+    if (TOLD) {
+      pre = (h ? p.delta : p.lse)[at];
+    } else {
+      Rows4<D> of;
+      fetch_rows<D>((const float*)p.out + w.first * p.ldo + (w.kv * group + head) * D, p.ldo, q0, last, l32, h, of);
+      float delta = 0.f;
+#pragma unroll
+      for (int g = 0; g < D / 8; ++g) {
+        delta = fmaf(gf[g].x, of[g].x, delta); delta = fmaf(gf[g].y, of[g].y, delta);
+        delta = fmaf(gf[g].z, of[g].z, delta); delta = fmaf(gf[g].w, of[g].w, delta);
+      }
+      delta += other_half(delta);
+      pre = h ? delta : p.lse[at];
+    }
   };
   int t = wave;
   if (t < tiles) fetch(t);
@@ -331,28 +351,47 @@ __global__ __launch_bounds__(64 * W) void packed_f32_bwd_dkv_kernel(PackedAttent
   store_sum<D, W>(real ? (float*)p.dv + (w.first + ki) * p.lddv + w.kv * D : nullptr, mine_g, TILE, wave, lane, one);
 }
 
+template <int D, bool CAUSAL, int W>
+__global__ __launch_bounds__(64 * W) void packed_f32_bwd_dkv_kernel(PackedAttention p, int slots) {
+  extern __shared__ __attribute__((aligned(16))) float f_smem[];
+  f32_bwd_dkv<D, CAUSAL, W, true>(p, slots, blockIdx.x, f_smem);
+}
+
+// Both in one launch, for few rows: the first `queries` blocks make dQ, the others dK and dV with a delta of their own.
+template <int D, bool CAUSAL, int W>
+__global__ __launch_bounds__(64 * W) void packed_f32_bwd_small_kernel(PackedAttention p, int slots, int queries) {
+  extern __shared__ __attribute__((aligned(16))) float f_smem[];
+  if ((int)blockIdx.x < queries) f32_bwd_dq<D, CAUSAL, W, false>(p, slots, blockIdx.x, f_smem);
+  else f32_bwd_dkv<D, CAUSAL, W, false>(p, slots, blockIdx.x - queries, f_smem);
+}
+
 namespace {
-template <auto K, int W, int FLOATS>
-void launch(unsigned blocks, const PackedAttention& p, int slots, hipStream_t st) {
+template <auto K, int W, int FLOATS, typename... A>
+void launch(unsigned blocks, hipStream_t st, A... a) {
   static const bool configured = [] {
     (void)hipFuncSetAttribute((const void*)K, hipFuncAttributeMaxDynamicSharedMemorySize, FLOATS * 4);
     return true;
   }();
   (void)configured;
-  hipLaunchKernelGGL(K, dim3(blocks), dim3(64 * W), FLOATS * 4, st, p, slots);
+  hipLaunchKernelGGL(K, dim3(blocks), dim3(64 * W), FLOATS * 4, st, a...);
 }
 template <int D, bool CAUSAL>
 void fwd(const PackedAttention& p, hipStream_t st) {
   constexpr int W = 2, T = tile_floats<D>();
   const int slots = packed_slots(p.T, p.n_seq, TR);
-  launch<packed_f32_fwd_kernel<D, CAUSAL, W>, W, T + W * 128 + W * T>(packed_blocks(slots, p.n_kv_heads, p.n_heads / p.n_kv_heads), p, slots, st);
+  launch<packed_f32_fwd_kernel<D, CAUSAL, W>, W, T + W * 128 + W * T>(packed_blocks(slots, p.n_kv_heads, p.n_heads / p.n_kv_heads), st, p, slots);
 }
 template <int D, bool CAUSAL>
 void bwd(const PackedAttention& p, hipStream_t st) {
-  constexpr int W = 2, T = tile_floats<D>();
+  constexpr int W = 2, T = tile_floats<D>(), WS = D == 128 ? 2 : 4;
   const int slots = packed_slots(p.T, p.n_seq, TR);
-  launch<packed_f32_bwd_dq_kernel<D, CAUSAL, W>, W, 2 * T + W * T>(packed_blocks(slots, p.n_kv_heads, p.n_heads / p.n_kv_heads), p, slots, st);
-  launch<packed_f32_bwd_dkv_kernel<D, CAUSAL, W>, W, 2 * T + W * 2 * TR + 2 * W * T>(packed_blocks(slots, p.n_kv_heads, 1), p, slots, st);
+  const unsigned queries = packed_blocks(slots, p.n_kv_heads, p.n_heads / p.n_kv_heads), keys = packed_blocks(slots, p.n_kv_heads, 1);
+  if (packed_bwd_small(p.T, queries + keys)) {
+    launch<packed_f32_bwd_small_kernel<D, CAUSAL, WS>, WS, 2 * T + WS * 2 * TR + 2 * WS * T>(queries + keys, st, p, slots, (int)queries);
+    return;
+  }
+  launch<packed_f32_bwd_dq_kernel<D, CAUSAL, W>, W, 2 * T + W * T>(queries, st, p, slots);
+  launch<packed_f32_bwd_dkv_kernel<D, CAUSAL, W>, W, 2 * T + W * 2 * TR + 2 * W * T>(keys, st, p, slots);
 }
 }  // namespace
 

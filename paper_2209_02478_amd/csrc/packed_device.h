@@ -22,6 +22,9 @@ inline int packed_slots(int64_t T, int64_t n_seq, int M) { return (int)packed_sl
 // heads of keys spread over the XCDs.
 inline unsigned packed_blocks(int slots, int kv_heads, int group) { return (unsigned)((((int64_t)slots * kv_heads + 7) / 8) * 8 * group); }
 
+// Whether a backward pass is made by one launch whose blocks for the keys make their own delta, and not by two that wait for each other.
+inline bool packed_bwd_small(int T, unsigned blocks) { return T <= 1024 && blocks <= 512; }
+
 // ends[s - 1], held to 0 .. T: whatever the array holds, no row outside the caller's is touched
 __device__ __forceinline__ int packed_end(const PackedAttention& p, int s) { return s > 0 ? min(max(p.ends[s - 1], 0), p.T) : 0; }
 
@@ -109,9 +112,9 @@ __device__ __forceinline__ bool packed_rows(const PackedAttention& p, int slots,
 
 // A block of one query head; false: it has no rows.
 template <int M, bool CAUSAL>
-__device__ __forceinline__ bool packed_place(const PackedAttention& p, int slots, PackedPlace& w) {
-  const int group = p.n_heads / p.n_kv_heads, i = blockIdx.x >> 3;
-  const int unit = i / group * 8 + (blockIdx.x & 7), slot = unit / p.n_kv_heads;
+__device__ __forceinline__ bool packed_place(const PackedAttention& p, int slots, int block, PackedPlace& w) {
+  const int group = p.n_heads / p.n_kv_heads, i = block >> 3;
+  const int unit = i / group * 8 + (block & 7), slot = unit / p.n_kv_heads;
   if (slot >= slots) return false;
   w.kv = __builtin_amdgcn_readfirstlane(unit - slot * p.n_kv_heads);
   w.head = __builtin_amdgcn_readfirstlane(w.kv * group + i % group);
@@ -119,10 +122,10 @@ __device__ __forceinline__ bool packed_place(const PackedAttention& p, int slots
 }
 // A block of all query heads of one head of keys.
 template <int M, bool CAUSAL>
-__device__ __forceinline__ bool packed_place_kv(const PackedAttention& p, int slots, PackedPlace& w) {
-  const int slot = (int)blockIdx.x / p.n_kv_heads;
+__device__ __forceinline__ bool packed_place_kv(const PackedAttention& p, int slots, int block, PackedPlace& w) {
+  const int slot = block / p.n_kv_heads;
   if (slot >= slots) return false;
-  w.kv = __builtin_amdgcn_readfirstlane((int)blockIdx.x - slot * p.n_kv_heads);
+  w.kv = __builtin_amdgcn_readfirstlane(block - slot * p.n_kv_heads);
   w.head = w.kv * (p.n_heads / p.n_kv_heads);
   return packed_rows<M, CAUSAL>(p, slots, __builtin_amdgcn_readfirstlane(slot), true, w);
 }

@@ -95,7 +95,7 @@ def within(got, ref, off, name):
     assert not bad.any(), (name, int(bad.sum()), float((np.abs(got - ref) / (off + 1e-37)).max()), np.argwhere(bad)[:3].tolist())
 
 
-LENGTHS = [[1], [2], [17], [0, 1, 0, 3, 0], [31, 32, 33], [63, 64, 65], [127, 128, 129, 1], [300], [5] * 9 + [200, 0, 77]]
+LENGTHS = [[1], [2], [17], [700, 1, 0, 65, 333], [0, 1, 0, 3, 0], [31, 32, 33], [63, 64, 65], [127, 128, 129, 1], [300], [5] * 9 + [200, 0, 77]]
 
 
 @pytest.mark.parametrize("causal", [0, 1])
