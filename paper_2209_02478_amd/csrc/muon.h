@@ -20,7 +20,7 @@ struct MuonMatrix {
   int32_t mp, np;                       // the smaller side and the larger, rounded up to whole tiles
 };
 struct MuonChunk { int32_t matrix, pad; int64_t start; };
-struct MuonTile { int32_t matrix; uint16_t i, j; };          // row and column of tiles
+struct MuonTile { int32_t matrix; uint16_t i, j; };          // row and column of tiles; matrix below 0: none
 struct MuonHyper { float lr, momentum, weight_decay, rms, eps; int nesterov, iterations; };
 
 inline const char* bad_muon(float lr, float momentum, float weight_decay, float rms, float eps, int iterations) {
@@ -33,8 +33,6 @@ inline const char* bad_muon(float lr, float momentum, float weight_decay, float 
 inline bool muon_small(int64_t rows, int64_t cols) {
   return (rows < cols ? rows : cols) <= kMuonSmallShort && (rows < cols ? cols : rows) <= kMuonSmallLong;
 }
-// whether a matrix takes the products' large tiles
-inline bool muon_large(int64_t rows, int64_t cols) { return (rows < cols ? rows : cols) > 512; }
 // The first `count` matrices of a table, small ones, which need no scratch.
 void muon_update_small(const MuonMatrix* mats, int count, const MuonHyper& h, hipStream_t st);
 constexpr int kMuonBlocks = 256;        // blocks of a product on large tiles: one to a compute unit, ids go to the 8 XCDs in turn

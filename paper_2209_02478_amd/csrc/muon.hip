@@ -126,12 +126,15 @@ __global__ __launch_bounds__(256) void muon_momentum_kernel(const MuonMatrix* ma
   if (threadIdx.x == 0) ((double*)(ws + t.partial))[c.start / chunk] = sum;
 }
 
-// X = u / (|u| + eps), 128 x 128 of it a block, zeros behind the matrix' last row and column.  A thread takes 4 x 4 elements at a
-// time, eight loads in flight, and turns them in registers where X is the matrix turned.
+// X = u / (|u| + eps), 128 x 128 of it to STRIPS blocks, zeros behind the matrix' last row and column.  A thread takes 4 x 4 elements at a
+// time, eight loads in flight, and turns them in registers where X is the matrix turned.  Four strips of 32 rows where the tiles are too few
+// to keep the memory busy.
+template <int STRIPS>
 __global__ __launch_bounds__(256) void muon_start_kernel(const MuonMatrix* mats, const MuonTile* tiles, char* ws, MuonHyper h) {
   __shared__ double lds[4];
   __shared__ __attribute__((aligned(16))) f16 turn[kMuonTile * kMuonTile];
-  const MuonTile tile = tiles[blockIdx.x];
+  const MuonTile tile = tiles[blockIdx.x / STRIPS];
+  if (tile.matrix < 0) return;
   const MuonMatrix& t = mats[tile.matrix];
   const int rows = t.rows, cols = t.cols, np = t.np, tid = threadIdx.x;
   const int64_t n = (int64_t)rows * cols;
@@ -145,7 +148,8 @@ __global__ __launch_bounds__(256) void muon_start_kernel(const MuonMatrix* mats,
   const int r0 = (tall ? tile.j : tile.i) * kMuonTile, c = (tid & 31) * 4, at = (tall ? tile.i : tile.j) * kMuonTile + c;   // of u
   const float *const grad = t.grad, *const mom = t.momentum;
   const bool whole = at - c + kMuonTile <= cols;
-  for (int k = 0; k < 4; ++k) {
+  const int strip = blockIdx.x % STRIPS * (4 / STRIPS);        // the block's first 32 rows of four
+  for (int k = strip; k < strip + 4 / STRIPS; ++k) {
     const int r = k * 32 + (tid >> 5) * 4;
     f32x4 g[4], m[4];
 #pragma unroll
@@ -169,15 +173,18 @@ __global__ __launch_bounds__(256) void muon_start_kernel(const MuonMatrix* mats,
   }
   if (!tall) return;
   __syncthreads();
+  constexpr int PIECES = 32 / STRIPS;                          // of four elements, of a row of X
 #pragma unroll 4
-  for (int k = 0; k < 16; ++k) {
-    const int i = k * 8 + (tid >> 5);
-    *(f16x4*)(x + (int64_t)i * np + c) = *(const f16x4*)&turn[turn_at(i, tid & 31)];
+  for (int k = 0; k < 16 / STRIPS; ++k) {
+    const int i = k * (256 / PIECES) + tid / PIECES, piece = strip * 8 + tid % PIECES;
+    *(f16x4*)(x + (int64_t)i * np + 4 * piece) = *(const f16x4*)&turn[turn_at(i, piece)];
   }
 }
 
 // STAGE 1: A = X X^T.  2: B = a I + b A + c A A.  3: X' = B X.  A block makes 128 x 128; for matrices of which larger tiles would be
-// mostly padding, or too few (muon_large).
+// mostly padding, or too few.  Two slots of 64 reduction indices, two blocks to a compute unit.  Bound by the LDS: 96 KB go through it for
+// 64 indices, 0.5 us of a unit with the meetings; a ring of four slots changes nothing (5 layers of 301, 77 and 999: first product 14.3 and
+// 14.5 us), nor do eight waves.  A launch costs 7 us beside that: its start and end, two table entries and the first tile from memory.
 template <int STAGE>
 __global__ __launch_bounds__(256, 2) void muon_product_kernel(const MuonMatrix* mats, const MuonTile* tiles, char* ws, int from) {
   using namespace large;
@@ -185,8 +192,9 @@ __global__ __launch_bounds__(256, 2) void muon_product_kernel(const MuonMatrix* 
   constexpr bool KM = STAGE != 3;
   typedef LTileOf<true, R> TA;
   typedef LTileOf<KM, R> TB;
-  __shared__ __attribute__((aligned(1024))) f16 smem[2][2][SIZE];
+  __shared__ __attribute__((aligned(1024))) f16 smem[2 * 2 * SIZE];   // [slot][A, B]
   const MuonTile tile = tiles[blockIdx.x];
+  if (tile.matrix < 0) return;
   const MuonMatrix& t = mats[tile.matrix];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave >> 1, wn = wave & 1;
   const int mp = __builtin_amdgcn_readfirstlane(t.mp), np = __builtin_amdgcn_readfirstlane(t.np);
@@ -207,12 +215,14 @@ __global__ __launch_bounds__(256, 2) void muon_product_kernel(const MuonMatrix* 
     off_b[j] = TB::src(ldb, R, wave * 4 + j, lane);
   }
   const uint64_t step_a = BK * 2, step_b = KM ? BK * 2 : (uint64_t)BK * 2 * ldb;
-  const uint32_t lds = l_lds_address(&smem[0][0][0]) + (uint32_t)wave * 4096u;
-  auto fetch = [&](int buf) {
+  const uint32_t lds = l_lds_address(smem) + (uint32_t)wave * 4096u;
+  const int steps = (K + BK - 1) / BK;
+  auto fetch = [&](int slot) {
+    const uint32_t to = lds + (uint32_t)slot * (4u * SIZE);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) l_direct_load(base_a, bytes_a, off_a[j], lds + (uint32_t)buf * (4u * SIZE) + j * 1024u);
+    for (int j = 0; j < 4; ++j) l_direct_load(base_a, bytes_a, off_a[j], to + j * 1024u);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) l_direct_load(base_b, bytes_b, off_b[j], lds + (uint32_t)buf * (4u * SIZE) + 2u * SIZE + j * 1024u);
+    for (int j = 0; j < 4; ++j) l_direct_load(base_b, bytes_b, off_b[j], to + 2u * SIZE + j * 1024u);
     base_a += step_a;
     base_b += step_b;
   };
@@ -225,19 +235,19 @@ __global__ __launch_bounds__(256, 2) void muon_product_kernel(const MuonMatrix* 
   for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const int steps = (K + BK - 1) / BK;
   fetch(0);
-  for (int k = 0, buf = 0; k < steps; ++k, buf ^= 1) {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (k + 1 < steps) fetch(buf ^ 1);
+  for (int k = 0; k < steps; ++k) {
+    __builtin_amdgcn_s_waitcnt(in_flight(0));
+    __syncthreads();                                         // (every wave is done reading the slot that is filled next)
+    if (k + 1 < steps) fetch(k + 1 & 1);
+    const bf16_t* const sa = (const bf16_t*)(smem + (k & 1) * 2 * SIZE);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       f16x8 af[4], bf[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) af[i] = __builtin_bit_cast(f16x8, fa.read((const bf16_t*)&smem[buf][0][0], 0, i, h));
+      for (int i = 0; i < 4; ++i) af[i] = __builtin_bit_cast(f16x8, fa.read(sa, 0, i, h));
 #pragma unroll
-      for (int j = 0; j < 4; ++j) bf[j] = __builtin_bit_cast(f16x8, fb.read((const bf16_t*)&smem[buf][1][0], 0, j, h));
+      for (int j = 0; j < 4; ++j) bf[j] = __builtin_bit_cast(f16x8, fb.read(sa + SIZE, 0, j, h));
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -246,7 +256,7 @@ __global__ __launch_bounds__(256, 2) void muon_product_kernel(const MuonMatrix* 
   }
   __syncthreads();
   // through LDS: row i of the tile in a row of 128 columns, 8-byte pieces permuted by the row
-  f16* const out = &smem[0][0][0];
+  f16* const out = smem;
   const int lr = lane & 15, lq = lane >> 4;
   auto at = [](int row, int piece) { return row * R + ((piece ^ (row & 31)) << 2); };
 #pragma unroll
@@ -289,9 +299,11 @@ __global__ __launch_bounds__(256, 2) void muon_product_kernel(const MuonMatrix* 
 }
 
 // The weights' step from the finished X, in the same blocks of 4 x 4 elements as the start.
+template <int STRIPS>
 __global__ __launch_bounds__(256) void muon_apply_kernel(const MuonMatrix* mats, const MuonTile* tiles, const char* ws, MuonHyper h, int from) {
   __shared__ __attribute__((aligned(16))) f16 turn[kMuonTile * kMuonTile];
-  const MuonTile tile = tiles[blockIdx.x];
+  const MuonTile tile = tiles[blockIdx.x / STRIPS];
+  if (tile.matrix < 0) return;
   const MuonMatrix& t = mats[tile.matrix];
   const int rows = t.rows, cols = t.cols, np = t.np, tid = threadIdx.x, c = (tid & 31) * 4;
   const bool tall = rows > cols;
@@ -301,15 +313,17 @@ __global__ __launch_bounds__(256) void muon_apply_kernel(const MuonMatrix* mats,
   float* const master = t.master;
   uint16_t* const lowp = t.lowp;
   const bool whole = at - c + kMuonTile <= cols;
+  const int strip = blockIdx.x % STRIPS * (4 / STRIPS);        // the block's first 32 rows of four
   if (tall) {
+    constexpr int PIECES = 32 / STRIPS;                        // of four elements, of a row of X
 #pragma unroll 4
-    for (int k = 0; k < 16; ++k) {
-      const int i = k * 8 + (tid >> 5);
-      *(f16x4*)&turn[turn_at(i, tid & 31)] = *(const f16x4*)(x + (int64_t)i * np + c);
+    for (int k = 0; k < 16 / STRIPS; ++k) {
+      const int i = k * (256 / PIECES) + tid / PIECES, piece = strip * 8 + tid % PIECES;
+      *(f16x4*)&turn[turn_at(i, piece)] = *(const f16x4*)(x + (int64_t)i * np + 4 * piece);
     }
     __syncthreads();
   }
-  for (int k = 0; k < 4; ++k) {
+  for (int k = strip; k < strip + 4 / STRIPS; ++k) {
     const int r = k * 32 + (tid >> 5) * 4;
     f32x4 w[4];
     f16x4 s[4];
@@ -330,13 +344,15 @@ __global__ __launch_bounds__(256) void muon_apply_kernel(const MuonMatrix* mats,
   }
 }
 
+constexpr int kSmallThreads = 1024;
 // A matrix of at most 128 x 256 (or turned) in one block: X, A and B stay in LDS, and the whole update is one launch.  Rows of X, A
 // and B are 16 bytes longer than their elements, so that neither the fragments' rows nor their columns meet in a bank.  The gradient
 // and the momentum are read twice, before and behind the norm, the second time out of the caches: held in registers they make the
 // code so long that fetching it takes longer.
-__global__ __launch_bounds__(512) void muon_small_kernel(const MuonMatrix* mats, MuonHyper h) {
+__global__ __launch_bounds__(kSmallThreads) void muon_small_kernel(const MuonMatrix* mats, MuonHyper h) {
   extern __shared__ __attribute__((aligned(16))) f16 s_smem[];
-  __shared__ double lds[8];
+  constexpr int WAVES = kSmallThreads / 64;
+  __shared__ double lds[WAVES];
   constexpr int PX = kMuonSmallLong + 8, PA = kMuonSmallShort + 8;
   f16 *const X = s_smem, *const A = X + kMuonSmallShort * PX, *const B = A + kMuonSmallShort * PA;
   const MuonMatrix& t = mats[blockIdx.x];
@@ -345,7 +361,7 @@ __global__ __launch_bounds__(512) void muon_small_kernel(const MuonMatrix* mats,
   const bool tall = rows > cols;
   const int m64 = (min(rows, cols) + 63) / 64 * 64, n64 = (max(rows, cols) + 63) / 64 * 64;   // what there is of X, with zeros behind
   // a lane takes four elements of a row, as many lanes as the row needs (a power of two), rows `apart` apart four at a time
-  const int lanes = cols <= 16 ? 2 : cols <= 32 ? 3 : cols <= 64 ? 4 : cols <= 128 ? 5 : 6, apart = 512 >> lanes;
+  const int lanes = cols <= 16 ? 2 : cols <= 32 ? 3 : cols <= 64 ? 4 : cols <= 128 ? 5 : 6, apart = kSmallThreads >> lanes;
   const int c = 4 * (tid & ((1 << lanes) - 1)), mine = tid >> lanes, many = min(max(cols - c, 0), 4);
   const float *const grad = t.grad;
   float *const mom = t.momentum, *const master = t.master;
@@ -371,8 +387,8 @@ __global__ __launch_bounds__(512) void muon_small_kernel(const MuonMatrix* mats,
         for (int e = 0; e < 4; ++e) sum += (double)u[e] * u[e];
       }
   }
-  for (int i = tid; i < m64 * PX / 8; i += 512) ((f16x8*)X)[i] = f16x8{};
-  const float inv = (float)((double)kHeld / (sqrt(block_sum<8>(sum, lds)) + (double)h.eps));
+  for (int i = tid; i < m64 * PX / 8; i += kSmallThreads) ((f16x8*)X)[i] = f16x8{};
+  const float inv = (float)((double)kHeld / (sqrt(block_sum<WAVES>(sum, lds)) + (double)h.eps));
   for (int r0 = mine; r0 < rows; r0 += 4 * apart) {
     f32x4 g[4], m[4];
     if (many)
@@ -392,7 +408,7 @@ __global__ __launch_bounds__(512) void muon_small_kernel(const MuonMatrix* mats,
   auto row_frag = [&](const f16* s, int pitch, int block, int k) { return *(const f16x8*)(s + (block * 16 + lr) * pitch + k + 8 * lq); };
   // a symmetric product of S's rows with themselves (A: of X's, K = n64; B: of A's, K = m64), tiles on and above the diagonal
   auto symmetric = [&](const f16* S, int pitch, int K, f16* to, bool second) {
-    for (int q = wave; q < mt * (mt + 1) / 2; q += 8) {
+    for (int q = wave; q < mt * (mt + 1) / 2; q += WAVES) {
       int i = 0, left = q;
       while (left >= mt - i) { left -= mt - i; ++i; }
       const int j = i + left;
@@ -421,7 +437,7 @@ __global__ __launch_bounds__(512) void muon_small_kernel(const MuonMatrix* mats,
     symmetric(A, PA, m64, B, true);
     __syncthreads();
     // X' = B X: 16 columns of X' come from the same 16 of X, which only their wave reads and writes
-    for (int j = wave; j < nt; j += 8) {
+    for (int j = wave; j < nt; j += WAVES) {
       f32x4 acc[kMuonSmallShort / 16];
 #pragma unroll
       for (int i = 0; i < kMuonSmallShort / 16; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -471,24 +487,31 @@ void muon_update_small(const MuonMatrix* mats, int count, const MuonHyper& h, hi
     return true;
   }();
   (void)configured;
-  hipLaunchKernelGGL(muon_small_kernel, dim3(count), dim3(512), LDS, st, mats, h);
+  hipLaunchKernelGGL(muon_small_kernel, dim3(count), dim3(kSmallThreads), LDS, st, mats, h);
+}
+
+template <int STAGE>
+static void product(const MuonMatrix* mats, const MuonUnits& u, char* ws, int from, hipStream_t st) {
+  if (u.large[STAGE - 1]) muon_large_product(STAGE, mats, u.large_tiles[STAGE - 1], u.large[STAGE - 1], ws, from, st);
+  const int n = STAGE == 3 ? u.n_full : u.n_tri;
+  if (n) hipLaunchKernelGGL((muon_product_kernel<STAGE>), dim3(n), dim3(256), 0, st, mats, STAGE == 3 ? u.full : u.tri, ws, from);
 }
 
 void muon_update(const MuonMatrix* mats, const MuonUnits& u, void* workspace, const MuonHyper& h, hipStream_t st) {
   if (u.n_chunks < 1) return;
   char* const ws = (char*)workspace;
+  const bool strips = u.n_cells < 1024;
   hipLaunchKernelGGL(muon_momentum_kernel, dim3(u.n_chunks), dim3(256), 0, st, mats, u.chunks, ws, h);
-  hipLaunchKernelGGL(muon_start_kernel, dim3(u.n_cells), dim3(256), 0, st, mats, u.cells, ws, h);
+  if (strips) hipLaunchKernelGGL((muon_start_kernel<4>), dim3(4 * u.n_cells), dim3(256), 0, st, mats, u.cells, ws, h);
+  else hipLaunchKernelGGL((muon_start_kernel<1>), dim3(u.n_cells), dim3(256), 0, st, mats, u.cells, ws, h);
   int from = 0;
   for (int i = 0; i < h.iterations; ++i, from ^= 1) {
-    if (u.large[0]) muon_large_product(1, mats, u.large_tiles[0], u.large[0], ws, from, st);
-    if (u.n_tri) hipLaunchKernelGGL((muon_product_kernel<1>), dim3(u.n_tri), dim3(256), 0, st, mats, u.tri, ws, from);
-    if (u.large[1]) muon_large_product(2, mats, u.large_tiles[1], u.large[1], ws, from, st);
-    if (u.n_tri) hipLaunchKernelGGL((muon_product_kernel<2>), dim3(u.n_tri), dim3(256), 0, st, mats, u.tri, ws, from);
-    if (u.large[2]) muon_large_product(3, mats, u.large_tiles[2], u.large[2], ws, from, st);
-    if (u.n_full) hipLaunchKernelGGL((muon_product_kernel<3>), dim3(u.n_full), dim3(256), 0, st, mats, u.full, ws, from);
+    product<1>(mats, u, ws, from, st);
+    product<2>(mats, u, ws, from, st);
+    product<3>(mats, u, ws, from, st);
   }
-  hipLaunchKernelGGL(muon_apply_kernel, dim3(u.n_cells), dim3(256), 0, st, mats, u.cells, ws, h, from);
+  if (strips) hipLaunchKernelGGL((muon_apply_kernel<4>), dim3(4 * u.n_cells), dim3(256), 0, st, mats, u.cells, ws, h, from);
+  else hipLaunchKernelGGL((muon_apply_kernel<1>), dim3(u.n_cells), dim3(256), 0, st, mats, u.cells, ws, h, from);
 }
 
 }  // namespace mk

@@ -460,7 +460,7 @@ static const char* bad_muon_list(const mimose_muon_matrix* t, int32_t count, int
 // the long tiles: 24 layers of 1024 (4096 wide), the first product takes 390 us instead of 263.
 static void muon_deal(std::vector<mk::MuonTile>& tiles, size_t from, const std::vector<mk::MuonMatrix>& mats, int stage, std::vector<int32_t>& starts) {
   constexpr int XCDS = 8, BLOCKS = mk::kMuonBlocks / XCDS;
-  struct Run { size_t from, to; int64_t each; };
+  struct Run { size_t from, to; int64_t each; };   // tiles, and the work of one
   std::vector<Run> runs;
   for (size_t i = from; i < tiles.size();) {
     const mk::MuonMatrix& m = mats[tiles[i].matrix];
@@ -500,6 +500,48 @@ static void muon_deal(std::vector<mk::MuonTile>& tiles, size_t from, const std::
   }
   starts.push_back((int32_t)(at - from));
 }
+// An order of the lists of tiles of 128 in which a matrix' tiles stay on one XCD, in all lists: block b runs on XCD b % 8, and what one
+// product leaves of a matrix in that XCD's L2 the next one finds there.  A matrix with more than an eighth of the work is cut
+// into as many runs as it has eighths.  Runs go to the XCD with least work, the largest first; places that are left over name no matrix.
+static void muon_spread(std::vector<mk::MuonTile>* lists, const size_t* from, int n_lists, const std::vector<int64_t>& work, int32_t first) {
+  constexpr int XCDS = 8;
+  int64_t all = 0;
+  for (int64_t w : work) all += w;
+  struct Run { int32_t matrix; int part, parts; int64_t work; };
+  std::vector<Run> runs;
+  for (size_t m = 0; m < work.size(); ++m) {
+    if (!work[m]) continue;
+    const int parts = (int)std::max<int64_t>(1, (work[m] * XCDS + all - 1) / all);
+    for (int k = 0; k < parts; ++k) runs.push_back({(int32_t)m, k, parts, work[m] / parts});
+  }
+  std::stable_sort(runs.begin(), runs.end(), [](const Run& a, const Run& b) { return a.work > b.work; });
+  std::vector<std::vector<int>> xcd_of(work.size());
+  for (size_t m = 0; m < work.size(); ++m) xcd_of[m].assign(XCDS, 0);
+  int64_t load[XCDS] = {};
+  for (const Run& r : runs) {
+    const int x = (int)(std::min_element(load, load + XCDS) - load);
+    load[x] += r.work;
+    xcd_of[r.matrix][r.part] = x;
+  }
+  std::vector<int> parts_of(work.size(), 1);
+  for (const Run& r : runs) parts_of[r.matrix] = r.parts;
+  for (int l = 0; l < n_lists; ++l) {
+    std::vector<mk::MuonTile>& list = lists[l];
+    std::vector<mk::MuonTile> queue[XCDS];
+    for (size_t i = from[l]; i < list.size();) {
+      size_t j = i;
+      while (j < list.size() && list[j].matrix == list[i].matrix) ++j;
+      const int32_t m = list[i].matrix - first;
+      for (size_t k = i; k < j; ++k) queue[xcd_of[m][(k - i) * parts_of[m] / (j - i)]].push_back(list[k]);
+      i = j;
+    }
+    size_t longest = 0;
+    for (const auto& q : queue) longest = std::max(longest, q.size());
+    list.resize(from[l]);
+    for (size_t i = 0; i < longest; ++i)
+      for (const auto& q : queue) list.push_back(i < q.size() ? q[i] : mk::MuonTile{-1, 0, 0});
+  }
+}
 static MuonPlan muon_plan(const mimose_muon_matrix* t, int32_t count, int32_t parts) {
   MuonPlan p;
   if ((p.why = bad_muon_list(t, count, parts))) return p;
@@ -528,17 +570,48 @@ static MuonPlan muon_plan(const mimose_muon_matrix* t, int32_t count, int32_t pa
   out.workspace_bytes = std::max<uint64_t>(16, (uint64_t)high);
   int part = 0;
   int64_t used = 0;
-  auto close = [&]() {
-    for (int s = 1; s <= 3; ++s) muon_deal(p.tiles[2 + s], part ? out.units[3 + s][part - 1] : 0, p.mats, s, p.starts);
-    out.units[0][part] = (int32_t)p.chunks.size();
-    for (int k = 0; k < 6; ++k) out.units[1 + k][part] = (int32_t)p.tiles[k].size();
-  };
+  int32_t first = 0;                                       // of the part's matrices
   // tiles of `side` of a matrix, in groups of four rows of tiles: blocks that run at the same time share rows and columns
   auto cover = [](std::vector<mk::MuonTile>& to, int32_t matrix, int64_t mp, int64_t np, int side, bool tri) {
     const int mt = (int)((mp + side - 1) / side), nt = (int)((np + side - 1) / side);
     for (int i0 = 0; i0 < mt; i0 += 4)
       for (int j = tri ? i0 : 0; j < nt; ++j)
         for (int i = i0; i < std::min(i0 + 4, mt) && (!tri || i <= j); ++i) to.push_back({matrix, (uint16_t)i, (uint16_t)j});
+  };
+  auto close = [&]() {
+    // Tiles of 256 for the matrices that they fit, where there are enough to fill the device: 24 layers of 1024 take 0.45 ms an
+    // iteration's last product with them and 0.68 without, of which 1.6 times as much work may be padding; 5 layers of 301 the other way round.
+    const int32_t end = (int32_t)p.mats.size();
+    auto fits = [](const mk::MuonMatrix& m) {
+      return m.mp > mk::kMuonTile && 10 * muon_up(m.mp, 256) * muon_up(m.np, 256) <= 16 * (int64_t)m.mp * m.np;
+    };
+    int64_t tiles = 0;
+    for (int32_t i = std::max(first, out.small); i < end; ++i)
+      if (fits(p.mats[i])) tiles += muon_up(p.mats[i].mp, 256) / 256 * (muon_up(p.mats[i].np, 256) / 256);
+    std::vector<int64_t> work(end - first, 0);
+    size_t from[3];
+    for (int k = 0; k < 3; ++k) from[k] = p.tiles[k].size();
+    for (int large = 0; large < 2; ++large) {                // the small tiles' cells come first
+      for (int32_t i = std::max(first, out.small); i < end; ++i) {
+        const mk::MuonMatrix& m = p.mats[i];
+        if ((tiles >= 256 && fits(m)) != (large != 0)) continue;
+        cover(p.tiles[0], i, m.mp, m.np, mk::kMuonTile, false);
+        if (large) {
+          cover(p.tiles[3], i, m.mp, m.mp, 256, true);
+          cover(p.tiles[4], i, m.mp, m.mp, 256, true);
+          cover(p.tiles[5], i, m.mp, m.np, 256, false);
+        } else {
+          cover(p.tiles[1], i, m.mp, m.mp, mk::kMuonTile, true);
+          cover(p.tiles[2], i, m.mp, m.np, mk::kMuonTile, false);
+          work[i - first] = (int64_t)m.mp * m.mp * m.np;
+        }
+      }
+      if (!large) muon_spread(p.tiles, from, 3, work, first);
+    }
+    for (int s = 1; s <= 3; ++s) muon_deal(p.tiles[2 + s], part ? out.units[3 + s][part - 1] : 0, p.mats, s, p.starts);
+    out.units[0][part] = (int32_t)p.chunks.size();
+    for (int k = 0; k < 6; ++k) out.units[1 + k][part] = (int32_t)p.tiles[k].size();
+    first = end;
   };
   for (int small = 1; small >= 0; --small)                 // the small ones come first, by themselves
     for (int32_t i = 0; i < count; ++i) {
@@ -548,7 +621,6 @@ static MuonPlan muon_plan(const mimose_muon_matrix* t, int32_t count, int32_t pa
       mk::MuonMatrix m = {t[i].master, (uint16_t*)t[i].lowp, t[i].grad, t[i].momentum};
       m.rows = (int32_t)rows;
       m.cols = (int32_t)cols;
-      const int32_t at = (int32_t)p.mats.size();
       if (small) {
         ++out.small;
       } else {
@@ -557,16 +629,7 @@ static MuonPlan muon_plan(const mimose_muon_matrix* t, int32_t count, int32_t pa
         m.np = (int32_t)muon_up(std::max(rows, cols), mk::kMuonTile);
         const int64_t x = 2 * (int64_t)m.mp * m.np, a = 2 * (int64_t)m.mp * m.mp;
         m.x[0] = (uint64_t)used; m.x[1] = m.x[0] + x; m.a = m.x[1] + x; m.b = m.a + a; m.partial = m.b + a;
-        for (int64_t c = 0; c < n; c += m.chunk) p.chunks.push_back({at, 0, c});
-        cover(p.tiles[0], at, m.mp, m.np, mk::kMuonTile, false);
-        if (mk::muon_large(rows, cols)) {
-          cover(p.tiles[3], at, m.mp, m.mp, 256, true);
-          cover(p.tiles[4], at, m.mp, m.mp, 256, true);
-          cover(p.tiles[5], at, m.mp, m.np, 256, false);
-        } else {
-          cover(p.tiles[1], at, m.mp, m.mp, mk::kMuonTile, true);
-          cover(p.tiles[2], at, m.mp, m.np, mk::kMuonTile, false);
-        }
+        for (int64_t c = 0; c < n; c += m.chunk) p.chunks.push_back({(int32_t)p.mats.size(), 0, c});
       }
       used += s;
       p.mats.push_back(m);

@@ -60,14 +60,26 @@ def test_one_matrix(shape):
         check(ms, table)
 
 
-@pytest.mark.parametrize("parts", [1, 3])
-def test_large_tiles(parts):
-    """Sides from the smallest that takes tiles of 256 on, whole tiles and not, beside smaller ones."""
-    ms = [matrix(s, i) for i, s in enumerate([(513, 513), (700, 1300), (64, 70), (1300, 700), (640, 520), (300, 400), (768, 768), (520, 2100)])]
-    table = mi.MuonTable(ms, parts=parts)
+def test_large_tiles():
+    """Enough tiles of 256 to be used, whole and not, beside smaller ones; and the same bits without them, in more parts."""
+    shapes = [(513, 513), (700, 1300), (64, 70), (1300, 700), (640, 520), (300, 400), (768, 768), (520, 2100), (130, 1000), (257, 300)] + 7 * [(2100, 520)]
+
+    def fresh():
+        return [matrix(s, i) for i, s in enumerate(shapes)]
+
+    ms = fresh()
+    table = mi.MuonTable(ms)
+    assert table.table.parts == 1 and all(table.table.units[k][0] > 0 for k in range(7))
     table.workspace.fill_(0xFF)
-    for _ in range(2):
-        check(ms, table)
+    check(ms, table)
+    others = fresh()
+    several = mi.MuonTable(others, parts=6)
+    assert not any(several.table.units[k][several.table.parts - 1] for k in (4, 5, 6))
+    several.workspace.fill_(0xFF)
+    mi.mimose_op_muon_step(several, **HYPER)
+    sync()
+    assert all(torch.equal(a["master"], b["master"]) for a, b in zip(ms, others))
+    check(ms, table)
 
 
 @pytest.mark.parametrize("parts", [1, 2, 5, 64])
