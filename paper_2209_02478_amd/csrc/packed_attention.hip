@@ -63,18 +63,27 @@ __device__ __forceinline__ int swizzle(int r) {
   return ((r >> 2) & 3) | (D == 64 ? (r & 2) << 1 : D == 128 ? (r & 3) << 2 : 0);
 }
 
-// A tile of TK rows in LDS: its direct loads by WAVES waves, and a wave's fragments of it.
-template <int D, int WAVES = 4>
+// One wave-level direct load of 4 bytes a lane, as l_direct_load.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"      // m0 is a reserved register: named as clobbered on purpose
+__device__ __forceinline__ void direct_load4(uint64_t base, uint32_t bytes, uint32_t offset, uint32_t lds_byte_address) {
+  const u32x4 r = {(uint32_t)base, (uint32_t)(base >> 32), bytes, 0x00020000u};                 // raw buffer
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dword %0, %1, 0 offen lds" : : "v"(offset), "s"(r), "s"(lds_byte_address) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+
+// A tile of ROWS rows in LDS: its direct loads by WAVES waves, and a wave's fragments of it.
+template <int D, int WAVES = 4, int ROWS = TK>
 struct Tile {
-  static constexpr int SIZE = TK * D;              // elements
-  static constexpr int LOADS = D / 8 / WAVES;      // 1 KB direct loads of each wave
+  static constexpr int SIZE = ROWS * D;                  // elements
+  static constexpr int LOADS = SIZE / 512 / WAVES;       // 1 KB direct loads of each wave
   uint32_t from[LOADS];                            // byte offset of the lane's chunk from the tile's first row
   int plain, turned;
   __device__ __forceinline__ void init(int wave, int lane, int ld) {
     constexpr int NC = D / 8;
 #pragma unroll
     for (int j = 0; j < LOADS; ++j) {
-      const int row = TK / WAVES * wave + j * (64 / NC) + lane / NC;
+      const int row = ROWS / WAVES * wave + j * (64 / NC) + lane / NC;
       from[j] = (uint32_t)(row * ld + (((lane % NC) ^ swizzle<D>(row)) << 3)) * 2u;
     }
     const int h = lane >> 5, r = lane & 31, q = 4 * h + ((lane & 15) >> 2);
@@ -531,18 +540,23 @@ __global__ __launch_bounds__(256) void packed_bwd_small_kernel(PackedAttention p
 }
 
 // Heads of 128: a wave with both gradients of 32 keys would need more registers than let two waves run on a SIMD.  So a pair of waves
-// has the same 32 keys: the first makes S and P and holds dV, the second makes dP and dS and holds dK; P passes from the one to the other
-// through LDS in fp32, behind a second barrier, which leaves the exponentials of the one beside the products of the other.
+// has the same 32 keys: the first makes S and P and holds dV, the second makes dP and dS and holds dK.  P passes from the one to the other
+// through LDS in fp32, and the second works a tile of 32 rows behind the first, so that they meet once for each tile.  Each makes its
+// product S or dP a tile ahead, so that the matrix units have it while the exponentials or differences of this one are taken.
+// Bound by the chain of a tile's steps in the block of the longest sequence's first keys: 64 keys to a block, not 128, halve what that
+// block has to do alone.  6 causal sequences of 1000-4096 rows, 16 heads, 4 of keys, the median of six runs (the fastest): 577 us (457);
+// blocks of 64 keys without the products ahead 595 (491), of 128 keys 605 (522), of 128 with both waves on the same tile and a second
+// barrier in it 645 (577), both gradients in one wave, one wave on a SIMD, 860.
 template <bool CAUSAL>
-__global__ __launch_bounds__(512) void packed_bwd_dkv_pair_kernel(PackedAttention p, int slots) {
-  constexpr int D = 128, KK = D / 16, DB = D / 32, BN = 128;
-  typedef Tile<D, 8> T;
-  __shared__ __attribute__((aligned(1024))) bf16_t tiles[2][2][T::SIZE];         // [buffer][Q, dO]
-  __shared__ __attribute__((aligned(16))) float4 passed[4][2][4][64];            // P: [keys' wave][half of the rows][registers / 4][lane]
-  __shared__ __attribute__((aligned(16))) float lse_s[2][TK], delta_s[2][TK];
+__global__ __launch_bounds__(256, 2) void packed_bwd_dkv_pair_kernel(PackedAttention p, int slots) {
+  constexpr int D = 128, KK = D / 16, DB = D / 32, BN = 64, ROWS = 32;
+  typedef Tile<D, 4, ROWS> T;
+  __shared__ __attribute__((aligned(1024))) bf16_t q_tiles[4][T::SIZE], g_tiles[2][T::SIZE];     // of Q and dO: [tile % 4], [tile % 2]
+  __shared__ __attribute__((aligned(16))) float4 passed[2][2][4][64];            // P: [tile % 2][keys' wave][registers / 4][lane]
+  __shared__ __attribute__((aligned(256))) float stat[4][2][64];                 // [tile % 4][lse, delta][row]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), kl = lane & 31, h = lane >> 5;
-  const int kw = wave & 3;
-  const bool values = wave < 4;                       // holds dV
+  const int kw = wave & 1;
+  const bool values = wave < 2;                       // holds dV
   PackedPlace w;
   if (!packed_place_kv<BN, CAUSAL>(p, slots, blockIdx.x, w)) return;
   const int w0 = w.row + kw * 32, ki = w0 + kl, kc = min(ki, w.n - 1);
@@ -558,8 +572,8 @@ __global__ __launch_bounds__(512) void packed_bwd_dkv_pair_kernel(PackedAttentio
   f32x16 acc[DB];
 #pragma unroll
   for (int db = 0; db < DB; ++db) zero(acc[db]);
-  const int qstart = CAUSAL ? w.row : 0;              // earlier queries never see these keys (a multiple of TK)
-  const int group = p.n_heads / p.n_kv_heads;
+  const int qstart = CAUSAL ? w.row : 0;              // earlier queries never see these keys (a multiple of ROWS)
+  const int group = p.n_heads / p.n_kv_heads, per_head = (w.n - qstart + ROWS - 1) / ROWS, count = per_head * group;
 
   T tq, tg;
   tq.init(wave, lane, (int)p.ldq);
@@ -567,101 +581,101 @@ __global__ __launch_bounds__(512) void packed_bwd_dkv_pair_kernel(PackedAttentio
   Stream qs, gs;
   qs.init((const bf16_t*)p.q + w.first * p.ldq + w.kv * group * D, (int)p.ldq);
   gs.init((const bf16_t*)p.dout + w.first * p.lddo + w.kv * group * D, (int)p.lddo);
-  const uint32_t lds = l_lds_address(&tiles[0][0][0]);
-  const int64_t stats = (int64_t)w.kv * group * p.T + w.first;
-  float pre_lse = 0.f, pre_delta = 0.f;
-  auto fetch = [&](int head, int q0, int buf) {
-    const uint64_t at = (uint64_t)head * (D * 2u);
-    tq.load(qs.at(q0) + at, qs.bytes(w.n - q0), wave, lds + (uint32_t)buf * (4u * T::SIZE));
-    tg.load(gs.at(q0) + at, gs.bytes(w.n - q0), wave, lds + (uint32_t)buf * (4u * T::SIZE) + 2u * T::SIZE);
-    if (tid < TK) {
-      const int q = min(q0 + tid, w.n - 1);
-      pre_lse = p.lse[stats + (int64_t)head * p.T + q];
-      pre_delta = p.delta[stats + (int64_t)head * p.T + q];
+  uint64_t stat_base;
+  uint32_t stat_pitch;                                // bytes from a head's lse, or delta, to the next one's
+  l_descriptor((values ? p.lse : p.delta) + (int64_t)w.kv * group * p.T + w.first, (uint32_t)p.T * 4u, stat_base, stat_pitch);
+  const uint32_t lds_q = l_lds_address(&q_tiles[0][0]), lds_g = l_lds_address(&g_tiles[0][0]), lds_stat = l_lds_address(&stat[0][0][0]);
+#pragma unroll
+  for (int kk = 0; kk < KK; ++kk) asm volatile("" : "+v"(own[kk]));     // waited for here: in the loop it would be a wait for every load
+  // the tiles of all heads that share these keys, one head after the other.  Behind a sequence's last row and behind the last tile
+  // everything is zeros: P is one there, and multiplies dO, or dP - delta, of zero.
+  struct At { int head, row; };
+  At ahead = {0, qstart}, next = ahead;               // of the next tiles to fetch, of Q and of the rest
+  auto fetch_q = [&](int tile) {
+    const int left = ahead.head < group ? w.n - ahead.row : 0;
+    tq.load(qs.at(ahead.row) + (uint64_t)ahead.head * (D * 2u), qs.bytes(left), wave, lds_q + (uint32_t)(tile & 3) * (2u * T::SIZE));
+    ahead.row += ROWS;
+    if (ahead.row >= w.n) { ahead.row = qstart; ++ahead.head; }
+  };
+  auto fetch = [&](int tile) {                        // this tile of dO and of lse or delta, and the one after it of Q
+    const int left = next.head < group ? w.n - next.row : 0;
+    tg.load(gs.at(next.row) + (uint64_t)next.head * (D * 2u), gs.bytes(left), wave, lds_g + (uint32_t)(tile & 1) * (2u * T::SIZE));
+    // (each of a role's waves: the same numbers to the same place)
+    direct_load4(stat_base + (uint64_t)next.head * stat_pitch + (uint64_t)next.row * 4u, (uint32_t)left * 4u, (uint32_t)lane * 4u,
+                 lds_stat + (uint32_t)(tile & 3) * 512u + (values ? 0u : 256u));
+    next = ahead;
+    fetch_q(tile + 1);
+  };
+  auto turn = [&](int tile) {                         // what was fetched has landed, and every wave is done with the tile before
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    fetch(tile + 1);
+  };
+  auto product = [&](const T& t, const bf16_t* rows) {
+    f32x16 s;
+    zero(s);
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(t.row(rows, 0, kk), own[kk], s, 0, 0, 0);
+    return s;
+  };
+  auto add = [&](const T& t, const bf16_t* rows, const f32x16& s) {
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const bf16x8 f = regs_to_frag(s, c);
+#pragma unroll
+      for (int db = 0; db < DB; ++db) acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(t.column(rows, db, 16 * c), f, acc[db], 0, 0, 0);
     }
   };
-  // a tile's first half: S and P, or dP
-  f32x16 s[2];
-  auto first = [&](int q0, int buf, auto values_) __attribute__((always_inline)) {
-    constexpr bool VALUES = decltype(values_)::value;
-#pragma unroll
-    for (int qb = 0; qb < 2; ++qb) {
-      zero(s[qb]);
-#pragma unroll
-      for (int kk = 0; kk < KK; ++kk)
-        s[qb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(VALUES ? tq.row(tiles[buf][0], qb, kk) : tg.row(tiles[buf][1], qb, kk), own[kk], s[qb], 0, 0, 0);
-    }
-    if (!VALUES) return;
-#pragma unroll
-    for (int qb = 0; qb < 2; ++qb)
+  fetch_q(0);
+  fetch(0);
+  turn(0);
+  if (values) {
+    f32x16 s = product(tq, q_tiles[0]);
+    int at = qstart, tile = 0;                        // the tile's first row
+    do {
+      const f32x16 following = product(tq, q_tiles[(tile + 1) & 3]);
 #pragma unroll
       for (int q4 = 0; q4 < 4; ++q4) {
-        const int qq = 32 * qb + 8 * q4 + 4 * h;
-        const float4 nl = *(const float4*)&lse_s[buf][qq];
-        const float nls[4] = {nl.x, nl.y, nl.z, nl.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int r = 4 * q4 + e;
-          s[qb][r] = fast_exp2(fmaf(s[qb][r], c2, nls[e]));
-        }
+        const float4 z = *(const float4*)&stat[tile & 3][0][8 * q4 + 4 * h];
+        s[4 * q4] = fast_exp2(fmaf(s[4 * q4], c2, -LOG2E * z.x));
+        s[4 * q4 + 1] = fast_exp2(fmaf(s[4 * q4 + 1], c2, -LOG2E * z.y));
+        s[4 * q4 + 2] = fast_exp2(fmaf(s[4 * q4 + 2], c2, -LOG2E * z.z));
+        s[4 * q4 + 3] = fast_exp2(fmaf(s[4 * q4 + 3], c2, -LOG2E * z.w));
       }
-    if (CAUSAL && q0 < w0 + 31) {                     // the tile touches the mask
-      const int from = ki - q0 - 4 * h;
-#pragma unroll
-      for (int qb = 0; qb < 2; ++qb)
+      if (CAUSAL && at < w0 + 31) {                   // the tile touches the mask, or lies behind it
+        const int from = ki - at - 4 * h;
 #pragma unroll
         for (int r = 0; r < 16; ++r)
-          if (32 * qb + 8 * (r >> 2) + (r & 3) < from) s[qb][r] = 0.f;
-    }
-#pragma unroll
-    for (int qb = 0; qb < 2; ++qb)
+          if (8 * (r >> 2) + (r & 3) < from) s[r] = 0.f;
+      }
 #pragma unroll
       for (int q4 = 0; q4 < 4; ++q4)
-        passed[kw][qb][q4][lane] = make_float4(s[qb][4 * q4], s[qb][4 * q4 + 1], s[qb][4 * q4 + 2], s[qb][4 * q4 + 3]);
-  };
-  // its second half: dV, or dS and dK
-  auto second = [&](int buf, auto values_) __attribute__((always_inline)) {
-    constexpr bool VALUES = decltype(values_)::value;
+        passed[tile & 1][kw][q4][lane] = make_float4(s[4 * q4], s[4 * q4 + 1], s[4 * q4 + 2], s[4 * q4 + 3]);
+      add(tg, g_tiles[tile & 1], s);
+      s = following;
+      at += ROWS;
+      if (at >= w.n) at = qstart;
+      turn(++tile);
+    } while (tile < count);
+  } else {
+    f32x16 s = product(tg, g_tiles[0]);
+    int tile = 0;
+    do {
+      turn(++tile);
+      const f32x16 following = product(tg, g_tiles[tile & 1]);
 #pragma unroll
-    for (int qb = 0; qb < 2; ++qb) {
-      if (!VALUES) {
-#pragma unroll
-        for (int q4 = 0; q4 < 4; ++q4) {
-          const float4 pr = passed[kw][qb][q4][lane], dl = *(const float4*)&delta_s[buf][32 * qb + 8 * q4 + 4 * h];
-          s[qb][4 * q4] = pr.x * (s[qb][4 * q4] - dl.x);
-          s[qb][4 * q4 + 1] = pr.y * (s[qb][4 * q4 + 1] - dl.y);
-          s[qb][4 * q4 + 2] = pr.z * (s[qb][4 * q4 + 2] - dl.z);
-          s[qb][4 * q4 + 3] = pr.w * (s[qb][4 * q4 + 3] - dl.w);
-        }
+      for (int q4 = 0; q4 < 4; ++q4) {
+        const float4 pr = passed[(tile - 1) & 1][kw][q4][lane], z = *(const float4*)&stat[(tile - 1) & 3][1][8 * q4 + 4 * h];
+        s[4 * q4] = pr.x * (s[4 * q4] - z.x);
+        s[4 * q4 + 1] = pr.y * (s[4 * q4 + 1] - z.y);
+        s[4 * q4 + 2] = pr.z * (s[4 * q4 + 2] - z.z);
+        s[4 * q4 + 3] = pr.w * (s[4 * q4 + 3] - z.w);
       }
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        const bf16x8 f = regs_to_frag(s[qb], c);
-#pragma unroll
-        for (int db = 0; db < DB; ++db)
-          acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(VALUES ? tg.column(tiles[buf][1], db, 32 * qb + 16 * c) : tq.column(tiles[buf][0], db, 32 * qb + 16 * c),
-                                                            f, acc[db], 0, 0, 0);
-      }
-    }
-  };
-  // the same barriers in both roles' loops
-  auto run = [&](auto values_) __attribute__((always_inline)) {
-    int buf = 0;
-    for (int head = 0; head < group; ++head)
-      for (int q0 = qstart; q0 < w.n; q0 += TK, buf ^= 1) {
-        if (tid < TK) { lse_s[buf][tid] = q0 + tid < w.n ? -LOG2E * pre_lse : -INFINITY; delta_s[buf][tid] = pre_delta; }
-        landed();
-        if (q0 + TK < w.n) fetch(head, q0 + TK, buf ^ 1);
-        else if (head + 1 < group) fetch(head + 1, qstart, buf ^ 1);
-        const bool some = w0 < w.n && !(CAUSAL && q0 + TK <= w0);   // a query of the tile sees this wave's keys
-        if (some) first(q0, buf, values_);
-        meet();                                       // P is there
-        if (some) second(buf, values_);
-      }
-  };
-  fetch(0, qstart, 0);
-  if (values) run(std::true_type());
-  else run(std::false_type());
+      add(tq, q_tiles[(tile - 1) & 3], s);
+      s = following;
+    } while (tile < count);
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");    // no direct load may land in LDS that is another block's by then
   if (ki < w.n) {
     if (values) store_rows<D>((bf16_t*)p.dv + (w.first + ki) * p.lddv + w.kv * D, acc, h, 1.f);
     else store_rows<D>((bf16_t*)p.dk + (w.first + ki) * p.lddk + w.kv * D, acc, h, p.scale);
@@ -692,7 +706,7 @@ void launch_bwd(const PackedAttention& p, hipStream_t st) {
   }
   hipLaunchKernelGGL((packed_bwd_dq_kernel<D, CAUSAL>), dim3(queries), dim3(256), 0, st, p, slots);
   if constexpr (D == 128) {
-    hipLaunchKernelGGL((packed_bwd_dkv_pair_kernel<CAUSAL>), dim3(packed_blocks(slots, kv, 1)), dim3(512), 0, st, p, slots);
+    hipLaunchKernelGGL((packed_bwd_dkv_pair_kernel<CAUSAL>), dim3(keys), dim3(256), 0, st, p, small);
   } else if ((int64_t)slots * kv >= 1024) {           // two blocks and more for every place that there is
     hipLaunchKernelGGL((packed_bwd_dkv_kernel<D, CAUSAL, 4, 1>), dim3(packed_blocks(slots, kv, 1)), dim3(256), 0, st, p, slots);
   } else {
