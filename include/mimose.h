@@ -565,6 +565,7 @@ typedef struct {                                      /* plain data, filled by m
   uint64_t workspace_bytes;
   int32_t matrices, parts, small, reserved_;
   int32_t units[7][64];                               /* units of work up to each part's end */
+  uint64_t fine[2];                                   /* a bit for each part: its symmetric, its last products are on tiles of 64 */
 } mimose_muon_table;
 uint64_t mimose_op_muon_table_bytes(const mimose_muon_matrix* matrices, int32_t count, int32_t parts);
 int mimose_op_muon_table(const mimose_muon_matrix* matrices, int32_t count, int32_t parts, void* device,

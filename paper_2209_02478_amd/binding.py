@@ -77,7 +77,7 @@ class mimose_muon_cfg(C.Structure):
 
 class mimose_muon_table(C.Structure):
     _fields_ = [("device", C.c_void_p), ("workspace_bytes", C.c_uint64)] + [(n, C.c_int32) for n in ("matrices", "parts", "small", "reserved_")] + \
-               [("units", (C.c_int32 * 64) * 7)]
+               [("units", (C.c_int32 * 64) * 7), ("fine", C.c_uint64 * 2)]
 
 
 class MimoseError(RuntimeError):

@@ -111,9 +111,11 @@ struct LTileOf {
       return (uint32_t)(r * (int)ld + kc * 8) * 2u;               // rows outside the matrix: behind the buffer's end
     }
     constexpr int RC = R / 8;                                     // chunks per k row
-    const int q = j * (64 / RC) + lane / RC, mc = (lane % RC) ^ (4 * (q & 3) + 2 * ((q >> 3) & 1));
+    const int q = j * (64 / RC) + lane / RC, mc = (lane % RC) ^ turn(q);
     return mc * 8 < rows ? (uint32_t)(q * (int)ld + mc * 8) * 2u : kOutside;
   }
+  // what the chunk numbers of k row q are permuted by; rows of 64 are two to a round of the banks
+  static __device__ __forceinline__ int turn(int q) { return R > 64 ? 4 * (q & 3) + 2 * ((q >> 3) & 1) : 2 * ((q >> 1) & 1) + 4 * ((q >> 3) & 1); }
   static __device__ __forceinline__ uint32_t two(int64_t ld) { return (uint32_t)(KM ? 16 : 2 * 64 / (R / 8)) * (uint32_t)ld * 2u; }
   // size of the buffer that starts at the tile's first row and this k tile: the rows that exist end it
   static __device__ __forceinline__ uint32_t bytes(int64_t ld, int rows) { return KM ? (uint32_t)min(rows, R) * (uint32_t)ld * 2u : kOutside; }
@@ -122,7 +124,7 @@ struct LTileOf {
     if (KM) return (((lane & 7) ^ ((4 * j + (lane >> 4)) & 7)) << 3) >= left;
     return lane / (R / 8) >= left - j * (64 / (R / 8));
   }
-  // this lane's place in the fragments of the 16-row blocks from first_block on (a multiple of 4)
+  // this lane's place in the fragments of the 16-row blocks from first_block on (a multiple of 4; of 2 with rows of 64)
   int at[2];
   __device__ __forceinline__ void init(int first_block, int lane) {
     if (KM) {
@@ -131,7 +133,7 @@ struct LTileOf {
         at[h] = (first_block * 16 + (lane & 15)) * LBK + (((4 * h + (lane >> 4)) ^ ((lane >> 1) & 7)) << 3);
     } else {
       const int g = lane >> 4, kq = (lane & 15) >> 2;
-      at[0] = (8 * g + kq) * R + (((2 * first_block) ^ (((lane & 3) >> 1) + 4 * kq + 2 * (g & 1))) << 3) + (lane & 1) * 4;
+      at[0] = (8 * g + kq) * R + (((2 * first_block) ^ (((lane & 3) >> 1) + turn(8 * g + kq))) << 3) + (lane & 1) * 4;
       at[1] = 0;
     }
   }

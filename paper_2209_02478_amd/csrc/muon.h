@@ -9,6 +9,7 @@
 namespace mk {
 
 constexpr int kMuonTile = 128;          // rows and columns of a block's tile; X, A and B are padded to whole tiles of zeros
+constexpr int kMuonFine = 64;           // a product's tiles where those are few or mostly padding
 constexpr int kMuonSmallShort = 128, kMuonSmallLong = 256;   // sides of the largest matrix that one block updates by itself, in LDS
 constexpr int64_t kMuonSide = 1 << 20;  // most rows or columns of a matrix
 
@@ -37,13 +38,14 @@ inline bool muon_small(int64_t rows, int64_t cols) {
 void muon_update_small(const MuonMatrix* mats, int count, const MuonHyper& h, hipStream_t st);
 constexpr int kMuonBlocks = 256;        // blocks of a product on large tiles: one to a compute unit, ids go to the 8 XCDs in turn
 // The units of work of one part of a list: elements in chunks, X in tiles, and the tiles of the products: of the symmetric ones on and
-// above the diagonal (tri) and of X (full), for matrices that take tiles of 128; for those that take 256 each product's tiles
+// above the diagonal (tri) and of X (full), for matrices that take tiles of 128 or 64; for those that take 256 each product's tiles
 // block by block, and where each block's begin (null: none).
 struct MuonUnits {
   const MuonChunk* chunks = nullptr;
   const MuonTile *cells = nullptr, *tri = nullptr, *full = nullptr, *large_tiles[3] = {nullptr, nullptr, nullptr};
   const int32_t* large[3] = {nullptr, nullptr, nullptr};
   int n_chunks = 0, n_cells = 0, n_tri = 0, n_full = 0;
+  bool fine_tri = false, fine_full = false;   // those are tiles of 64
 };
 // One part of a list after the other uses the scratch.
 void muon_update(const MuonMatrix* mats, const MuonUnits& u, void* workspace, const MuonHyper& h, hipStream_t st);

@@ -181,18 +181,21 @@ __global__ __launch_bounds__(256) void muon_start_kernel(const MuonMatrix* mats,
   }
 }
 
-// STAGE 1: A = X X^T.  2: B = a I + b A + c A A.  3: X' = B X.  A block makes 128 x 128; for matrices of which larger tiles would be
-// mostly padding, or too few.  Two slots of 64 reduction indices, two blocks to a compute unit.  Bound by the LDS: 96 KB go through it for
-// 64 indices, 0.5 us of a unit with the meetings; a ring of four slots changes nothing (5 layers of 301, 77 and 999: first product 14.3 and
-// 14.5 us), nor do eight waves.  A launch costs 7 us beside that: its start and end, two table entries and the first tile from memory.
-template <int STAGE>
+// STAGE 1: A = X X^T.  2: B = a I + b A + c A A.  3: X' = B X.  A block makes R x R, 128 or 64; for matrices of which larger tiles would
+// be mostly padding, or too few.  R of 128: two slots of 64 reduction indices, two blocks to a compute unit; bound by the LDS, through which
+// 96 KB go for 64 indices, 0.5 us of a unit with the meetings; a ring of four slots changes nothing, nor do eight waves.  R of 64: 48 KB
+// for a quarter of the product, but blocks for four times as many units, and four slots, so that a load may take three rounds.  5 layers
+// of 301, 77 and 999: the products take 14.4, 10.3 and 10.0 us on tiles of 128, 8.6, 6.4 and 11.5 on those of 64; one matrix of 301: a step of
+// 17 launches on tiles of 64 77 us, little more than the launches by themselves.
+template <int STAGE, int R>
 __global__ __launch_bounds__(256, 2) void muon_product_kernel(const MuonMatrix* mats, const MuonTile* tiles, char* ws, int from) {
   using namespace large;
-  constexpr int R = kMuonTile, SIZE = R * BK;                // elements of an operand tile
+  constexpr int SIZE = R * BK, SLOTS = R == 64 ? 4 : 2;       // elements of an operand tile
+  constexpr int N = R / 32, LOADS = R / 32;                  // blocks of 16 x 16 of a wave, and its loads of a tile
   constexpr bool KM = STAGE != 3;
   typedef LTileOf<true, R> TA;
   typedef LTileOf<KM, R> TB;
-  __shared__ __attribute__((aligned(1024))) f16 smem[2 * 2 * SIZE];   // [slot][A, B]
+  __shared__ __attribute__((aligned(1024))) f16 smem[SLOTS * 2 * SIZE];   // [slot][A, B]
   const MuonTile tile = tiles[blockIdx.x];
   if (tile.matrix < 0) return;
   const MuonMatrix& t = mats[tile.matrix];
@@ -206,64 +209,66 @@ __global__ __launch_bounds__(256, 2) void muon_product_kernel(const MuonMatrix* 
   const f16* pa = (STAGE == 1 ? x : STAGE == 2 ? a : b) + (int64_t)ti * R * lda;
   const f16* pb = STAGE == 3 ? x + tj * R : (STAGE == 1 ? x : a) + (int64_t)tj * R * ldb;
   uint64_t base_a, base_b;
-  uint32_t bytes_a, bytes_b, off_a[4], off_b[4];
+  uint32_t bytes_a, bytes_b, off_a[LOADS], off_b[LOADS];
   l_descriptor(pa, TA::bytes(lda, R), base_a, bytes_a);
   l_descriptor(pb, TB::bytes(ldb, R), base_b, bytes_b);      // (columns of X: no bound, every row is whole)
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    off_a[j] = TA::src(lda, R, wave * 4 + j, lane);
-    off_b[j] = TB::src(ldb, R, wave * 4 + j, lane);
+  for (int j = 0; j < LOADS; ++j) {
+    off_a[j] = TA::src(lda, R, wave * LOADS + j, lane);
+    off_b[j] = TB::src(ldb, R, wave * LOADS + j, lane);
   }
   const uint64_t step_a = BK * 2, step_b = KM ? BK * 2 : (uint64_t)BK * 2 * ldb;
-  const uint32_t lds = l_lds_address(smem) + (uint32_t)wave * 4096u;
+  const uint32_t lds = l_lds_address(smem) + (uint32_t)wave * (LOADS * 1024u);
   const int steps = (K + BK - 1) / BK;
   auto fetch = [&](int slot) {
     const uint32_t to = lds + (uint32_t)slot * (4u * SIZE);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) l_direct_load(base_a, bytes_a, off_a[j], to + j * 1024u);
+    for (int j = 0; j < LOADS; ++j) l_direct_load(base_a, bytes_a, off_a[j], to + j * 1024u);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) l_direct_load(base_b, bytes_b, off_b[j], to + 2u * SIZE + j * 1024u);
+    for (int j = 0; j < LOADS; ++j) l_direct_load(base_b, bytes_b, off_b[j], to + 2u * SIZE + j * 1024u);
     base_a += step_a;
     base_b += step_b;
   };
   TA fa;
   TB fb;
-  fa.init(wm * 4, lane);
-  fb.init(wn * 4, lane);
-  f32x4 acc[4][4];
+  fa.init(wm * N, lane);
+  fb.init(wn * N, lane);
+  f32x4 acc[N][N];
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < N; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  fetch(0);
+    for (int j = 0; j < N; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int k = 0; k < SLOTS - 1 && k < steps; ++k) fetch(k);
   for (int k = 0; k < steps; ++k) {
-    __builtin_amdgcn_s_waitcnt(in_flight(0));
+    if (SLOTS == 4 && k + 2 < steps) __builtin_amdgcn_s_waitcnt(in_flight(4 * LOADS));
+    else if (SLOTS == 4 && k + 1 < steps) __builtin_amdgcn_s_waitcnt(in_flight(2 * LOADS));
+    else __builtin_amdgcn_s_waitcnt(in_flight(0));
     __syncthreads();                                         // (every wave is done reading the slot that is filled next)
-    if (k + 1 < steps) fetch(k + 1 & 1);
-    const bf16_t* const sa = (const bf16_t*)(smem + (k & 1) * 2 * SIZE);
+    if (k + SLOTS - 1 < steps) fetch(k + SLOTS - 1 & SLOTS - 1);
+    const bf16_t* const sa = (const bf16_t*)(smem + (k & SLOTS - 1) * 2 * SIZE);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      f16x8 af[4], bf[4];
+      f16x8 af[N], bf[N];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) af[i] = __builtin_bit_cast(f16x8, fa.read(sa, 0, i, h));
+      for (int i = 0; i < N; ++i) af[i] = __builtin_bit_cast(f16x8, fa.read(sa, 0, i, h));
 #pragma unroll
-      for (int j = 0; j < 4; ++j) bf[j] = __builtin_bit_cast(f16x8, fb.read(sa + SIZE, 0, j, h));
+      for (int j = 0; j < N; ++j) bf[j] = __builtin_bit_cast(f16x8, fb.read(sa + SIZE, 0, j, h));
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < N; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(bf[j], af[i], acc[i][j], 0, 0, 0);
+        for (int j = 0; j < N; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(bf[j], af[i], acc[i][j], 0, 0, 0);
     }
   }
   __syncthreads();
-  // through LDS: row i of the tile in a row of 128 columns, 8-byte pieces permuted by the row
+  // through LDS: row i of the tile in a row of R columns, 8-byte pieces permuted by the row
   f16* const out = smem;
   const int lr = lane & 15, lq = lane >> 4;
-  auto at = [](int row, int piece) { return row * R + ((piece ^ (row & 31)) << 2); };
+  auto at = [](int row, int piece) { return row * R + ((piece ^ (row & R / 4 - 1)) << 2); };
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < N; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int row = wm * 64 + i * 16 + lr, piece = wn * 16 + j * 4 + lq;
+    for (int j = 0; j < N; ++j) {
+      const int row = wm * (R / 2) + i * 16 + lr, piece = wn * (R / 8) + j * 4 + lq;
       f32x4 v = acc[i][j];
       if (STAGE == 2) {
         const f16x4 s = *(const f16x4*)(a + ((int64_t)ti * R + row) * mp + tj * R + piece * 4);
@@ -283,13 +288,13 @@ __global__ __launch_bounds__(256, 2) void muon_product_kernel(const MuonMatrix* 
   const int ldc = STAGE == 3 ? np : mp;
 #pragma unroll 4
   for (int s = 0; s < R * R / 4 / 256; ++s) {
-    const int row = s * 8 + (tid >> 5), piece = tid & 31;
+    const int row = s * (1024 / R) + tid / (R / 4), piece = tid % (R / 4);
     *(f16x4*)(c + ((int64_t)ti * R + row) * ldc + tj * R + piece * 4) = *(const f16x4*)(out + at(row, piece));
   }
   if (STAGE != 3 && ti != tj) {
 #pragma unroll 4
     for (int s = 0; s < R * R / 4 / 256; ++s) {              // the same below the diagonal
-      const int col = s * 8 + (tid >> 5), row = (tid & 31) * 4;
+      const int col = s * (1024 / R) + tid / (R / 4), row = tid % (R / 4) * 4;
       f16x4 o;
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[e] = out[at(row + e, col >> 2) + (col & 3)];
@@ -494,7 +499,10 @@ template <int STAGE>
 static void product(const MuonMatrix* mats, const MuonUnits& u, char* ws, int from, hipStream_t st) {
   if (u.large[STAGE - 1]) muon_large_product(STAGE, mats, u.large_tiles[STAGE - 1], u.large[STAGE - 1], ws, from, st);
   const int n = STAGE == 3 ? u.n_full : u.n_tri;
-  if (n) hipLaunchKernelGGL((muon_product_kernel<STAGE>), dim3(n), dim3(256), 0, st, mats, STAGE == 3 ? u.full : u.tri, ws, from);
+  if (n < 1) return;
+  const MuonTile* const list = STAGE == 3 ? u.full : u.tri;
+  if (STAGE == 3 ? u.fine_full : u.fine_tri) hipLaunchKernelGGL((muon_product_kernel<STAGE, kMuonFine>), dim3(n), dim3(256), 0, st, mats, list, ws, from);
+  else hipLaunchKernelGGL((muon_product_kernel<STAGE, kMuonTile>), dim3(n), dim3(256), 0, st, mats, list, ws, from);
 }
 
 void muon_update(const MuonMatrix* mats, const MuonUnits& u, void* workspace, const MuonHyper& h, hipStream_t st) {

@@ -579,8 +579,8 @@ static MuonPlan muon_plan(const mimose_muon_matrix* t, int32_t count, int32_t pa
         for (int i = i0; i < std::min(i0 + 4, mt) && (!tri || i <= j); ++i) to.push_back({matrix, (uint16_t)i, (uint16_t)j});
   };
   auto close = [&]() {
-    // Tiles of 256 for the matrices that they fit, where there are enough to fill the device: 24 layers of 1024 take 0.45 ms an
-    // iteration's last product with them and 0.68 without, of which 1.6 times as much work may be padding; 5 layers of 301 the other way round.
+    // Tiles of 256 for matrices that they pad to no more than 1.6 times the work, where there are enough to fill the device: the last
+    // product of 24 layers of 1024 takes 0.45 ms an iteration on them and 0.68 on tiles of 128.
     const int32_t end = (int32_t)p.mats.size();
     auto fits = [](const mk::MuonMatrix& m) {
       return m.mp > mk::kMuonTile && 10 * muon_up(m.mp, 256) * muon_up(m.np, 256) <= 16 * (int64_t)m.mp * m.np;
@@ -588,6 +588,23 @@ static MuonPlan muon_plan(const mimose_muon_matrix* t, int32_t count, int32_t pa
     int64_t tiles = 0;
     for (int32_t i = std::max(first, out.small); i < end; ++i)
       if (fits(p.mats[i])) tiles += muon_up(p.mats[i].mp, 256) / 256 * (muon_up(p.mats[i].np, 256) / 256);
+    // The others' symmetric products on tiles of 64 where those of 128 are few, or have 18 % more of padding; their last product where they
+    // are fewer still.  A step on tiles of 128, the symmetric products on those of 64, all three on those of 64: one matrix of 301 131,
+    // 89 and 77 us; 4 of 512 (40 and 64 tiles of 128) 160, 112 and 95; 12 of 384 (72, 108) 141, 109 and 111; a layer of 768 (126, 432)
+    // 417, 348 and 361; 5 layers of 301, 77 and 999 (180, 360, much padding) 202, 151 and 154; 12 of 640 (180, 300) 231, 238 and 262;
+    // 2 of 2048 (272, 512) 581, 620 and 699.
+    int64_t coarse[2] = {}, quarters[2] = {};                // of the symmetric products, of the last one
+    auto count = [](int64_t* to, int64_t mt, int64_t nt) { to[0] += mt * (mt + 1) / 2; to[1] += mt * nt; };
+    for (int32_t i = std::max(first, out.small); i < end; ++i) {
+      const mk::MuonMatrix& m = p.mats[i];
+      if (tiles >= 256 && fits(m)) continue;
+      const int64_t shorter = std::min(m.rows, m.cols), longer = std::max(m.rows, m.cols);
+      count(coarse, m.mp / mk::kMuonTile, m.np / mk::kMuonTile);
+      count(quarters, muon_up(shorter, mk::kMuonFine) / mk::kMuonFine, muon_up(longer, mk::kMuonFine) / mk::kMuonFine);
+    }
+    const bool fine[2] = {coarse[0] < 160 || 118 * quarters[0] < 400 * coarse[0], coarse[1] < 100};
+    for (int k = 0; k < 2; ++k)
+      if (fine[k]) out.fine[k] |= (uint64_t)1 << part;
     std::vector<int64_t> work(end - first, 0);
     size_t from[3];
     for (int k = 0; k < 3; ++k) from[k] = p.tiles[k].size();
@@ -601,8 +618,9 @@ static MuonPlan muon_plan(const mimose_muon_matrix* t, int32_t count, int32_t pa
           cover(p.tiles[4], i, m.mp, m.mp, 256, true);
           cover(p.tiles[5], i, m.mp, m.np, 256, false);
         } else {
-          cover(p.tiles[1], i, m.mp, m.mp, mk::kMuonTile, true);
-          cover(p.tiles[2], i, m.mp, m.np, mk::kMuonTile, false);
+          const int32_t shorter = std::min(m.rows, m.cols), longer = std::max(m.rows, m.cols);
+          cover(p.tiles[1], i, shorter, shorter, fine[0] ? mk::kMuonFine : mk::kMuonTile, true);
+          cover(p.tiles[2], i, shorter, longer, fine[1] ? mk::kMuonFine : mk::kMuonTile, false);
           work[i - first] = (int64_t)m.mp * m.mp * m.np;
         }
       }
@@ -712,6 +730,8 @@ int mimose_op_muon_step(const mimose_muon_table* table, const mimose_muon_cfg* c
     u.cells = lists[0] + from[1]; u.n_cells = count[1];
     u.tri = lists[1] + from[2]; u.n_tri = count[2];
     u.full = lists[2] + from[3]; u.n_full = count[3];
+    u.fine_tri = table->fine[0] >> i & 1;
+    u.fine_full = table->fine[1] >> i & 1;
     for (int s = 0; s < 3; ++s, starts += mk::kMuonBlocks + 1) {
       u.large_tiles[s] = lists[3 + s] + from[4 + s];
       u.large[s] = count[4 + s] ? starts : nullptr;

@@ -156,6 +156,25 @@ def test_the_same_whatever_the_list():
         assert all(torch.equal(a, b) for a, b in zip(r, results[0]))
 
 
+def test_tiles_of_128_and_of_64():
+    """Enough tiles of 128 to be used; and the same bits in parts that have too few and take those of 64."""
+    shapes = 30 * [(383, 383)]
+    results = []
+    for parts in (1, 2, 8):
+        ms = [matrix(s, i) for i, s in enumerate(shapes)]
+        table = mi.MuonTable(ms, parts=parts)
+        every = (1 << table.table.parts) - 1
+        assert list(table.table.fine) == {1: [0, 0], 2: [every, 0], 8: [every, every]}[parts]
+        if parts == 1:
+            check(ms, table)
+        else:
+            mi.mimose_op_muon_step(table, **HYPER)
+        sync()
+        results.append([t[k] for t in ms for k in sorted(t)])
+    for r in results[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(r, results[0]))
+
+
 def test_captured_on_two_workspaces():
     """Two captured steps with a workspace each, replayed side by side, beside an eager one."""
     sets = [[matrix((90, 150), s), matrix((310, 150), s + 1)] for s in (20, 30, 40)]
