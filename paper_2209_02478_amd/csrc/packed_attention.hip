@@ -693,8 +693,15 @@ void launch_fwd(const PackedAttention& p, int causal, hipStream_t st) {
 template <int D, bool CAUSAL>
 void launch_bwd(const PackedAttention& p, hipStream_t st) {
   const int slots = packed_slots(p.T, p.n_seq, BM), kv = p.n_kv_heads, small = packed_slots(p.T, p.n_seq, 64);
-  const unsigned queries = packed_blocks(slots, kv, p.n_heads / kv), keys = packed_blocks(small, kv, 1);
-  if (packed_bwd_small(p.T, queries + keys)) {
+  const int group = p.n_heads / kv;
+  const unsigned queries = packed_blocks(slots, kv, group), keys = packed_blocks(small, kv, 1);
+  // One launch where launches cost more than the shorter chain of tiles that four groups of waves have, or pairs: rows to a block
+  // of keys, and few blocks.  One launch and two, us, sequences x rows, query heads / heads of keys: heads of 64, 12 / 12: 4x64 7.7 and
+  // 12.7, 1x1024 26.6 and 35.3, 8x256 23.5 and 25.0, 8x512 49.8 and 42.9; 16 / 4: 4x64 10.8 and 13.8, 8x128 17.4 and 18.0, 2x256 25.9
+  // and 22.9, 1x1024 82.7 and 57.3; heads of 128, 12 / 12: 2x256 19.4 and 24.5, 8x128 23.1 and 20.3; 16 / 4: 1x16 15.1 and 12.8.
+  const bool few = (int64_t)p.T * group <= (int64_t)p.n_seq * (group == 1 ? 1024 : 512) &&
+                   (D == 128 ? group <= 2 && queries + keys <= 320 : queries + keys <= 1024);
+  if (few) {
     constexpr int LDS = std::max(4 * Tile<D>::SIZE, dkv_elements<D, 2>()) * 2;
     static const bool configured = [] {
       (void)hipFuncSetAttribute((const void*)packed_bwd_small_kernel<D, CAUSAL>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
@@ -707,7 +714,11 @@ void launch_bwd(const PackedAttention& p, hipStream_t st) {
   hipLaunchKernelGGL((packed_bwd_dq_kernel<D, CAUSAL>), dim3(queries), dim3(256), 0, st, p, slots);
   if constexpr (D == 128) {
     hipLaunchKernelGGL((packed_bwd_dkv_pair_kernel<CAUSAL>), dim3(keys), dim3(256), 0, st, p, small);
-  } else if ((int64_t)slots * kv >= 1024) {           // two blocks and more for every place that there is
+  } else if ((int64_t)slots * kv >= (D == 32 ? 224 : 160) + 96 * group) {
+    // Blocks of 128 keys enough to fill the device; the longer their chain of tiles, that of all heads that share the keys, the more of
+    // them.  128 keys in one group and 64 keys in four, us, behind a mask, heads of 64: 12 / 12 192 blocks 17.0 and 16.9, 288 23.1 and
+    // 27.1, 1728 139 and 195; 16 / 4 320 78 and 62, 576 182 and 174, 640 112 and 120, 1280 209 and 252; heads of 32, 12 / 12: 288 18.0 and
+    // 17.7, 396 25.7 and 26.8, 1368 25 and 36.
     hipLaunchKernelGGL((packed_bwd_dkv_kernel<D, CAUSAL, 4, 1>), dim3(packed_blocks(slots, kv, 1)), dim3(256), 0, st, p, slots);
   } else {
     hipLaunchKernelGGL((packed_bwd_dkv_kernel<D, CAUSAL, 2, 4>), dim3(keys), dim3(512), 0, st, p, small);

@@ -377,16 +377,26 @@ void launch(unsigned blocks, hipStream_t st, A... a) {
 }
 template <int D, bool CAUSAL>
 void fwd(const PackedAttention& p, hipStream_t st) {
-  constexpr int W = 2, T = tile_floats<D>();
+  constexpr int T = tile_floats<D>();
   const int slots = packed_slots(p.T, p.n_seq, TR);
-  launch<packed_f32_fwd_kernel<D, CAUSAL, W>, W, T + W * 128 + W * T>(packed_blocks(slots, p.n_kv_heads, p.n_heads / p.n_kv_heads), st, p, slots);
+  const unsigned blocks = packed_blocks(slots, p.n_kv_heads, p.n_heads / p.n_kv_heads);
+  // Four waves to 32 rows while blocks are few (and, with heads of 128, rows have tiles for all of them).  Four and two, us, sequences x
+  // rows, query heads: heads of 64 behind a mask, 12: 4x64 9.8 and 9.2, 4x128 11.3 and 14.5, 1x1024 59 and 89, 8x128 (480 blocks) 16.5 and
+  // 16.8, 8x256 (864) 31 and 33, 8x512 (1632) 76 and 71; heads of 128, 12: 4x64 15.4 and 13.1, 1x1024 (396) 94 and 147, 8x128 35 and 28.
+  const bool four = D == 128 ? blocks <= 400 && p.T > (int64_t)p.n_seq * 96 : blocks <= 640;
+  if (four) launch<packed_f32_fwd_kernel<D, CAUSAL, 4>, 4, T + 4 * 128 + 4 * T>(blocks, st, p, slots);
+  else launch<packed_f32_fwd_kernel<D, CAUSAL, 2>, 2, T + 2 * 128 + 2 * T>(blocks, st, p, slots);
 }
 template <int D, bool CAUSAL>
 void bwd(const PackedAttention& p, hipStream_t st) {
   constexpr int W = 2, T = tile_floats<D>(), WS = D == 128 ? 2 : 4;
   const int slots = packed_slots(p.T, p.n_seq, TR);
   const unsigned queries = packed_blocks(slots, p.n_kv_heads, p.n_heads / p.n_kv_heads), keys = packed_blocks(slots, p.n_kv_heads, 1);
-  if (packed_bwd_small(p.T, queries + keys)) {
+  // One launch, of four waves to 32 rows, while its blocks are few enough to leave compute units for so many.  One launch and two, us,
+  // sequences x rows, query heads / heads of keys: heads of 64, 2 / 1: 4x64 11.6 and 21.5, 1x1024 95 and 212; 16 / 4: 8x512 235 and 285;
+  // 12 / 12: 8x128 31 and 35, 8x256 75 and 69, 8x512 211 and 155; heads of 32, 12 / 12: 8x512 80 and 97; heads of 128 (two waves), 12 / 12:
+  // 2x256 51 and 77, 8x128 63 and 63, 8x256 164 and 134; 16 / 4: 4x128 99 and 99, 8x128 119 and 104.
+  if (D == 128 ? queries + keys <= 512 : keys <= (D == 32 ? 2048u : 640u)) {
     launch<packed_f32_bwd_small_kernel<D, CAUSAL, WS>, WS, 2 * T + WS * 2 * TR + 2 * WS * T>(queries + keys, st, p, slots, (int)queries);
     return;
   }

@@ -12,8 +12,9 @@ struct PackedPlace {
 };
 
 // Lengths live on the device alone, so the host cannot count the row blocks.  Up to 64 sequences: a block finds its place among them
-// in an order by work (packed_sorted).  More: row blocks of M rows are numbered by slots, sequence s has those from f(s) = ends[s-1] / M + s on.  f grows by at least ceil(rows / M) from a sequence to the next,
-// and f(n_seq) <= T / M + n_seq: no table, no second launch, and at most one slot a sequence is idle.
+// in an order by work (packed_sorted).  More: row blocks of M rows are numbered by slots, sequence s has those from
+// f(s) = ends[s-1] / M + s on.  f grows by at least ceil(rows / M) from a sequence to the next, and f(n_seq) <= T / M + n_seq: no
+// table, no second launch, and at most one slot a sequence is idle.
 constexpr int kPackedSorted = 64;
 inline int64_t packed_slots64(int64_t T, int64_t n_seq, int M) { return T / M + n_seq; }
 inline int packed_slots(int64_t T, int64_t n_seq, int M) { return (int)packed_slots64(T, n_seq, M); }
@@ -21,9 +22,6 @@ inline int packed_slots(int64_t T, int64_t n_seq, int M) { return (int)packed_sl
 // heads follow each other on one XCD, whose L2 then fetches the rows of keys and values once for all of them, and the
 // heads of keys spread over the XCDs.
 inline unsigned packed_blocks(int slots, int kv_heads, int group) { return (unsigned)((((int64_t)slots * kv_heads + 7) / 8) * 8 * group); }
-
-// Whether a backward pass is made by one launch whose blocks for the keys make their own delta, and not by two that wait for each other.
-inline bool packed_bwd_small(int T, unsigned blocks) { return T <= 1024 && blocks <= 512; }
 
 // ends[s - 1], held to 0 .. T: whatever the array holds, no row outside the caller's is touched
 __device__ __forceinline__ int packed_end(const PackedAttention& p, int s) { return s > 0 ? min(max(p.ends[s - 1], 0), p.T) : 0; }

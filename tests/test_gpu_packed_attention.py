@@ -106,6 +106,18 @@ def test_lengths(dtype, h, hk, d, lengths, causal):
     Call(dtype, h, hk, d, lengths, behind=len(lengths) % 3, seed=sum(lengths)).check(causal)
 
 
+# backward passes of one launch and of two, and each way in which blocks share out the keys
+WAYS = [(1, 12, 12, 64, [70] * 24), (1, 12, 12, 32, [40] * 40), (1, 8, 2, 64, [190]), (1, 6, 6, 64, [190, 3]), (1, 8, 2, 32, [200, 129]), (1, 2, 1, 128, [65, 140]),
+        (1, 8, 2, 128, [190, 1]), (1, 6, 6, 128, [300]), (0, 12, 12, 64, [33] * 28), (0, 16, 16, 32, [33] * 64), (0, 8, 8, 128, [33] * 20), (0, 2, 1, 128, [400, 31]),
+        (0, 4, 4, 64, [500, 0, 65])]
+
+
+@pytest.mark.parametrize("causal", [1, 0])
+@pytest.mark.parametrize("dtype,h,hk,d,lengths", WAYS, ids=[f"{x[0]}-{x[1]}-{x[2]}-{x[3]}-{len(x[4])}x{x[4][0]}" for x in WAYS])
+def test_ways(dtype, h, hk, d, lengths, causal):
+    Call(dtype, h, hk, d, lengths, behind=2, seed=d + len(lengths)).check(causal)
+
+
 @pytest.mark.parametrize("dtype", [1, 0])
 @pytest.mark.parametrize("h,hk", [(1, 1), (8, 1), (6, 6), (12, 4), (10, 5), (9, 3)])
 def test_heads(dtype, h, hk):
@@ -250,24 +262,23 @@ def test_offsets_past_32_bits():
     q, k, v, do = (buf[:, i * d:(i + 1) * d] for i in range(4))
     ends = torch.tensor([0, 0, T - 100, T], dtype=torch.int32, device=DEV)[[2, 3]].contiguous()
     buf[:-100, :4 * d] = 0
-    res = {}
-    for name, (rows, x, l) in {"far": (T, (q, k, v, do), ld), "near": (100, [small[:, i * d:(i + 1) * d] for i in range(4)], 4 * d)}.items():
-        e = ends if name == "far" else torch.tensor([100], dtype=torch.int32, device=DEV)
-        out = torch.zeros(rows, ld if name == "far" else d, dtype=torch.bfloat16, device=DEV)
-        grads = torch.zeros(rows, ld if name == "far" else 3 * d, dtype=torch.bfloat16, device=DEV)
-        lse = torch.zeros(h, rows, device=DEV)
-        ws = torch.empty(mi.mimose_op_packed_attention_bwd_workspace_bytes(rows, h, h, d), dtype=torch.uint8, device=DEV)
-        lo, lg = out.stride(0), grads.stride(0)
-        head = (e, len(e), rows, h, h, d, 1, 0.125)
-        mi.mimose_op_packed_attention_fwd(1, x[0], l, x[1], l, x[2], l, out, lo, lse, *head)
-        mi.mimose_op_packed_attention_bwd(1, x[0], l, x[1], l, x[2], l, out, lo, lse, x[3], l, grads, lg, grads[:, d:], lg, grads[:, 2 * d:], lg,
-                                          *head, workspace=ws, workspace_bytes=ws.numel())
-        sync()
-        res[name] = (out[-100:, :d].clone(), grads[-100:, :3 * d].clone(), lse[:, -100:].clone())
-        del out, grads
-    for a, b in zip(res["far"], res["near"]):
-        assert torch.equal(a, b)
-    assert float(res["near"][0].float().abs().max()) > 0
+    out, grads = (torch.zeros(T, ld, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    lse = torch.zeros(h, T, device=DEV)
+    ws = torch.empty(mi.mimose_op_packed_attention_bwd_workspace_bytes(T, h, h, d), dtype=torch.uint8, device=DEV)
+    head = (ends, 2, T, h, h, d, 1, 0.125)
+    mi.mimose_op_packed_attention_fwd(1, q, ld, k, ld, v, ld, out, ld, lse, *head)
+    mi.mimose_op_packed_attention_bwd(1, q, ld, k, ld, v, ld, out, ld, lse, do, ld, grads, ld, grads[:, d:], ld, grads[:, 2 * d:], ld, *head,
+                                      workspace=ws, workspace_bytes=ws.numel())
+    sync()
+    rows = lambda x: x.double().cpu().numpy().reshape(100, 1, d)  # noqa: E731
+    operands = [rows(small[:, i * d:(i + 1) * d]) for i in range(4)]
+    got, got_lse = rows(out[-100:, :d]), lse[:, -100:].double().cpu().numpy()
+    want, want_lse, off, lse_off = oa.forward(*operands[:3], [100], 0.125, 1, UNIT[1])
+    within(got, want, off, "out")
+    within(got_lse, want_lse, lse_off, "lse")
+    want = oa.backward(*operands[:3], got, got_lse, operands[3], [100], 0.125, 1, UNIT[1])
+    for i, name in enumerate(("dq", "dk", "dv")):
+        within(rows(grads[-100:, i * d:(i + 1) * d]), want[i], want[3 + i], name)
 
 
 def test_nothing_to_do():
