@@ -6,6 +6,11 @@
 // boundary.  Why 256 x 256: a compute unit draws about 54 bytes per clock from the L2, tiles of 128 need 64 of it at full rate, of
 // 256 half as much.  Tiles differ in their number of k tiles, by matrix: the host deals them out to the blocks once, the longest first,
 // a matrix' neighbouring tiles to one XCD (see ops_abi.cpp).
+//
+// 48 matrices each of 1024 x 1024, 256 x 1024 and 1024 x 4096: the three products take 284, 162 and 500 us, 0.92, 0.64 and 1.04 PFLOP/s of
+// what is needed (of the symmetric ones the half above the diagonal; tiles of 256 make 5/8 of 1024 x 1024); a product of 8192^3 of the
+// library runs at 1.20.  Bound by the matrix units and, in the shorter second one, by whole rounds of tiles and their stores: with the
+// second factor asked for as it is stored and the tile below the diagonal written 16 bytes to a row, it took 175, the first 292.
 #include "muon_device.h"
 
 namespace mk {
@@ -168,7 +173,9 @@ __global__ __launch_bounds__(512) void muon_large_kernel(const MuonMatrix* mats,
   };
 
   // A finished tile: 16 rows of 64 columns at a time through 2 KB of LDS, the part of the free slot of A that this wave's next loads
-  // fill; out along the rows, and for a tile above the diagonal by columns too (transposing reads), to its place below.
+  // fill; out along the rows, and for a tile above the diagonal by columns too (transposing reads), to its place below: of two times 16
+  // rows the four lanes of a quad hand each other their pieces of 16 bytes, so that they write 64 bytes of one row, not of four.
+  // What the second stage adds is asked for before the first store: a load behind stores has to wait for them.
   auto store = [&]() __attribute__((always_inline)) {
     // (padding ends on 128 rows and columns: a wave's part exists or does not)
     stored = 0;
@@ -184,26 +191,36 @@ __global__ __launch_bounds__(512) void muon_large_kernel(const MuonMatrix* mats,
     auto fence = [&]() __attribute__((always_inline)) { asm volatile("" ::: "memory"); };
     const int m0 = cur.i + wm * 128, n0 = cur.j + wn * 64;
     f16* const rows = cur.c + (int64_t)(m0 + sr) * cur.ldc + n0 + sc * 8;
-    f16* const below = cur.c + (int64_t)(n0 + l) * cur.ldc + m0;
+    f16* const below = cur.c + (int64_t)(n0 + (l & ~3)) * cur.ldc + m0 + 8 * (l & 3);
     const f16* const self = cur.s + (int64_t)(m0 + lr) * cur.ldc + n0 + 4 * lq;
     // transposing reads: within 16 lanes, lane i gets column i of 4 rows; its own address is 4 columns of one of the rows
     const int tr = lr >> 2, tc = 16 * lq + 4 * (lr & 3);
-    f16x4 s[2][FN];
-    auto ask = [&](int i) __attribute__((always_inline)) {
+    f16x4 s[STAGE == 2 ? FM : 1][FN];
+    if (STAGE == 2) {
 #pragma unroll
-      for (int j = 0; j < FN; ++j) s[i & 1][j] = *(const f16x4*)(self + (int64_t)i * 16 * cur.ldc + 16 * j);
+      for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) s[i][j] = *(const f16x4*)(self + (int64_t)i * 16 * cur.ldc + 16 * j);
+    }
+    u32x4 z[4];                                                   // of two times 16 rows: eight each, of the column of this lane
+    // across a quad's lanes: z[k] of lane v becomes z[v] of lane k
+    auto swap = [&](u32x4& even, u32x4& odd, auto lanes, bool upper) __attribute__((always_inline)) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t got = __builtin_amdgcn_update_dpp(0, upper ? even[e] : odd[e], decltype(lanes)::value, 0xF, 0xF, false);
+        even[e] = upper ? got : even[e];
+        odd[e] = upper ? odd[e] : got;
+      }
     };
-    if (STAGE == 2) ask(0);
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
-      if (STAGE == 2 && i + 1 < FM) ask(i + 1);
 #pragma unroll
       for (int j = 0; j < FN; ++j) {
         f16x4 o;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           float v = acc[i][j][e];
-          if (STAGE == 2) v = fmaf(kB, (float)s[i & 1][j][e], kC * kBack * v) + (m0 + 16 * i + lr == n0 + 16 * j + 4 * lq + e ? kA * kHeld : 0.f);
+          if (STAGE == 2) v = fmaf(kB, (float)s[i][j][e], kC * kBack * v) + (m0 + 16 * i + lr == n0 + 16 * j + 4 * lq + e ? kA * kHeld : 0.f);
           else v *= kBack;
           o[e] = (f16)v;
         }
@@ -216,14 +233,24 @@ __global__ __launch_bounds__(512) void muon_large_kernel(const MuonMatrix* mats,
       if (STAGE != 3 && cur.i != cur.j) {
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-          s16x4 z[2];
+          s16x4 part[2];
 #pragma unroll
           for (int q = 0; q < 2; ++q) {
             const int r = 8 * half + 4 * q + tr;
-            z[q] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_l*)(turn + own + r * 128 + (((tc >> 3) ^ (r >> 1)) << 4) + (tc & 7) * 2));
+            part[q] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_l*)(turn + own + r * 128 + (((tc >> 3) ^ (r >> 1)) << 4) + (tc & 7) * 2));
           }
           typedef short s16x8 __attribute__((ext_vector_type(8)));
-          *(s16x8*)(below + i * 16 + 8 * half) = (s16x8)__builtin_shufflevector(z[0], z[1], 0, 1, 2, 3, 4, 5, 6, 7);
+          z[2 * (i & 1) + half] = __builtin_bit_cast(u32x4, (s16x8)__builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
+        }
+        if (i & 1) {
+          typedef std::integral_constant<int, 0xB1> NextLane;     // quad_perm 1 0 3 2
+          typedef std::integral_constant<int, 0x4E> NextPair;     // quad_perm 2 3 0 1
+          swap(z[0], z[1], NextLane(), l & 1);
+          swap(z[2], z[3], NextLane(), l & 1);
+          swap(z[0], z[2], NextPair(), l & 2);
+          swap(z[1], z[3], NextPair(), l & 2);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) *(u32x4*)(below + (int64_t)k * cur.ldc + (i - 1) * 16) = z[k];
         }
       }
       fence();

@@ -190,6 +190,7 @@ __global__ __launch_bounds__(64 * W) void packed_f32_fwd_kernel(PackedAttention 
 }
 
 // ------------------------------------------------------------------ dQ
+// 12 sequences of 153-397 rows without mask, 12 heads of 64: 75 us, 60 TFLOP/s, the matrix units 60 % busy while a unit has work.
 // TELL: delta is written out for the keys' gradients, which are made after.
 template <int D, bool CAUSAL, int W, bool TELL>
 __device__ __forceinline__ void f32_bwd_dq(const PackedAttention& p, int slots, int block, float* f_smem) {
@@ -263,6 +264,8 @@ __global__ __launch_bounds__(64 * W) void packed_f32_bwd_dq_kernel(PackedAttenti
 }
 
 // ------------------------------------------------------------------ dK, dV
+// The same sequences: 98 us, 61 TFLOP/s, 56 % busy (a product of 4096^3 of the library: 139).  With the own rows in registers 97, with four
+// waves to 32 rows 112 to 124, with one 104.
 // TOLD: delta is there; else it is made of dO and O.
 template <int D, bool CAUSAL, int W, bool TOLD>
 __device__ __forceinline__ void f32_bwd_dkv(const PackedAttention& p, int slots, int block, float* f_smem) {
