@@ -153,7 +153,7 @@ __device__ __forceinline__ void store_rows(bf16_t* dst, const f32x16 (&acc)[D / 
 // taken, which is what bounds it: with heads of 64 exponentials and their neighbours need two issue slots for each of the matrix
 // units', with heads of 128 as many (there 44 % and 53 % of the time is theirs).  6 causal sequences of 1000-4096 rows, 16 heads of
 // 128, 4 of keys: 215 us, 0.87 PFLOP/s of the pairs that see each other (scores not made ahead: 229); 32 sequences of 153-512 without mask,
-// 12 heads of 64: 32 us; 16 causal ones of 128-661, 16 heads of 64, 4 of keys: 20 us, of which the longest sequence's 11 tiles are 9.
+// 12 heads of 64: 32 us; 16 causal ones of 128-661, 16 heads of 64, 4 of keys: 20 us.
 template <int D, bool CAUSAL>
 __global__ __launch_bounds__(256, 2) void packed_fwd_kernel(PackedAttention p, int slots) {
   constexpr int KK = D / 16, DB = D / 32;
@@ -273,7 +273,7 @@ __global__ __launch_bounds__(256, 2) void packed_fwd_kernel(PackedAttention p, i
 
 // ------------------------------------------------------------------ dQ
 // 32 queries to a wave, as in the forward pass; three products of a tile.  6 causal sequences of 1000-4096 rows, 16 heads of 128: 272 to
-// 320 us (the clock falls under it), 0.88 PFLOP/s, the matrix units 49 % busy; 16 of 128-661, heads of 64: 24.8 us.  Two loops, whole tiles
+// 320 us (the clock falls under it), 1.03 to 0.88 PFLOP/s, the matrix units 49 % busy; 16 of 128-661, heads of 64: 24.8 us.  Two loops, whole tiles
 // and those at the mask's edge, gain less than 1 %.
 // smem: [buffer][K, V].  TELL: delta is written out for the keys' gradients, which are made after.
 template <int D, bool CAUSAL, bool TELL>
