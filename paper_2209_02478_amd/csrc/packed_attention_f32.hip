@@ -264,14 +264,15 @@ __global__ __launch_bounds__(64 * W) void packed_f32_bwd_dq_kernel(PackedAttenti
 }
 
 // ------------------------------------------------------------------ dK, dV
-// The same sequences: 98 us, 61 TFLOP/s, 56 % busy (a product of 4096^3 of the library: 139).  With the own rows in registers 97, with four
-// waves to 32 rows 112 to 124, with one 104.
+// A wave has one tile of LDS, for the rows of dO and then for those of Q: with a tile for each, a compute unit holds six waves with heads of
+// 64 and two with 128, instead of eight and four (12 sequences of 153-397 rows without mask, 12 heads of 64: 100 us, now 94, 64 TFLOP/s, the matrix
+// units 67 % busy while a unit has work, a product of 4096^3 of the library 139; heads of 128, the whole backward pass 410 and 278).
 // TOLD: delta is there; else it is made of dO and O.
 template <int D, bool CAUSAL, int W, bool TOLD>
 __device__ __forceinline__ void f32_bwd_dkv(const PackedAttention& p, int slots, int block, float* f_smem) {
   constexpr int TILE = tile_floats<D>();
   float *const own_k = f_smem, *const own_v = own_k + TILE, *const rowstat = own_v + TILE;   // rowstat [W][2][TR]: lse, delta of a tile
-  float *const mine_q = rowstat + W * 2 * TR, *const mine_g = mine_q + W * TILE;
+  float* const mine = rowstat + W * 2 * TR;           // a tile of dO, then of Q, to each wave
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, h = lane >> 5;
   PackedPlace w;
   if (!packed_place_kv<TR, CAUSAL>(p, slots, block, w)) return;
@@ -289,9 +290,12 @@ __device__ __forceinline__ void f32_bwd_dkv(const PackedAttention& p, int slots,
   // the tiles of all heads that share these keys, one head after the other; a wave takes every W-th
   const int qstart = CAUSAL ? w.row : 0, per_head = (w.n - qstart + TR - 1) / TR, tiles = per_head * group;
   float pre = 0.f;                                    // lse (lanes 0 ..) and delta (lanes 32 ..) of the tile's rows
-  auto fetch = [&](int t) {
+  auto fetch_q = [&](int t) {
     const int head = t / per_head, q0 = qstart + (t - head * per_head) * TR;
     fetch_rows<D>(qb + head * D, p.ldq, q0, last, l32, h, qf);
+  };
+  auto fetch_g = [&](int t) {
+    const int head = t / per_head, q0 = qstart + (t - head * per_head) * TR;
     fetch_rows<D>(gb + head * D, p.lddo, q0, last, l32, h, gf);
     const int64_t at = stats + (int64_t)head * p.T + min(q0 + l32, last);
     if (TOLD) {
@@ -310,23 +314,25 @@ __device__ __forceinline__ void f32_bwd_dkv(const PackedAttention& p, int slots,
     }
   };
   int t = wave;
-  if (t < tiles) fetch(t);
+  if (t < tiles) {
+    fetch_q(t);
+    fetch_g(t);
+  }
   __syncthreads();
   f32x16 dk[D / 32], dv[D / 32];
 #pragma unroll
   for (int db = 0; db < D / 32; ++db) { clear(dk[db]); clear(dv[db]); }
-  float *const tile_q = mine_q + wave * TILE, *const tile_g = mine_g + wave * TILE, *const st = rowstat + wave * 2 * TR;
+  float *const tile = mine + wave * TILE, *const st = rowstat + wave * 2 * TR;
   for (; t < tiles; t += W) {
     const int q0 = qstart + t % per_head * TR;
     f32x16 s, dp;
     scores<D>(qf, own_k, l32, h, s);
     scores<D>(gf, own_v, l32, h, dp);
     wave_sync();
-    stash<D>(tile_q, l32, h, qf);
-    stash<D>(tile_g, l32, h, gf);
+    stash<D>(tile, l32, h, gf);
     st[lane] = pre;
     wave_sync();
-    if (t + W < tiles) fetch(t + W);
+    if (t + W < tiles) fetch_g(t + W);
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       const float4 nl = *(const float4*)&st[8 * g + 4 * h], dl = *(const float4*)&st[TR + 8 * g + 4 * h];
@@ -339,19 +345,25 @@ __device__ __forceinline__ void f32_bwd_dkv(const PackedAttention& p, int slots,
         dp[r] = pr * (dp[r] - ds[e]);
       }
     }
-    accumulate<D>(tile_g, l32, h, s, dv);
-    accumulate<D>(tile_q, l32, h, dp, dk);
+    accumulate<D>(tile, l32, h, s, dv);
+    wave_sync();
+    stash<D>(tile, l32, h, qf);
+    wave_sync();
+    if (t + W < tiles) fetch_q(t + W);
+    accumulate<D>(tile, l32, h, dp, dk);
   }
   wave_sync();
-  put_part<D>(tile_q, lane, dk);
-  put_part<D>(tile_g, lane, dv);
+  put_part<D>(tile, lane, dk);
   __syncthreads();
   float factor[W], one[W];
 #pragma unroll
   for (int i = 0; i < W; ++i) { factor[i] = p.scale; one[i] = 1.f; }
   const bool real = ki < w.n;
-  store_sum<D, W>(real ? (float*)p.dk + (w.first + ki) * p.lddk + w.kv * D : nullptr, mine_q, TILE, wave, lane, factor);
-  store_sum<D, W>(real ? (float*)p.dv + (w.first + ki) * p.lddv + w.kv * D : nullptr, mine_g, TILE, wave, lane, one);
+  store_sum<D, W>(real ? (float*)p.dk + (w.first + ki) * p.lddk + w.kv * D : nullptr, mine, TILE, wave, lane, factor);
+  __syncthreads();
+  put_part<D>(tile, lane, dv);
+  __syncthreads();
+  store_sum<D, W>(real ? (float*)p.dv + (w.first + ki) * p.lddv + w.kv * D : nullptr, mine, TILE, wave, lane, one);
 }
 
 template <int D, bool CAUSAL, int W>
@@ -392,19 +404,28 @@ void fwd(const PackedAttention& p, hipStream_t st) {
 }
 template <int D, bool CAUSAL>
 void bwd(const PackedAttention& p, hipStream_t st) {
-  constexpr int W = 2, T = tile_floats<D>(), WS = D == 128 ? 2 : 4;
+  constexpr int W = 2, T = tile_floats<D>(), WS = 4;
   const int slots = packed_slots(p.T, p.n_seq, TR);
   const unsigned queries = packed_blocks(slots, p.n_kv_heads, p.n_heads / p.n_kv_heads), keys = packed_blocks(slots, p.n_kv_heads, 1);
+  const int group = p.n_heads / p.n_kv_heads;
   // One launch, of four waves to 32 rows, while its blocks are few enough to leave compute units for so many.  One launch and two, us,
-  // sequences x rows, query heads / heads of keys: heads of 64, 2 / 1: 4x64 11.6 and 21.5, 1x1024 95 and 212; 16 / 4: 8x512 235 and 285;
-  // 12 / 12: 8x128 31 and 35, 8x256 75 and 69, 8x512 211 and 155; heads of 32, 12 / 12: 8x512 80 and 97; heads of 128 (two waves), 12 / 12:
-  // 2x256 51 and 77, 8x128 63 and 63, 8x256 164 and 134; 16 / 4: 4x128 99 and 99, 8x128 119 and 104.
-  if (D == 128 ? queries + keys <= 512 : keys <= (D == 32 ? 2048u : 640u)) {
-    launch<packed_f32_bwd_small_kernel<D, CAUSAL, WS>, WS, 2 * T + WS * 2 * TR + 2 * WS * T>(queries + keys, st, p, slots, (int)queries);
+  // sequences x rows, query heads / heads of keys (blocks of queries), behind a mask: heads of 64, 12 / 12: 4x64 11.8 and 18.6, 8x256 (864) 64
+  // and 68, 8x512 (1632) 159 and 140; 16 / 4: 4x128 (320) 37 and 37, 8x256 (1152) 87 and 78; 2 / 1: 1x1024 (66) 93 and 139, 16x512 (544)
+  // 98 and 91; heads of 32, 12 / 12: 8x512 81 and 99, 16x512 (3264) 151 and 137; 16 / 4: 8x128 (640) 25 and 28, 8x256 60 and 47; heads of
+  // 128, 12 / 12: 8x128 (480) 54 and 58, 8x256 134 and 100; 16 / 4: 2x256 (288) 109 and 115, 8x128 (640) 88 and 74.
+  const unsigned most = D == 128 ? 480 : group == 1 ? (D == 32 ? 1700 : 900) : (D == 32 ? 700 : 500);
+  if (queries <= most) {
+    launch<packed_f32_bwd_small_kernel<D, CAUSAL, WS>, WS, 2 * T + WS * 2 * TR + WS * T>(queries + keys, st, p, slots, (int)queries);
     return;
   }
   launch<packed_f32_bwd_dq_kernel<D, CAUSAL, W>, W, 2 * T + W * T>(queries, st, p, slots);
-  launch<packed_f32_bwd_dkv_kernel<D, CAUSAL, W>, W, 2 * T + W * 2 * TR + 2 * W * T>(keys, st, p, slots);
+  // Four waves to 32 keys where these have tiles for all of them, or blocks are few.  Two and four, us, the whole pass, (blocks of keys): heads
+  // of 64, 12 / 12 without mask: 64x128 (3840) 183 and 201, 16x512 (3264) 449 and 430, 2x2048 (1560) 879 and 731; behind a mask 122 and
+  // 142, 252 and 267, 456 and 432; 16 / 4 behind a mask: 32x512 (2176) 594 and 581; heads of 128, 16 / 4: 8x512 (544) 439 and 333,
+  // 16x512 (1088) 627 and 649; 12 / 12: 8x256 (864) 101 and 114.
+  const bool four = D == 128 ? keys <= 640 : keys <= 1024 || (int64_t)p.T * group >= (int64_t)p.n_seq * (CAUSAL ? 640 : 320);
+  if (four) launch<packed_f32_bwd_dkv_kernel<D, CAUSAL, 4>, 4, 2 * T + 4 * 2 * TR + 4 * T>(keys, st, p, slots);
+  else launch<packed_f32_bwd_dkv_kernel<D, CAUSAL, 2>, 2, 2 * T + 2 * 2 * TR + 2 * T>(keys, st, p, slots);
 }
 }  // namespace
 
