@@ -352,9 +352,10 @@ __global__ __launch_bounds__(256) void muon_apply_kernel(const MuonMatrix* mats,
 
 constexpr int kSmallThreads = 1024;
 // A matrix of at most 128 x 256 (or turned) in one block: X, A and B stay in LDS, and the whole update is one launch.  Rows of X, A
-// and B are 16 bytes longer than their elements, so that neither the fragments' rows nor their columns meet in a bank.  The gradient
-// and the momentum are read twice, before and behind the norm, the second time out of the caches (held in registers, by eight waves:
-// 29.6 us instead of 26.9).  Bound by the chain of its 15 products: 12 matrices of 64 x 64 to 64 x 256, 16 waves each, 22.4 us.
+// and B are 16 bytes longer than their elements, so that neither the fragments' rows nor their columns meet in a bank.  What
+// the norm is taken of stays in registers until it is known, and the weights are asked for before the products.  Bound by the chain of
+// 15 products and their meetings: 12 matrices of 64 x 64 to 64 x 256, 16 waves each, 22.1 us (all read again where they are used 22.4, by
+// eight waves 26.9), one of 5 x 5 13.9, four of 100 x 77 37.
 __global__ __launch_bounds__(kSmallThreads) void muon_small_kernel(const MuonMatrix* mats, MuonHyper h) {
   extern __shared__ __attribute__((aligned(16))) f16 s_smem[];
   constexpr int WAVES = kSmallThreads / 64;
@@ -371,44 +372,49 @@ __global__ __launch_bounds__(kSmallThreads) void muon_small_kernel(const MuonMat
   const int c = 4 * (tid & ((1 << lanes) - 1)), mine = tid >> lanes, many = min(max(cols - c, 0), 4);
   const float *const grad = t.grad;
   float *const mom = t.momentum, *const master = t.master;
+  constexpr int AGAIN = kMuonSmallShort * kMuonSmallLong / 16 / kSmallThreads;   // a lane's fours of rows, at most
   double sum = 0.0;
-  auto two = [&](int r, f32x4& g, f32x4& m) {
-    r = min(r, rows - 1) * cols;
-    g = load_row4(grad + r, c, cols);
-    m = load_row4(mom + r, c, cols);
-  };
-  for (int r0 = mine; r0 < rows; r0 += 4 * apart) {
-    f32x4 g[4], m[4];
-    if (many)
+  f32x4 u[AGAIN][4];
 #pragma unroll
-      for (int q = 0; q < 4; ++q) two(r0 + apart * q, g[q], m[q]);
+  for (int a = 0; a < AGAIN; ++a) {
+    const int r0 = mine + a * 4 * apart;
+    if (!many || r0 >= rows) continue;
+    f32x4 g[4], m[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int r = min(r0 + apart * q, rows - 1) * cols;
+      g[q] = load_row4(grad + r, c, cols);
+      m[q] = load_row4(mom + r, c, cols);
+    }
 #pragma unroll
     for (int q = 0; q < 4; ++q)
-      if (many && r0 + apart * q < rows) {
+      if (r0 + apart * q < rows) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) m[q][e] = fmaf(h.momentum, m[q][e], g[q][e]);
         store_row4(mom + (r0 + apart * q) * cols, nullptr, c, cols, m[q]);
-        const f32x4 u = direction(h, g[q], m[q]);            // (zeros behind the row)
+        u[a][q] = direction(h, g[q], m[q]);                  // (zeros behind the row)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sum += (double)u[e] * u[e];
+        for (int e = 0; e < 4; ++e) sum += (double)u[a][q][e] * u[a][q][e];
       }
   }
+  f32x4 w[AGAIN][4];                                         // asked for here, used behind the products
+#pragma unroll
+  for (int a = 0; a < AGAIN; ++a)
+    if (many && mine + a * 4 * apart < rows)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) w[a][q] = load_row4(master + min(mine + (4 * a + q) * apart, rows - 1) * cols, c, cols);
   for (int i = tid; i < m64 * PX / 8; i += kSmallThreads) ((f16x8*)X)[i] = f16x8{};
   const float inv = (float)((double)kHeld / (sqrt(block_sum<WAVES>(sum, lds)) + (double)h.eps));
-  for (int r0 = mine; r0 < rows; r0 += 4 * apart) {
-    f32x4 g[4], m[4];
-    if (many)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) two(r0 + apart * q, g[q], m[q]);
+  for (int a = 0; a < AGAIN; ++a)
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
-      if (many && r0 + apart * q < rows) {
-        const f32x4 u = direction(h, g[q], m[q]);
+    for (int q = 0; q < 4; ++q) {
+      const int r = mine + (4 * a + q) * apart;
+      if (r >= rows) continue;
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (e < many) X[tall ? (c + e) * PX + r0 + apart * q : (r0 + apart * q) * PX + c + e] = (f16)(u[e] * inv);
-      }
-  }
+      for (int e = 0; e < 4; ++e)
+        if (e < many) X[tall ? (c + e) * PX + r : r * PX + c + e] = (f16)(u[a][q][e] * inv);
+    }
   __syncthreads();
   const int mt = m64 / 16, nt = n64 / 16;
   auto row_frag = [&](const f16* s, int pitch, int block, int k) { return *(const f16x8*)(s + (block * 16 + lr) * pitch + k + 8 * lq); };
@@ -468,21 +474,17 @@ __global__ __launch_bounds__(kSmallThreads) void muon_small_kernel(const MuonMat
     __syncthreads();
   }
   const float step = step_size(t, h);
-  for (int r0 = mine; r0 < rows; r0 += 4 * apart) {
-    f32x4 w[4];
-    if (many)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) w[q] = load_row4(master + min(r0 + apart * q, rows - 1) * cols, c, cols);
+  for (int a = 0; a < AGAIN; ++a)
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
-      if (many && r0 + apart * q < rows) {
-        const int r = r0 + apart * q;
-        f32x4 v;
+    for (int q = 0; q < 4; ++q) {
+      const int r = mine + (4 * a + q) * apart;
+      if (!many || r >= rows) continue;
+      f32x4 v;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = (float)X[tall ? min(c + e, cols - 1) * PX + r : r * PX + c + e];
-        store_row4(master + r * cols, t.lowp ? t.lowp + r * cols : nullptr, c, cols, stepped(h, w[q], v, step));
-      }
-  }
+      for (int e = 0; e < 4; ++e) v[e] = (float)X[tall ? min(c + e, cols - 1) * PX + r : r * PX + c + e];
+      store_row4(master + r * cols, t.lowp ? t.lowp + r * cols : nullptr, c, cols, stepped(h, w[a][q], v, step));
+    }
 }
 
 void muon_update_small(const MuonMatrix* mats, int count, const MuonHyper& h, hipStream_t st) {
