@@ -354,7 +354,7 @@ constexpr int kSmallThreads = 1024;
 // A matrix of at most 128 x 256 (or turned) in one block: X, A and B stay in LDS, and the whole update is one launch.  Rows of X, A
 // and B are 16 bytes longer than their elements, so that neither the fragments' rows nor their columns meet in a bank.  What
 // the norm is taken of stays in registers until it is known, and the weights are asked for before the products.  Bound by the chain of
-// 15 products and their meetings: 12 matrices of 64 x 64 to 64 x 256, 16 waves each, 22.1 us (all read again where they are used 22.4, by
+// 15 products and their meetings: 12 matrices of 64 x 64 to 64 x 256, 16 waves each, 22.8 us (all read again where they are used 23.1, by
 // eight waves 26.9), one of 5 x 5 13.9, four of 100 x 77 37.
 __global__ __launch_bounds__(kSmallThreads) void muon_small_kernel(const MuonMatrix* mats, MuonHyper h) {
   extern __shared__ __attribute__((aligned(16))) f16 s_smem[];
