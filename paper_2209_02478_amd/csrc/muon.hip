@@ -43,9 +43,11 @@ __device__ __forceinline__ f32x4 load_row4(const float* row, int c, int cols) {
     if (c + e < cols) v[e] = row[c + e];
   return v;
 }
-// the same where rows are asked for together: no branch between the loads.  whole: the four elements exist in every lane
+// the same where rows are asked for together: no branch between the loads.  whole: the four elements exist in every lane.
+// PAST: past the caches
+template <bool PAST>
 __device__ __forceinline__ f32x4 load_edge4(const float* row, int c, int cols, bool whole) {
-  if (whole) return *(const f32x4_at4*)(row + c);
+  if (whole) return PAST ? __builtin_nontemporal_load((const f32x4_at4*)(row + c)) : *(const f32x4_at4*)(row + c);
   f32x4 v;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
@@ -88,7 +90,9 @@ __device__ __forceinline__ int turn_at(int row, int piece) { return row * kMuonT
 
 }  // namespace
 
-// Momentum, and each chunk's sum of u^2.  Bound by HBM: 264 M elements in 583-650 us, 4.9 to 5.4 TB/s of the 12 bytes each (a copy: 4.9).
+// Momentum, and each chunk's sum of u^2.  Bound by HBM: 264 M elements in 540 us, 5.9 TB/s of the 12 bytes each; through the caches, of which
+// the next kernel finds nothing again in a list as large as that, 640.
+template <bool PAST>
 __global__ __launch_bounds__(256) void muon_momentum_kernel(const MuonMatrix* mats, const MuonChunk* chunks, char* ws, MuonHyper h) {
   __shared__ double lds[4];
   const MuonChunk c = chunks[blockIdx.x];
@@ -100,7 +104,8 @@ __global__ __launch_bounds__(256) void muon_momentum_kernel(const MuonMatrix* ma
   auto four = [&](int64_t i, const f32x4& gv, f32x4 mv) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) mv[e] = fmaf(h.momentum, mv[e], gv[e]);
-    *(f32x4*)(m + i) = mv;
+    if (PAST) __builtin_nontemporal_store(mv, (f32x4*)(m + i));
+    else *(f32x4*)(m + i) = mv;
     const f32x4 u = direction(h, gv, mv);
 #pragma unroll
     for (int e = 0; e < 4; ++e) sum += (double)u[e] * u[e];
@@ -110,8 +115,9 @@ __global__ __launch_bounds__(256) void muon_momentum_kernel(const MuonMatrix* ma
     f32x4 gv[4], mv[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      gv[q] = *(const f32x4*)(g + i + q * 1024);
-      mv[q] = *(const f32x4*)(m + i + q * 1024);
+      const f32x4 *const gp = (const f32x4*)(g + i + q * 1024), *const mp = (const f32x4*)(m + i + q * 1024);
+      gv[q] = PAST ? __builtin_nontemporal_load(gp) : *gp;
+      mv[q] = PAST ? __builtin_nontemporal_load(mp) : *mp;
     }
 #pragma unroll
     for (int q = 0; q < 4; ++q) four(i + q * 1024, gv[q], mv[q]);
@@ -128,7 +134,7 @@ __global__ __launch_bounds__(256) void muon_momentum_kernel(const MuonMatrix* ma
 
 // X = u / (|u| + eps), 128 x 128 of it to STRIPS blocks, zeros behind the matrix' last row and column.  A thread takes 4 x 4 elements at a
 // time, eight loads in flight, and turns them in registers where X is the matrix turned.  Four strips of 32 rows where the tiles are too few
-// to keep the memory busy.  Bound by HBM: 264 M elements in 535 us, 4.9 TB/s of 10 bytes each.
+// to keep the memory busy.  Bound by HBM: 264 M elements in 511 us, 5.2 TB/s of 10 bytes each (u through the caches 540).
 template <int STRIPS>
 __global__ __launch_bounds__(256) void muon_start_kernel(const MuonMatrix* mats, const MuonTile* tiles, char* ws, MuonHyper h) {
   __shared__ double lds[4];
@@ -155,8 +161,8 @@ __global__ __launch_bounds__(256) void muon_start_kernel(const MuonMatrix* mats,
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const int64_t row = (int64_t)min(r0 + r + q, rows - 1) * cols;
-      g[q] = load_edge4(grad + row, at, cols, whole);
-      m[q] = load_edge4(mom + row, at, cols, whole);
+      g[q] = load_edge4<STRIPS == 1>(grad + row, at, cols, whole);
+      m[q] = load_edge4<STRIPS == 1>(mom + row, at, cols, whole);
     }
     f16 o[4][4];
 #pragma unroll
@@ -303,8 +309,8 @@ __global__ __launch_bounds__(256, 2) void muon_product_kernel(const MuonMatrix* 
   }
 }
 
-// The weights' step from the finished X, in the same blocks of 4 x 4 elements as the start.  Bound by HBM: 264 M elements in 655 us,
-// 4.8 TB/s of 12 bytes each.
+// The weights' step from the finished X, in the same blocks of 4 x 4 elements as the start.  Bound by HBM: 264 M elements in 588 us,
+// 5.4 TB/s of 12 bytes each (weights through the caches 645; written past them too 620).
 template <int STRIPS>
 __global__ __launch_bounds__(256) void muon_apply_kernel(const MuonMatrix* mats, const MuonTile* tiles, const char* ws, MuonHyper h, int from) {
   __shared__ __attribute__((aligned(16))) f16 turn[kMuonTile * kMuonTile];
@@ -335,7 +341,7 @@ __global__ __launch_bounds__(256) void muon_apply_kernel(const MuonMatrix* mats,
     f16x4 s[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      w[q] = load_edge4(master + (int64_t)min(r0 + r + q, rows - 1) * cols, at, cols, whole);
+      w[q] = load_edge4<STRIPS == 1>(master + (int64_t)min(r0 + r + q, rows - 1) * cols, at, cols, whole);
       s[q] = tall ? *(const f16x4*)&turn[turn_at(c + q, r >> 2)] : *(const f16x4*)(x + (int64_t)(r + q) * np + c);
     }
 #pragma unroll
@@ -511,9 +517,12 @@ static void product(const MuonMatrix* mats, const MuonUnits& u, char* ws, int fr
 void muon_update(const MuonMatrix* mats, const MuonUnits& u, void* workspace, const MuonHyper& h, hipStream_t st) {
   if (u.n_chunks < 1) return;
   char* const ws = (char*)workspace;
-  const bool strips = u.n_cells < 512;  // a step with strips and without, us: 9 cells 74 and 90, 360 152 and 163, 720 452 and 447
-  hipLaunchKernelGGL(muon_momentum_kernel, dim3(u.n_chunks), dim3(256), 0, st, mats, u.chunks, ws, h);
-  if (strips) hipLaunchKernelGGL((muon_start_kernel<4>), dim3(4 * u.n_cells), dim3(256), 0, st, mats, u.cells, ws, h);
+  // Few tiles: in strips, and through the caches, which keep what the next kernel reads.  A step with strips and without, us: 9 cells 74
+  // and 90, 360 152 and 163, 720 452 and 447; past the caches and through them: 720 430 and 427, 1728 818 and 839, 5184 1960 and 2010.
+  const bool few = u.n_cells < 512;
+  if (few) hipLaunchKernelGGL((muon_momentum_kernel<false>), dim3(u.n_chunks), dim3(256), 0, st, mats, u.chunks, ws, h);
+  else hipLaunchKernelGGL((muon_momentum_kernel<true>), dim3(u.n_chunks), dim3(256), 0, st, mats, u.chunks, ws, h);
+  if (few) hipLaunchKernelGGL((muon_start_kernel<4>), dim3(4 * u.n_cells), dim3(256), 0, st, mats, u.cells, ws, h);
   else hipLaunchKernelGGL((muon_start_kernel<1>), dim3(u.n_cells), dim3(256), 0, st, mats, u.cells, ws, h);
   int from = 0;
   for (int i = 0; i < h.iterations; ++i, from ^= 1) {
@@ -521,7 +530,7 @@ void muon_update(const MuonMatrix* mats, const MuonUnits& u, void* workspace, co
     product<2>(mats, u, ws, from, st);
     product<3>(mats, u, ws, from, st);
   }
-  if (strips) hipLaunchKernelGGL((muon_apply_kernel<4>), dim3(4 * u.n_cells), dim3(256), 0, st, mats, u.cells, ws, h, from);
+  if (few) hipLaunchKernelGGL((muon_apply_kernel<4>), dim3(4 * u.n_cells), dim3(256), 0, st, mats, u.cells, ws, h, from);
   else hipLaunchKernelGGL((muon_apply_kernel<1>), dim3(u.n_cells), dim3(256), 0, st, mats, u.cells, ws, h, from);
 }
 
