@@ -154,11 +154,14 @@ __device__ __forceinline__ void store_rows(bf16_t* dst, const f32x16 (&acc)[D / 
 // units', with heads of 128 as many (there 44 % and 53 % of the time is theirs).  6 causal sequences of 1000-4096 rows, 16 heads of
 // 128, 4 of keys: 215 us, 0.87 PFLOP/s of the pairs that see each other (scores not made ahead: 229); 32 sequences of 153-512 without mask,
 // 12 heads of 64: 32 us; 16 causal ones of 128-661, 16 heads of 64, 4 of keys: 20 us.
-template <int D, bool CAUSAL>
-__global__ __launch_bounds__(256, 2) void packed_fwd_kernel(PackedAttention p, int slots) {
+// G groups of four waves have the same queries and every G-th tile of keys, in tiles of their own; their parts are joined at the end.
+template <int D, bool CAUSAL, int G>
+__global__ __launch_bounds__(256 * G, 2) void packed_fwd_kernel(PackedAttention p, int slots) {
   constexpr int KK = D / 16, DB = D / 32;
-  __shared__ __attribute__((aligned(1024))) bf16_t tiles[2][2][Tile<D>::SIZE];   // [buffer][K, V]
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), ql = lane & 31, h = lane >> 5;
+  __shared__ __attribute__((aligned(1024))) bf16_t all_tiles[G][2][2][Tile<D>::SIZE];   // [group][buffer][K, V]
+  const int tid = threadIdx.x, lane = tid & 63, all = __builtin_amdgcn_readfirstlane(tid >> 6), ql = lane & 31, h = lane >> 5;
+  const int g = all >> 2, wave = all & 3;
+  auto& tiles = all_tiles[g];
   PackedPlace w;
   if (!packed_place<BM, CAUSAL>(p, slots, blockIdx.x, w)) return;
   const int w0 = w.row + wave * 32, qi = w0 + ql, qc = min(qi, w.n - 1);
@@ -246,25 +249,48 @@ __global__ __launch_bounds__(256, 2) void packed_fwd_kernel(PackedAttention p, i
     s[0] = next[0];
     s[1] = next[1];
   };
-  fetch_k(0, 0);
-  fetch_v(0, 0);
-  if (TK < kend) fetch_k(TK, 1);
+  constexpr int NEXT = G * TK;                        // from a tile of the group to its next one
+  int k0 = g * TK, buf = 0;
+  if (k0 < kend) {
+    fetch_k(k0, 0);
+    fetch_v(k0, 0);
+  }
+  if (k0 + NEXT < kend) fetch_k(k0 + NEXT, 1);
   landed();
-  if (w0 < w.n) scores(0, s);
+  if (w0 < w.n) scores(0, s);                         // (of a group without a tile: unused)
   meet();                                             // the first tile of K is used up
-  // the tiles that this wave's queries see, then those that only other waves' do
+  // the tiles that this wave's queries see, then those that only other waves' do, as many turns for each group
   const int seen = w0 >= w.n ? 0 : CAUSAL ? min(kend, w0 + 32) : kend;
-  int k0 = 0, buf = 0;
+  const int turns = (kend + NEXT - 1) / NEXT;
+  int done = 0;
   auto turn = [&]() __attribute__((always_inline)) {
-    if (k0 > 0) landed();
-    if (k0 + 2 * TK < kend) fetch_k(k0 + 2 * TK, buf);
-    if (k0 + TK < kend) fetch_v(k0 + TK, buf ^ 1);
+    if (done > 0) landed();
+    if (k0 + 2 * NEXT < kend) fetch_k(k0 + 2 * NEXT, buf);
+    if (k0 + NEXT < kend) fetch_v(k0 + NEXT, buf ^ 1);
   };
-  for (; k0 < seen; k0 += TK, buf ^= 1) {
+  for (; k0 < seen; k0 += NEXT, buf ^= 1, ++done) {
     turn();
     step(k0, buf);
   }
-  for (; k0 < kend; k0 += TK, buf ^= 1) turn();
+  for (; done < turns; k0 += NEXT, buf ^= 1, ++done) turn();
+  if constexpr (G == 2) {                             // the other group's part
+    float* const part = (float*)&all_tiles[0] + (wave * (16 * DB + 2)) * 64 + lane;
+    static_assert((16 * DB + 2) * 4 * 64 * sizeof(float) <= sizeof(all_tiles));
+    __syncthreads();
+    if (g == 1) {
+#pragma unroll
+      for (int i = 0; i < 16 * DB; ++i) part[i * 64] = o[i / 16][i & 15];
+      part[16 * DB * 64] = m;
+      part[(16 * DB + 1) * 64] = l;
+    }
+    __syncthreads();
+    if (g == 1) return;
+    const float m1 = part[16 * DB * 64], top = fmaxf(m, m1), f0 = fast_exp2((m - top) * c2), f1 = fast_exp2((m1 - top) * c2);
+#pragma unroll
+    for (int i = 0; i < 16 * DB; ++i) o[i / 16][i & 15] = fmaf(part[i * 64], f1, o[i / 16][i & 15] * f0);
+    l = fmaf(part[(16 * DB + 1) * 64], f1, l * f0);
+    m = top;
+  }
   if (qi < w.n) {
     store_rows<D>((bf16_t*)p.out + (w.first + qi) * p.ldo + w.head * D, o, h, 1.f / l);
     if (h == 0) p.lse[(int64_t)w.head * p.T + w.first + qi] = m * p.scale + __logf(l);
@@ -696,8 +722,16 @@ template <int D>
 void launch_fwd(const PackedAttention& p, int causal, hipStream_t st) {
   const int slots = packed_slots(p.T, p.n_seq, BM);
   const dim3 grid(packed_blocks(slots, p.n_kv_heads, p.n_heads / p.n_kv_heads));
-  if (causal) hipLaunchKernelGGL((packed_fwd_kernel<D, true>), grid, dim3(256), 0, st, p, slots);
-  else hipLaunchKernelGGL((packed_fwd_kernel<D, false>), grid, dim3(256), 0, st, p, slots);
+  // Few blocks of long rows: two groups of waves to the same queries.  One and two, us, sequences x rows, query heads (blocks), heads of 64:
+  // behind a mask 1x1024, 12 (108) 19.3 and 17.0, 2x2048, 12 (408) 34.0 and 28.9, 16 (544) 35.5 and 34.4, 8x512, 12 (480) 14.4 and 17.6, 2 (80)
+  // 12.6 and 12.1, 2x256, 2 (12) 9.0 and 9.4; without 1x1024, 16 (144) 19.3 and 17.2, 2x2048, 12 46.9 and 50.1; heads of 128: 1x1024 26.9 and 25.2.
+  if (grid.x <= (causal ? 448u : 256u) && p.T >= (int64_t)p.n_seq * 640) {
+    if (causal) hipLaunchKernelGGL((packed_fwd_kernel<D, true, 2>), grid, dim3(512), 0, st, p, slots);
+    else hipLaunchKernelGGL((packed_fwd_kernel<D, false, 2>), grid, dim3(512), 0, st, p, slots);
+    return;
+  }
+  if (causal) hipLaunchKernelGGL((packed_fwd_kernel<D, true, 1>), grid, dim3(256), 0, st, p, slots);
+  else hipLaunchKernelGGL((packed_fwd_kernel<D, false, 1>), grid, dim3(256), 0, st, p, slots);
 }
 template <int D, bool CAUSAL>
 void launch_bwd(const PackedAttention& p, hipStream_t st) {

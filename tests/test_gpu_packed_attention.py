@@ -110,7 +110,8 @@ def test_lengths(dtype, h, hk, d, lengths, causal):
 WAYS = [(1, 12, 12, 64, [70] * 24), (1, 12, 12, 32, [40] * 40), (1, 8, 2, 64, [190]), (1, 6, 6, 64, [190, 3]), (1, 8, 2, 32, [200, 129]), (1, 2, 1, 128, [65, 140]),
         (1, 8, 2, 128, [190, 1]), (1, 6, 6, 128, [300]), (0, 12, 12, 64, [33] * 28), (0, 16, 16, 32, [33] * 64), (0, 8, 8, 128, [33] * 20), (0, 2, 1, 128, [400, 31]),
         (0, 4, 4, 64, [500, 0, 65]), (0, 12, 12, 64, [33] * 40), (0, 12, 12, 64, [33] * 50), (0, 8, 8, 128, [33] * 32), (0, 8, 8, 128, [33] * 42),
-        (0, 8, 2, 128, [200] * 8), (0, 8, 2, 64, [200] * 9), (0, 16, 4, 32, [150] * 9)]
+        (0, 8, 2, 128, [200] * 8), (0, 8, 2, 64, [200] * 9), (0, 16, 4, 32, [150] * 9), (1, 2, 1, 64, [700]),
+        (1, 4, 2, 128, [650, 700]), (1, 2, 2, 32, [1000]), (1, 1, 1, 64, [641, 640])]
 
 
 @pytest.mark.parametrize("causal", [1, 0])
