@@ -696,7 +696,7 @@ class MuonTable:
                 if x is None or x.shape != shape or x.dtype != dtype or not x.is_contiguous() or not x.is_cuda or x.device != device:
                     raise ValueError(f"{name}: a contiguous tensor of shape {tuple(shape)} of {dtype} on the list's one device is required")
                 setattr(e, name, x.data_ptr() or None)
-            e.rows, e.cols = shape
+            e.rows, e.cols = (min(n, 2**31 - 1) for n in shape)   # (a side that 32 bits do not hold is one that the library refuses)
         nbytes = mimose_op_muon_table_bytes(entries, parts)
         if stream is None:
             stream = torch.cuda.current_stream(device).cuda_stream
