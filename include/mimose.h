@@ -542,15 +542,18 @@ int mimose_op_adamw_step(const mimose_adamw_table* table, const mimose_adamw_cfg
  *     X = u / (|u| + eps), |u| the root of the sum of squares;   cfg.iterations times X <- a X + b A X + c A A X with A = X X^T
  *         (A = X^T X from the right where rows > cols; a, b, c = 3.4445, -4.7750, 2.0315)
  *     master <- master - lr (rms sqrt(max(rows, cols)) X + weight_decay master)
- * so that a step's elements are about lr rms large.  X, A and b A + c A A are held in fp16 (times 2^10) between products, sums in fp32:
- * X is 0.1 to 0.7 % off the exact one (2-norm), most where its singular values reach over orders of magnitude.  All zeros is the
+ * so that a step's elements are about lr rms large.  X, A and a I + b A + c A A are held in fp16 (times 2^10) between products, sums in fp32:
+ * after five iterations X is 0.1 to 0.7 % off the exact one (2-norm), most where its singular values reach over orders of magnitude (of
+ * what is 0 but for rounding an iteration makes 3.4 times as much).  All zeros is the
  * initial momentum.  Pointers 16-byte aligned; sides up to 2^20; a matrix may be empty; no matrix may share memory that is written
  * with another.
  * mimose_op_muon_table lays a list out in device memory of mimose_op_muon_table_bytes (0: the list is refused) and waits for the
  * copy; the table holds the addresses, not the tensors.  A step works on the matrices in parts, in the list's order, one after the
- * other in one scratch: the fewer, the fuller the device, the more, the smaller the scratch (parts: at most so many, 1 to 64; about
- * 8 bytes for each element of the largest part).  mimose_op_muon_step needs 16-byte aligned scratch of table->workspace_bytes,
- * whose content it neither needs nor keeps.
+ * other in one scratch: the fewer, the fuller the device, the more, the smaller the scratch (parts: at most so many, 1 to 64).  A
+ * matrix needs 4 S (S + L) bytes and up to 8 KB, S and L its shorter and its longer side rounded up to 128, and none up to 128 x 256: 8
+ * bytes for each element of a large square one, 5 of 1024 x 4096, but 72 of 8 x 1024; the scratch is that of the part with most.
+ * mimose_op_muon_step needs 16-byte aligned scratch of table->workspace_bytes, whose content it neither needs nor keeps.
+ * lr, weight_decay, rms >= 0, momentum from 0 to below 1, eps >= 1e-30, all finite; 1 to 64 iterations.
  */
 typedef struct {
   float* master; void* lowp; const float* grad; float* momentum;

@@ -733,10 +733,13 @@ class MuonTable:
     """The device table and the scratch of a list of matrices, for mimose_op_muon_step; keeps the tensors alive.
 
     matrices: dicts of contiguous tensors [rows, cols] of one device, master, grad, momentum (fp32) and lowp (bf16 or None).
-    parts: a step works on the list in at most so many parts, in a scratch that is that much smaller (about 8 bytes for each element
-    of the largest part).  stream (an address; None: torch's current one) is the one that steps run on; a step on another has to have
-    ended before the table is let go, and two steps that run at once need a workspace each.  Like AdamWTable it holds addresses:
-    gradients have to be written in place."""
+    parts: a step works on the list in at most so many parts, in a scratch that is that much smaller: that of the part with most, where a matrix
+    takes 4 S (S + L) bytes, S and L its shorter and its longer side rounded up to 128, and none up to 128 x 256.  stream (an address; None:
+    torch's current one) is the one that steps run on; a step on another has to have ended before the table is let go, and two steps that
+    run at once need a workspace each.
+
+    Made once, where the tensors stay where they are: 12 matrices take 0.07 ms, 72 0.44, 144 (264 M elements, whose step takes 6.1) 0.68.
+    Like AdamWTable it holds addresses: gradients have to be written in place."""
 
     def __init__(self, matrices, parts: int = 1, stream=None):
         import torch

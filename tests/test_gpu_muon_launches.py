@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import paper_2209_02478_amd as mi
-from gpu_util import sync
+from gpu_util import DEV, sync
 from test_gpu_muon import HYPER, check, matrix
 
 pytestmark = pytest.mark.gpu
@@ -81,3 +81,15 @@ def test_what_is_not_a_number_stays_in_its_matrix(parts, wrong):
     for i in (0, 2, 3, 4):
         assert torch.isfinite(ms[i]["master"]).all()
         assert all(torch.equal(ms[i][k], alone[i][k]) for k in ms[i])
+
+
+@pytest.mark.parametrize("shape", [(8, 1024), (1024, 8), (1, 4096), (129, 129), (128, 257), (1024, 1024), (1024, 4096), (768, 130)])
+def test_scratch_is_what_the_header_says(shape):
+    table = mi.MuonTable([{k: torch.zeros(shape, device=DEV) for k in ("master", "grad", "momentum")} for _ in range(3)], parts=3)
+    S, L = (-(-n // 128) * 128 for n in sorted(shape))
+    assert table.table.parts == 3 and 4 * S * (S + L) < table.workspace.numel() <= 4 * S * (S + L) + 8192
+
+
+def test_no_scratch_for_matrices_of_one_block():
+    table = mi.MuonTable([{k: torch.zeros(s, device=DEV) for k in ("master", "grad", "momentum")} for s in ((128, 256), (256, 128), (3, 5))])
+    assert table.workspace.numel() == 16
