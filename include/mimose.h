@@ -543,10 +543,11 @@ int mimose_op_adamw_step(const mimose_adamw_table* table, const mimose_adamw_cfg
  *         (A = X^T X from the right where rows > cols; a, b, c = 3.4445, -4.7750, 2.0315)
  *     master <- master - lr (rms sqrt(max(rows, cols)) X + weight_decay master)
  * so that a step's elements are about lr rms large.  X, A and a I + b A + c A A are held in fp16 (times 2^10) between products, sums in fp32:
- * after five iterations X is 0.1 to 0.7 % off the exact one (2-norm), most where its singular values reach over orders of magnitude (of
- * what is 0 but for rounding an iteration makes 3.4 times as much).  All zeros is the
- * initial momentum.  Pointers 16-byte aligned; sides up to 2^20; a matrix may be empty; no matrix may share memory that is written
- * with another.
+ * after five iterations X of full rank is 0.1 to 0.7 % off the exact one (2-norm of its elements), most where its singular values
+ * reach over orders of magnitude.  What would be 0 but for rounding grows 3.4-fold in an iteration, to singular values of 0.01 to
+ * 0.03, so that X of low rank is further off: 768 x 768 of rank 64 by 2.3 %, of 17 by 4.5, of 1 by 15.  All zeros is the initial
+ * momentum.  Pointers 16-byte aligned; sides up to 2^20; a matrix may be empty; no matrix may share memory that is written with
+ * another.
  * mimose_op_muon_table lays a list out in device memory of mimose_op_muon_table_bytes (0: the list is refused) and waits for the
  * copy; the table holds the addresses, not the tensors.  A step works on the matrices in parts, in the list's order, one after the
  * other in one scratch: the fewer, the fuller the device, the more, the smaller the scratch (parts: at most so many, 1 to 64).  A

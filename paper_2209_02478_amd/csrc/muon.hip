@@ -7,7 +7,9 @@
 // The polynomial takes every singular value of X from (0, 1] near 1 and keeps it below 1.21, so that no element of X, A or B
 // is above 1.21, 1.47 and 11.  The products' operands are therefore held in fp16 times 2^10: as many bits as any 16-bit type has
 // (values from 6e-8 of the largest on keep all eleven; bf16 keeps eight, and the step is then 1 to 5 % off instead of 0.1 to
-// 0.6), at the same rate of the matrix units.  Sums are fp32, the norm's fp64 (squares of gradients of 1e-20 are numbers there).
+// 0.6), at the same rate of the matrix units.  That is of full rank: a rounding's part outside of X's singular directions grows 3.44-fold in an
+// iteration, five of them make it 0.01 to 0.03 large there, and X of rank 64, 17 or 1 (768 x 768) is 2.3, 4.5 or 15 % off.
+// Sums are fp32, the norm's fp64 (squares of gradients of 1e-20 are numbers there).
 // A and A A are symmetric: only tiles on and above the diagonal are multiplied, and stored twice.  What is held of an iteration's
 // factor is B = a I + b A + c A A, so that X' = B X: a X beside the product would be read again, and the error is the same
 // (0.13 and 0.64 % either way for gradients of 768 x 768 from a normal distribution and with few large directions).

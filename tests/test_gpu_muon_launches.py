@@ -93,3 +93,15 @@ def test_scratch_is_what_the_header_says(shape):
 def test_no_scratch_for_matrices_of_one_block():
     table = mi.MuonTable([{k: torch.zeros(s, device=DEV) for k in ("master", "grad", "momentum")} for s in ((128, 256), (256, 128), (3, 5))])
     assert table.workspace.numel() == 16
+
+
+@pytest.mark.parametrize("rank", [1, 4, 17])
+@pytest.mark.parametrize("shape", [(60, 140), (131, 301), (301, 131)], ids=str)
+def test_gradients_of_low_rank(shape, rank):
+    """The gradient of as few tokens: most singular values are 0 but for rounding, which the bound follows through the iterations."""
+    t = matrix(shape, rank)
+    g = torch.Generator().manual_seed(rank)
+    u = torch.randn(shape[0], rank, generator=g, dtype=torch.float64) @ torch.randn(rank, shape[1], generator=g, dtype=torch.float64)
+    t["grad"].copy_(u)
+    t["momentum"].zero_()
+    check([t], mi.MuonTable([t]))
