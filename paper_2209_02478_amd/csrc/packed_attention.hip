@@ -150,10 +150,12 @@ __device__ __forceinline__ void store_rows(bf16_t* dst, const f32x16 (&acc)[D / 
 
 // ------------------------------------------------------------------ forward
 // 32 queries to a wave, which holds its part of Q in registers; the scores of a tile are made while the exponentials of the one before are
-// taken, which is what bounds it: with heads of 64 exponentials and their neighbours need two issue slots for each of the matrix
-// units', with heads of 128 as many (there 44 % and 53 % of the time is theirs).  6 causal sequences of 1000-4096 rows, 16 heads of
-// 128, 4 of keys: 215 us, 0.87 PFLOP/s of the pairs that see each other (scores not made ahead: 229); 32 sequences of 153-512 without mask,
-// 12 heads of 64: 32 us; 16 causal ones of 128-661, 16 heads of 64, 4 of keys: 20 us.
+// taken.  With heads of 64 exponentials and their neighbours need two issue slots for each of the matrix units', with heads of 128 as many.
+// 6 causal sequences of 1000-4096 rows, 16 heads of 128, 4 of keys: 215 to 227 us by card, 0.87 to 0.83 PFLOP/s of the pairs that see each
+// other (scores not made ahead: 229 beside 215); 32 sequences of 153-512 without mask, 12 heads of 64: 33 to 34 us; 16 causal ones of 128-661, 16
+// heads of 64, 4 of keys: 21.  Neither pipe is full: of a wave's cycles 41 % (16 sequences), 35 % (32) and 20 % (6) go by in waits for loads and
+// meetings, 28, 30 and 39 % in waits for its turn to issue, 30, 35 and 41 % in instructions.  Nor is it the longest sequence's chain alone: that
+// sequence by itself takes 12, 11 and 91 us.
 // G groups of four waves have the same queries and every G-th tile of keys, in tiles of their own; their parts are joined at the end.
 template <int D, bool CAUSAL, int G>
 __global__ __launch_bounds__(256 * G, 2) void packed_fwd_kernel(PackedAttention p, int slots) {
@@ -725,6 +727,8 @@ void launch_fwd(const PackedAttention& p, int causal, hipStream_t st) {
   // Few blocks of long rows: two groups of waves to the same queries.  One and two, us, sequences x rows, query heads (blocks), heads of 64:
   // behind a mask 1x1024, 12 (108) 19.3 and 17.0, 2x2048, 12 (408) 34.0 and 28.9, 16 (544) 35.5 and 34.4, 8x512, 12 (480) 14.4 and 17.6, 2 (80)
   // 12.6 and 12.1, 2x256, 2 (12) 9.0 and 9.4; without 1x1024, 16 (144) 19.3 and 17.2, 2x2048, 12 46.9 and 50.1; heads of 128: 1x1024 26.9 and 25.2.
+  // The rows of a sequence are taken to be T / n_seq, since lengths are the device's: of one long sequence among short ones this keeps one
+  // group where two would be faster (4 heads of 64, 4096 beside 15 of 16 rows 54 and 43, 1024 beside 15 17.8 and 15.7).
   if (grid.x <= (causal ? 448u : 256u) && p.T >= (int64_t)p.n_seq * 640) {
     if (causal) hipLaunchKernelGGL((packed_fwd_kernel<D, true, 2>), grid, dim3(512), 0, st, p, slots);
     else hipLaunchKernelGGL((packed_fwd_kernel<D, false, 2>), grid, dim3(512), 0, st, p, slots);
@@ -742,6 +746,10 @@ void launch_bwd(const PackedAttention& p, hipStream_t st) {
   // of keys, and few blocks.  One launch and two, us, sequences x rows, query heads / heads of keys: heads of 64, 12 / 12: 4x64 7.7 and
   // 12.7, 1x1024 26.6 and 35.3, 8x256 23.5 and 25.0, 8x512 49.8 and 42.9; 16 / 4: 4x64 10.8 and 13.8, 8x128 17.4 and 18.0, 2x256 25.9
   // and 22.9, 1x1024 82.7 and 57.3; heads of 128, 12 / 12: 2x256 19.4 and 24.5, 8x128 23.1 and 20.3; 16 / 4: 1x16 15.1 and 12.8.
+  // Rows to a sequence are taken to be T / n_seq.  One long sequence among short ones, one launch and two, heads of 64, 4 / 4: 4096 beside 15 of
+  // 16 rows 83 and 102 (one is taken), 1024 beside 15 25.4 and 34.4 (one); 4 / 2: 160 and 132 (two), 44.1 and 41.6 (one); heads of 128, 2 / 2: 179
+  // and 183 (one).  A buffer of eight times the rows, and four times the sequences, all empty: 12 / 12 2x512 29.3 instead of 17.1, 8x256 21.3
+  // instead of 23.8, 16 / 4 8x128 18.6 instead of 17.3.
   const bool few = (int64_t)p.T * group <= (int64_t)p.n_seq * (group == 1 ? 1024 : 512) &&
                    (D == 128 ? group <= 2 && queries + keys <= 320 : queries + keys <= 1024);
   if (few) {

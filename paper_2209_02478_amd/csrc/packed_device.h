@@ -35,7 +35,9 @@ __device__ __forceinline__ int rotated(int v) { return __builtin_amdgcn_update_d
 // the block's w is the largest with S(w) > slot, by bisection.  Else the longest sequence's blocks first, which share the rows they stream.
 // Against slots in the order of the rows, us: 16 causal sequences of 128-661 rows, 16 heads of 64: forward 25.2 -> 21.1, dQ 29.2 -> 25.6,
 // dK/dV 45.5 -> 32.9; 6 of 1000-4096, heads of 128: 240 -> 226, 313 -> 298, 822 -> 746; fp32, 12 of 153-397 without mask: dQ 80.8 -> 74.3,
-// dK/dV 107 -> 97.5.
+// dK/dV 107 -> 97.5.  Of 64 sequences, the most that a wave has lanes for, it gains and loses: 64 causal ones of 128-661, slots and this, forward
+// and backward: 16 / 4 heads of 64 57 -> 59 and 184 -> 160, of 128 103 -> 106 and 332 -> 320; 12 / 12 of 64 49 -> 60 and 157 -> 169, fp32 422 -> 428
+// and 740 -> 704.
 template <int M, bool BY_WORK>
 __device__ __forceinline__ bool packed_sorted(const PackedAttention& p, int slot, bool own_keys, PackedPlace& w) {
   const int lane = threadIdx.x & 63;
